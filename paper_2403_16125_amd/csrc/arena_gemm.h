@@ -1,0 +1,652 @@
+// Tiled matrix products on the matrix cores, with the epilogues of the layer
+// operators.  C[m, n] = sum_k A(m, k) B(n, k), 16-bit operands, 32-bit sums.
+//
+// Each operand lies either with k contiguous (row m or n of ld elements) or
+// with m or n contiguous (row k of ld elements), so the forward, data-gradient
+// and weight-gradient products of a layer read the tensors as they are: no
+// transposed copies.
+//
+// A block computes a BM x BN tile with WM x WN waves, 64 of k at a time, from
+// two LDS buffers: while one is multiplied, the other is filled by direct
+// global-to-LDS loads.  Those write 16 bytes per lane in lane order, so the
+// bank swizzle sits on the global side (which chunk a lane fetches):
+//   k contiguous: row r of 8 chunks; position p holds chunk p ^ (r & 7), and a
+//     fragment read (16 rows, one chunk each) meets every bank once;
+//   m or n contiguous: row k of R / 16 granules of 32 bytes; position q holds
+//     granule q ^ f(k), f = (k & 3) | ((k >> 3) & 3) << 2, so the 16 rows that
+//     one transposing read touches lie in different granules.
+// The product is formed transposed (the B fragment is the first operand), so a
+// lane holds four neighbouring columns of one row of C.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "arena_layer_internal.h"
+
+namespace arena {
+namespace mm {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+    typedef __bf16 E;
+    typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 V4 __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x4 mfma(V8 a, V8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+struct F16 {
+    typedef _Float16 E;
+    typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 V4 __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x4 mfma(V8 a, V8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// act(z) and act'(z).
+__device__ __forceinline__ float act_value(float z, int act)
+{
+    if (act == kSilu) return z / (1.0f + __expf(-z));
+    if (act == kGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    return z > 0.0f ? z : (z == z ? 0.0f : z);
+}
+
+__device__ __forceinline__ void act_both(float z, int act, float* v, float* d)
+{
+    if (act == kSilu) {
+        const float s = 1.0f / (1.0f + __expf(-z));
+        *v = z * s;
+        *d = s * (1.0f + z * (1.0f - s));
+    } else if (act == kGelu) {
+        const float c = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+        *v = z * c;
+        *d = c + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    } else {
+        *v = z > 0.0f ? z : (z == z ? 0.0f : z);
+        *d = z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
+    }
+}
+
+__device__ const u32x4 g_zero_chunk = {0, 0, 0, 0};   // what a lane past the end of k fetches
+
+typedef __attribute__((address_space(1))) const void GlobalVoid;
+typedef __attribute__((address_space(3))) void LdsVoid;
+
+__device__ __forceinline__ void load_to_lds(const char* src, char* dst)
+{
+    __builtin_amdgcn_global_load_lds((GlobalVoid*)src, (LdsVoid*)dst, 16, 0, 0);
+}
+
+// Which matrix and row a row of the B tile is.  The gated forward product
+// interleaves 32 gate and 32 up features, so one wave holds both of a feature.
+template <bool DUAL>
+__device__ __forceinline__ int tile_row(int r)
+{
+    return DUAL ? ((r >> 6) << 5) + (r & 31) : r;
+}
+
+// One operand's share of a tile: R rows of C (or columns) x 64 of k.
+template <typename P, int R, bool TR, bool DUAL>
+struct Loader {
+    static constexpr int kThreads = P::kThreads;
+    static constexpr int kChunks = R * 8 / kThreads;
+    static constexpr int kGran = R / 16;
+    uint32_t off[kChunks];   // byte offset of this lane's chunk from the segment's base at step 0
+    int64_t step;            // bytes from one step to the next
+    int row0, ld;
+
+    static __device__ __forceinline__ int k_of(int it, int tid)   // k of the chunk within the step
+    {
+        if (TR) return (it * kThreads + tid) / (R / 8);
+        const int r = it * (kThreads / 8) + (tid >> 3);
+        return ((tid & 7) ^ (r & 7)) * 8;
+    }
+
+    __device__ __forceinline__ void init(int tid, int first, int n, int64_t ld_)
+    {
+        ld = (int)ld_;
+        row0 = first;
+        step = TR ? ld_ * (2 * kBK) : 2 * kBK;
+#pragma unroll
+        for (int it = 0; it < kChunks; ++it) {
+            if (TR) {
+                const int c = it * kThreads + tid;
+                const int k = c / (R / 8), pos = c % (R / 8);
+                const int f = ((k & 3) | (((k >> 3) & 3) << 2)) & (kGran - 1);
+                int col = first + (((pos >> 1) ^ f) << 4) + ((pos & 1) << 3);
+                if (col >= n) col = 0;
+                off[it] = (uint32_t)k * (uint32_t)(ld * 2) + (uint32_t)col * 2;
+            } else {
+                const int r = it * (kThreads / 8) + (tid >> 3);
+                const int row = min(first + tile_row<DUAL>(r), n - 1) - first;
+                off[it] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(((tid & 7) ^ (r & 7)) << 4);
+            }
+        }
+    }
+
+    // base of step 0 of a segment
+    __device__ __forceinline__ const char* base(const void* p, int64_t batch) const
+    {
+        const char* q = (const char*)p + 2 * batch;
+        return TR ? q : q + 2 * (int64_t)row0 * ld;
+    }
+
+    template <bool TAIL>
+    __device__ __forceinline__ void fetch(const char* p0, const char* p1, char* lds, int tid, int left) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+        for (int it = 0; it < kChunks; ++it) {
+            const char* p = p0;
+            if (DUAL) p = ((it * (kThreads / 8) + wave * 8) >> 5) & 1 ? p1 : p0;
+            const char* src = p + off[it];
+            if (TAIL && k_of(it, tid) >= left) src = (const char*)&g_zero_chunk;
+            load_to_lds(src, lds + (it * kThreads + wave * 64) * 16);
+        }
+    }
+};
+
+// A wave's fragment reader: 16 rows x 32 of k for one MFMA.
+template <typename P, int R, bool TR>
+struct Frags {
+    typedef typename P::T::V8 V8;
+    typedef typename P::T::V4 V4;
+    int lo;      // byte address of fragment 0, first half of the step
+    __device__ __forceinline__ void init(int lane, int row)
+    {
+        if (TR) {
+            const int i = lane & 15, g = lane >> 4;
+            const int f = ((i >> 2) | (g << 2)) & (R / 16 - 1);
+            lo = (g * 8 + (i >> 2)) * (R * 2) + (((row >> 4) ^ f) << 5) + (i & 3) * 8;
+        } else {
+            const int r = row + (lane & 15);
+            lo = r * 128 + (((lane >> 4) ^ (r & 7)) << 4);
+        }
+    }
+    // fragment i (rows row + 16 i), half kk of the step
+    __device__ __forceinline__ V8 get(const char* lds, int i, int kk) const
+    {
+        if (TR) {
+            typedef __attribute__((address_space(3))) s16x4 LdsV;
+            const char* p = lds + ((lo ^ (i << 5)) + kk * 32 * (R * 2));
+            union { s16x4 s[2]; V8 v; } w;
+            w.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV*)p);
+            w.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV*)(p + 4 * (R * 2)));
+            return w.v;
+        }
+        return *(const V8*)(lds + ((lo ^ (kk << 6)) + i * 2048));
+    }
+};
+
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool ATR_, bool BTR_, int EPI_>
+struct Tile {
+    typedef T_ T;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
+    static constexpr int EPI = EPI_;
+    static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    static constexpr int kCols = DUAL ? BN / 2 : BN;     // columns of C of a tile
+    static_assert(!DUAL || BN / WN == 64, "a wave of the gated product holds 32 gate and 32 up features");
+};
+
+template <typename E>
+__device__ __forceinline__ void store4(E* p, f32x4 v, int left, bool vec)
+{
+    typedef E E4 __attribute__((ext_vector_type(4)));
+    if (vec && left >= 4) {
+        E4 w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = (E)v[r];
+        *(E4*)p = w;
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) p[r] = (E)v[r];
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ f32x4 load4(const E* p, int left, bool vec)
+{
+    typedef E E4 __attribute__((ext_vector_type(4)));
+    f32x4 v = {0, 0, 0, 0};
+    if (vec && left >= 4) {
+        const E4 w = *(const E4*)p;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (float)w[r];
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) v[r] = (float)p[r];
+    }
+    return v;
+}
+
+// Writes four columns (n .. n + 3, those below N) of row m; z is the batch index.
+template <typename T>
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, f32x4 v, bool mirror)
+{
+    typedef typename T::E E;
+    const int left = A.N - n;
+    const int64_t at = (A.pairs ? 0 : z * A.sc) + (int64_t)m * A.ldc + n;
+    void* c = A.c[A.pairs ? z : 0];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] *= A.alpha;
+    if (A.beta != 0.0f) {
+        const void* p = A.e[A.pairs ? z : 0];
+        const int64_t from = (A.pairs ? 0 : z * A.se) + (int64_t)m * A.lde + n;
+        const f32x4 e = A.out == kOutF32 ? load4((const float*)p + from, left, A.vec)
+                                         : load4((const E*)p + from, left, A.vec);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += A.beta * e[r];
+    }
+    if (A.diag != 0.0f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (m == n + r) v[r] -= A.diag;
+    if (A.out == kOutF32) store4((float*)c + at, v, left, A.vec);
+    else if (A.out == kOutBf16) store4((__bf16*)c + at, v, left, A.vec);
+    else store4((E*)c + at, v, left, A.vec);
+    if (mirror) {
+        E* q = (E*)c + z * A.sc + (int64_t)n * A.ldc + m;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) q[(int64_t)r * A.ldc] = (E)v[r];
+    }
+}
+
+// Values kept for the backward pass: the upper 24 bits of a float, 16 in a row
+// of heads and 8 in a row of tails (all rows of heads, then all of tails).  In
+// 16 bits they would cost the gradients two more roundings of the operands'
+// size (1.8 times the error of one rounding of the result instead of 1.4); the
+// tails are a sixth of the bytes that the pass writes here.
+__device__ __forceinline__ void store24(void* p, const GemmArgs& A, int m, int n, f32x4 v)
+{
+    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
+    const int64_t at = (int64_t)m * A.ldg + n;
+    U4 head;
+    uint32_t tail = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t b = __float_as_uint(v[r]);
+        head[r] = (uint16_t)(b >> 16);
+        tail |= ((b >> 8) & 0xffu) << (8 * r);
+    }
+    *(U4*)((uint16_t*)p + at) = head;
+    *(uint32_t*)((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at) = tail;
+}
+
+__device__ __forceinline__ f32x4 load24(const void* p, const GemmArgs& A, int m, int n)
+{
+    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
+    const int64_t at = (int64_t)m * A.ldg + n;
+    const U4 head = *(const U4*)((const uint16_t*)p + at);
+    const uint32_t tail = *(const uint32_t*)((const uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at);
+    f32x4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = __uint_as_float((uint32_t)head[r] << 16 | ((tail >> (8 * r)) & 0xffu) << 8);
+    return v;
+}
+
+// h = act(g) u from the 32-bit sums, rounded to 16 bits as the next product's operand.
+template <typename T>
+__device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, f32x4 g, f32x4 u)
+{
+    typedef typename T::E E;
+    f32x4 h;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const bool in = n + r < A.N;
+        g[r] = in ? g[r] : 0.0f;
+        u[r] = in ? u[r] : 0.0f;
+        h[r] = in ? act_value(g[r], A.act) * u[r] : 0.0f;
+    }
+    store4((E*)A.c[0] + (int64_t)m * A.ldc + n, h, 4, true);
+    if (A.g) {
+        store24(A.g, A, m, n, g);
+        store24(A.u, A, m, n, u);
+    }
+}
+
+// v = the gradient of h = act(g) u:  of g  v u act'(g),  of u  v act(g).
+template <typename T>
+__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, f32x4 v)
+{
+    typedef typename T::E E;
+    const f32x4 g = load24(A.g, A, m, n), u = load24(A.u, A, m, n);
+    f32x4 dg, du;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const bool in = n + r < A.N;
+        float a, d;
+        act_both(g[r], A.act, &a, &d);
+        du[r] = in ? v[r] * a : 0.0f;
+        dg[r] = in ? v[r] * u[r] * d : 0.0f;
+    }
+    store4((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, 4, true);
+    store4((E*)A.c[1] + (int64_t)m * A.ldc + n, du, 4, true);
+}
+
+// Tile of a block: blocks go to the 8 XCDs in turn, so each XCD gets a run of
+// consecutive tiles (its L2 then holds the operands that they share), taken in
+// bands of 8 tile rows.
+__device__ __forceinline__ void tile_of(int bid, int n_blocks, int tiles_m, int tiles_n, bool sym, int* tm, int* tn)
+{
+    const int per = n_blocks >> 3, more = n_blocks & 7;
+    const int x = bid & 7, i = bid >> 3;
+    const int t = x * per + min(x, more) + i;
+    if (sym) {
+        int r = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+        while (r * (r + 1) / 2 > t) --r;
+        while ((r + 1) * (r + 2) / 2 <= t) ++r;
+        *tm = r;
+        *tn = t - r * (r + 1) / 2;
+        return;
+    }
+    const int band = 8 * tiles_n, b = t / band, in = t - b * band;
+    const int rows = min(8, tiles_m - b * 8);
+    *tm = b * 8 + in % rows;
+    *tn = in / rows;
+}
+
+template <typename P>
+__global__ __launch_bounds__(P::kThreads, 2) void gemm_kernel(const GemmArgs A)
+{
+    typedef typename P::T T;
+    __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
+    __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
+    __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
+    __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / P::WN, wn = wave % P::WN;
+    int tm, tn;
+    tile_of(blockIdx.x, gridDim.x, A.tiles_m, A.tiles_n, A.sym, &tm, &tn);
+    const int zb = blockIdx.y;                 // batch index
+    const int m0 = tm * P::BM, n0 = tn * P::kCols;
+
+    Loader<P, P::BM, P::ATR, false> la;
+    Loader<P, P::BN, P::BTR, P::DUAL> lb;
+    la.init(tid, m0, A.M, A.lda);
+    lb.init(tid, n0, A.N, A.ldb);
+    Frags<P, P::BM, P::ATR> fa;
+    Frags<P, P::BN, P::BTR> fb;
+    fa.init(lane, wm * (P::BM / P::WM));
+    fb.init(lane, wn * (P::BN / P::WN));
+
+    f32x4 acc[P::FM][P::FN];
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+    const int sps = (A.K + kBK - 1) / kBK;     // steps of a segment
+    int s = 0, end = sps * A.nseg;
+    if (A.splits > 1) {
+        s = blockIdx.z * A.per;
+        end = min(end, s + A.per);
+    }
+    const int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
+    const int sel = A.pairs ? zb : 0;
+
+    auto where = [&](int step, const char** pa, const char** pb, const char** pb1, int* left) {
+        int q = step, seg = sel;
+        if (A.nseg == 2 && step >= sps) { q -= sps; seg = 1; }
+        *pa = la.base(A.a[seg], za) + q * la.step;
+        *pb = lb.base(A.b[seg], zB) + q * lb.step;
+        *pb1 = P::DUAL ? lb.base(A.b[1], 0) + q * lb.step : *pb;
+        *left = A.K - q * kBK;
+    };
+    auto fetch = [&](int step, char* sa, char* sb) {
+        const char *pa, *pb, *pb1;
+        int left;
+        where(step, &pa, &pb, &pb1, &left);
+        if (left >= kBK) {
+            la.template fetch<false>(pa, pa, sa, tid, left);
+            lb.template fetch<false>(pb, pb1, sb, tid, left);
+        } else {
+            la.template fetch<true>(pa, pa, sa, tid, left);
+            lb.template fetch<true>(pb, pb1, sb, tid, left);
+        }
+    };
+    auto multiply = [&](const char* sa, const char* sb) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename T::V8 a[P::FM], b[P::FN];
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) b[j] = fb.get(sb, j, kk);
+#pragma unroll
+            for (int i = 0; i < P::FM; ++i) a[i] = fa.get(sa, i, kk);
+#pragma unroll
+            for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < P::FN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);
+        }
+    };
+    // One step: the loads of this step have landed and every wave is done
+    // with the other buffer (one barrier), then the next step's loads start.
+    auto turn = [&](int step, char* sa, char* sb, char* ta, char* tb) {
+        __syncthreads();
+        if (step + 1 < end) fetch(step + 1, ta, tb);
+        multiply(sa, sb);
+    };
+    if (s < end) fetch(s, sa0, sb0);
+    for (; s < end; s += 2) {
+        turn(s, sa0, sb0, sa1, sb1);
+        if (s + 1 < end) turn(s + 1, sa1, sb1, sa0, sb0);
+    }
+
+    // epilogue: lane holds rows m = .. + (lane & 15), columns 4 (lane >> 4) + 0..3 of each fragment
+    const int mr = m0 + wm * (P::BM / P::WM) + (lane & 15);
+    const int nr = n0 + wn * (P::DUAL ? 32 : P::BN / P::WN) + 4 * (lane >> 4);
+    if (A.splits > 1) {
+        const int64_t plane = (int64_t)A.M * A.N;
+        float* out = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1);
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) {
+                const bool up = P::DUAL && j >= P::FN / 2;
+                const int m = mr + i * 16, n = nr + (up ? j - P::FN / 2 : j) * 16;
+                if (m < A.M && n < A.N)
+                    store4(out + (up ? plane : 0) + (int64_t)m * A.N + n, acc[i][j], A.N - n, A.N % 4 == 0);
+            }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = mr + i * 16;
+        if (m >= A.M) continue;
+        if constexpr (P::EPI == kGatedFwd) {
+#pragma unroll
+            for (int j = 0; j < P::FN / 2; ++j) {
+                const int n = nr + j * 16;
+                if (n < A.pad) gated_fwd_out<T>(A, m, n, acc[i][j], acc[i][j + P::FN / 2]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) {
+                const int n = nr + j * 16;
+                if constexpr (P::EPI == kGatedBwd) {
+                    if (n < A.pad) gated_bwd_out<T>(A, m, n, acc[i][j]);
+                } else if (n < A.N) {
+                    plain_out<T>(A, zb, m, n, acc[i][j], A.sym && tm != tn);
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of a split product in their order and applies the epilogue;
+// a thread takes four columns of a row.
+template <typename T, int EPI>
+__global__ __launch_bounds__(256) void join_kernel(const GemmArgs A)
+{
+    const int quads = ((EPI == kPlain ? A.N : A.pad) + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)A.M * quads) return;
+    const int m = (int)(i / quads), n = (int)(i % quads) * 4;
+    const int64_t plane = (int64_t)A.M * A.N, each = plane * A.batch * (EPI == kGatedFwd ? 2 : 1);
+    const float* p = A.part + (int64_t)blockIdx.y * plane * (EPI == kGatedFwd ? 2 : 1) + (int64_t)m * A.N + n;
+    f32x4 v = {0, 0, 0, 0}, u = {0, 0, 0, 0};
+    const bool vec = A.N % 4 == 0;
+    if (n < A.N)
+        for (int s = 0; s < A.splits; ++s) {
+            v += load4(p + s * each, A.N - n, vec);
+            if (EPI == kGatedFwd) u += load4(p + s * each + plane, A.N - n, vec);
+        }
+    if constexpr (EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
+    else if constexpr (EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v);
+    else plain_out<T>(A, blockIdx.y, m, n, v, false);
+}
+
+// Few rows of A (tokens): nothing of B is used twice, so it goes from memory
+// to registers and no LDS tile is filled.  A block takes 16 columns of C, its
+// waves share k, and their sums meet in LDS in the waves' order.  Operands
+// with k contiguous, any alignment.
+template <typename T>
+__device__ __forceinline__ typename T::V8 load_k(const typename T::E* p, int left)
+{
+    typename T::V8 v;
+    if (left >= 8) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename T::E)0.0f;
+    }
+    return v;
+}
+
+template <typename T, int NT, bool DUAL, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
+{
+    typedef typename T::E E;
+    typedef typename T::V8 V8;
+    constexpr int NB = DUAL ? 2 : 1;
+    __shared__ f32x4 part[WAVES][NT * NB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16, kc = (lane >> 4) * 8;
+    const int row = min(n0 + (lane & 15), A.N - 1);
+    const E* w[NB];
+    const E* x[NT];
+    w[0] = (const E*)A.b[0] + (int64_t)row * A.ldb + kc;
+    if (DUAL) w[NB - 1] = (const E*)A.b[1] + (int64_t)row * A.ldb + kc;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        x[t] = (const E*)A.a[0] + (int64_t)min(t * 16 + (lane & 15), A.M - 1) * A.lda + kc;
+    f32x4 acc[NB][NT];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0, 0, 0, 0};
+
+    constexpr int U = NT >= 4 ? 2 : 4;          // steps of 32 in flight
+    const int steps = (A.K + 31) / 32, per = (steps + WAVES - 1) / WAVES;
+    int k = wave * per * 32;
+    const int end = min(A.K, k + per * 32);
+    for (; k + 32 * U <= end; k += 32 * U) {
+        V8 wv[NB][U], xv[NT][U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) __builtin_memcpy(&wv[b][i], w[b] + k + 32 * i, 16);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) __builtin_memcpy(&xv[t][i], x[t] + k + 32 * i, 16);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[b][t] = T::mfma(wv[b][i], xv[t][i], acc[b][t]);
+    }
+    for (; k < end; k += 32) {
+        const int left = A.K - k - kc;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const V8 wv = load_k<T>(w[b] + k, left);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[b][t] = T::mfma(wv, load_k<T>(x[t] + k, left), acc[b][t]);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) part[wave][b * NT + t][lane] = acc[b][t];
+    __syncthreads();
+    for (int t = wave; t < NT; t += WAVES) {
+        const int m = t * 16 + (lane & 15), n = n0 + 4 * (lane >> 4);
+        f32x4 v = part[0][t][lane], u = part[0][(NB - 1) * NT + t][lane];
+#pragma unroll
+        for (int q = 1; q < WAVES; ++q) {
+            v += part[q][t][lane];
+            if (DUAL) u += part[q][(NB - 1) * NT + t][lane];
+        }
+        if (m >= A.M) continue;
+        if constexpr (DUAL) {
+            if (n < A.pad) gated_fwd_out<T>(A, m, n, v, u);
+        } else {
+            if (n < A.N) plain_out<T>(A, 0, m, n, v, false);
+        }
+    }
+}
+
+template <typename P>
+hipError_t launch_tile(const GemmArgs& A, hipStream_t s)
+{
+    gemm_kernel<P><<<dim3(A.sym ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n, A.batch, A.splits),
+                     P::kThreads, 0, s>>>(A);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || A.splits == 1) return e;
+    const int64_t quads = (int64_t)A.M * (((P::EPI == kPlain ? A.N : A.pad) + 3) / 4);
+    join_kernel<typename P::T, P::EPI><<<dim3((unsigned)((quads + 255) / 256), A.batch), 256, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+template <typename T, bool ATR, bool BTR, int EPI>
+hipError_t launch_layout(const GemmArgs& A, int tile, hipStream_t s)
+{
+    if (tile == 256) return launch_tile<Tile<T, 256, 256, 2, 4, ATR, BTR, EPI>>(A, s);
+    return launch_tile<Tile<T, 128, 128, 2, 2, ATR, BTR, EPI>>(A, s);
+}
+
+template <typename T>
+hipError_t launch_gemm_t(const GemmArgs& A, Product what, int tile, hipStream_t s)
+{
+    switch (what) {
+    case kRowsRows: return launch_layout<T, false, false, kPlain>(A, tile, s);
+    case kRowsCols: return launch_layout<T, false, true, kPlain>(A, tile, s);
+    case kColsCols: return launch_layout<T, true, true, kPlain>(A, tile, s);
+    case kGateUp: return launch_layout<T, false, false, kGatedFwd>(A, tile, s);
+    case kGateUpBack: return launch_layout<T, false, true, kGatedBwd>(A, tile, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <typename T, bool DUAL>
+hipError_t launch_skinny_n(const GemmArgs& A, hipStream_t s)
+{
+    const int blocks = (A.N + 15) / 16;
+    if (A.M <= 16) skinny_kernel<T, 1, DUAL, 8><<<blocks, 512, 0, s>>>(A);
+    else if (A.M <= 32) skinny_kernel<T, 2, DUAL, 8><<<blocks, 512, 0, s>>>(A);
+    else skinny_kernel<T, 4, DUAL, 8><<<blocks, 512, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_skinny_t(const GemmArgs& A, bool dual, hipStream_t s)
+{
+    return dual ? launch_skinny_n<T, true>(A, s) : launch_skinny_n<T, false>(A, s);
+}
+
+}  // namespace mm
+}  // namespace arena

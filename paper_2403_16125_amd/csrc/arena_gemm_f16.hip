@@ -1,0 +1,15 @@
+// The tiled and skinny products in float16.
+#include "arena_gemm.h"
+
+namespace arena {
+namespace mm {
+
+hipError_t launch_gemm_f16(const GemmArgs& A, Product what, int tile, hipStream_t s)
+{
+    return launch_gemm_t<F16>(A, what, tile, s);
+}
+
+hipError_t launch_skinny_f16(const GemmArgs& A, bool dual, hipStream_t s) { return launch_skinny_t<F16>(A, dual, s); }
+
+}  // namespace mm
+}  // namespace arena

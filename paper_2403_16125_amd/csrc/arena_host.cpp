@@ -16,6 +16,7 @@
 
 #include "arena.h"
 #include "arena_internal.h"
+#include "arena_layer_internal.h"
 
 using arena::TypeDev;
 
@@ -1348,3 +1349,23 @@ arena_status arena_schedule(arena_ctx* c, const arena_sched_desc* d, void* strea
 }
 
 }  // extern "C"
+
+// The context as the layer operators (arena_layer_host.cpp) see it.
+namespace arena {
+
+int ctx_device(const arena_ctx* c) { return c->device; }
+
+void ctx_clear(arena_ctx* c) { c->err.clear(); }
+
+arena_status ctx_fail(arena_ctx* c, arena_status s, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    c->err = buf;
+    return s;
+}
+
+}  // namespace arena

@@ -1,0 +1,124 @@
+// Internal interface between the host side of the layer operators and their
+// HIP kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "arena_layer.h"
+
+namespace arena {
+
+// Defined beside arena_ctx: the context's device, and its error text.
+int ctx_device(const arena_ctx* c);
+void ctx_clear(arena_ctx* c);
+arena_status ctx_fail(arena_ctx* c, arena_status s, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
+
+namespace mm {
+
+constexpr int kBK = 64;                 // k per step
+constexpr int kMaxLd = 1 << 22;         // row stride limit, elements: 256 rows stay within 32-bit byte offsets
+
+enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2 };
+enum Out { kOut16 = 0, kOutF32 = 1, kOutBf16 = 2 };   // the operands' own type, float, bf16
+enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
+
+struct GemmArgs {
+    // segments of k (nseg = 2: the second operand pair follows the first), or
+    // with pairs = 1 the operands of batch index 0 and 1, or the gate and up
+    // matrices of the gated forward product (b)
+    const void* a[2];
+    const void* b[2];
+    void* c[2];
+    int64_t lda, ldb, ldc;    // elements
+    int64_t sa, sb, sc;       // batch strides, elements
+    int32_t M, N, K;
+    int32_t nseg, pairs, batch;
+    int32_t tiles_m, tiles_n, sym;
+    int32_t vec;              // every matrix of the epilogue takes four columns at a time
+    // plain: C = alpha * product + beta * e - diag on the diagonal
+    const void* e[2];
+    int64_t lde, se;
+    float alpha, beta, diag;
+    int32_t out;
+    // gated, forward: c[0] = act(g) u, and g, u unless null; backward: c[0] and
+    // c[1] the gradients of g and u.  Rows of ldc elements (c) and ldg values of
+    // 24 bits (g, u: M rows of 16-bit heads, then M rows of 8-bit tails);
+    // columns N .. pad - 1 are written as zeros
+    void *g, *u;
+    int64_t ldg;
+    int32_t act, pad;
+    // split k: block z of `splits` takes `per` steps and leaves its sums in part
+    int32_t splits, per;
+    float* part;
+};
+
+// Products by the layouts of their operands (rows: k contiguous; cols: m or n
+// contiguous) and epilogue.
+enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack };
+
+// tile: 256 or 128.  The host has checked that operands are 16-byte aligned
+// with strides and batch strides of multiples of 8, and that values between
+// the matrix's edge and the next multiple of 8 along the contiguous axis are
+// readable (and zero where that axis is k).
+hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, int tile, hipStream_t s);
+
+constexpr int kSkinnyRows = 64;         // rows of A (tokens) that the kernel without LDS tiles takes
+
+// C = A B^T with both operands' k contiguous, M <= kSkinnyRows; dual: the gated
+// forward product.
+hipError_t launch_skinny(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
+
+// Copies rows x cols 16-bit values with zeros in columns cols .. ld_to - 1.
+hipError_t launch_pack(const void* from, int64_t ld_from, void* to, int64_t ld_to, int64_t rows, int64_t cols,
+                       hipStream_t s);
+
+}  // namespace mm
+
+// Norms around a block.
+struct NormArgs {
+    const void *x, *y, *gate, *w_post, *b_post, *w_pre, *b_pre;
+    int64_t ld_x, ld_y, ld_gate, ld_r, ld_n;
+    void *r, *n;
+    float* stats;                 // [tokens][4]: mean and 1/deviation of the block's output, then of the stream
+    int64_t tokens, gate_rows;    // gate_rows: tokens of one gate row (all of them: tokens, at least 1)
+    int32_t width, layer;         // layer: subtract the mean
+    float eps, scale;
+    // backward
+    const void *dn, *dr, *res;    // gradients of n and r; res: r (x where there is no block output)
+    int64_t ld_dn, ld_dr, ld_res, ld_dx, ld_dy;
+    void *dx, *dy;
+    void *dgate, *dw_post, *db_post, *dw_pre, *db_pre;
+    float* part;                  // workers' column sums, see norm_plan
+    int32_t workers, rows_each;   // workers of the backward, tokens of each
+};
+
+// Column sums that a worker keeps: of dw_pre, db_pre, dw_post, db_post and its
+// first and last gate row's dgate.
+constexpr int kNormSums = 6;
+constexpr int kNormMaxWidth = 16384;
+
+void norm_plan(int64_t tokens, int64_t gate_rows, int width, int* workers, int* rows_each);
+hipError_t launch_norm_forward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s);
+hipError_t launch_norm_backward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s);
+
+// Orthogonalised update: the passes over the gradient.
+struct UpdateArgs {
+    const void* grad;             // [batch][rows][cols]
+    const float* momentum;        // nullable
+    float* momentum_out;
+    int64_t ld_grad, ld_mom, ld_mom_out, s_grad, s_mom, s_mom_out;
+    int32_t rows, cols, batch, nesterov;
+    float mu, eps;
+    _Float16* x;                  // [batch][rows_p][ld_x], zero past rows and cols
+    int32_t rows_p, ld_x;
+    double* part;                 // [batch][blocks] sums of squares
+    int32_t blocks;
+};
+
+constexpr int kUpdateBlocks = 256;      // most blocks that share a matrix's sum of squares
+
+hipError_t launch_update_sum(const UpdateArgs& A, int dtype, hipStream_t s);
+hipError_t launch_update_scale(const UpdateArgs& A, int dtype, hipStream_t s);
+
+}  // namespace arena
