@@ -16,7 +16,8 @@
 //     granule q ^ f(k), f = (k & 3) | ((k >> 3) & 3) << 2, so the 16 rows that
 //     one transposing read touches lie in different granules.
 // The product is formed transposed (the B fragment is the first operand), so a
-// lane holds four neighbouring columns of one row of C.
+// lane holds four neighbouring columns of one row of C, and eight after a trip
+// through LDS.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -85,13 +86,14 @@ __device__ __forceinline__ void load_to_lds(const char* src, char* dst)
     __builtin_amdgcn_global_load_lds((GlobalVoid*)src, (LdsVoid*)dst, 16, 0, 0);
 }
 
-// Which matrix and row a row of the B tile is.  The gated forward product
-// interleaves 32 gate and 32 up features, so one wave holds both of a feature.
-template <bool DUAL>
-__device__ __forceinline__ int tile_row(int r)
-{
-    return DUAL ? ((r >> 6) << 5) + (r & 31) : r;
-}
+// Which matrix and row a row of the B tile is.  In the gated forward product a
+// wave's rows are gate features, then as many up features, so one wave holds
+// both of a feature.
+template <int W>        // rows of a wave
+struct Dual {
+    static __device__ __forceinline__ int row(int r) { return r / W * (W / 2) + r % (W / 2); }
+    static __device__ __forceinline__ int up(int r) { return r / (W / 2) & 1; }
+};
 
 // One operand's share of a tile: R rows of C (or columns) x 64 of k.
 template <typename P, int R, bool TR, bool DUAL>
@@ -126,7 +128,7 @@ struct Loader {
                 off[it] = (uint32_t)k * (uint32_t)(ld * 2) + (uint32_t)col * 2;
             } else {
                 const int r = it * (kThreads / 8) + (tid >> 3);
-                const int row = min(first + tile_row<DUAL>(r), n - 1) - first;
+                const int row = min(first + (DUAL ? Dual<P::BN / P::WN>::row(r) : r), n - 1) - first;
                 off[it] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)(((tid & 7) ^ (r & 7)) << 4);
             }
         }
@@ -146,7 +148,7 @@ struct Loader {
 #pragma unroll
         for (int it = 0; it < kChunks; ++it) {
             const char* p = p0;
-            if (DUAL) p = ((it * (kThreads / 8) + wave * 8) >> 5) & 1 ? p1 : p0;
+            if (DUAL) p = Dual<P::BN / P::WN>::up(it * (kThreads / 8) + wave * 8) ? p1 : p0;
             const char* src = p + off[it];
             if (TAIL && k_of(it, tid) >= left) src = (const char*)&g_zero_chunk;
             load_to_lds(src, lds + (it * kThreads + wave * 64) * 16);
@@ -193,75 +195,67 @@ struct Tile {
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
     static constexpr int EPI = EPI_;
     static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int kWavesEach = BM == 256 ? kThreads / 256 : 2;     // waves a SIMD, for the register limit
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     static constexpr int kCols = DUAL ? BN / 2 : BN;     // columns of C of a tile
-    static_assert(!DUAL || BN / WN == 64, "a wave of the gated product holds 32 gate and 32 up features");
 };
 
-template <typename E>
-__device__ __forceinline__ void store4(E* p, f32x4 v, int left, bool vec)
+// C neighbouring values of a row, `left` of them inside the matrix.  Rows may
+// start on any value: the wide accesses are unaligned where they do not.
+template <typename E, int C>
+__device__ __forceinline__ void put(E* p, const float (&v)[C], int left)
 {
-    typedef E E4 __attribute__((ext_vector_type(4)));
-    if (vec && left >= 4) {
-        E4 w;
+    if (left >= C) {
+        E w[C];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = (E)v[r];
-        *(E4*)p = w;
+        for (int r = 0; r < C; ++r) w[r] = (E)v[r];
+        __builtin_memcpy(p, w, sizeof(w));
     } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < C; ++r)
             if (r < left) p[r] = (E)v[r];
     }
 }
 
-template <typename E>
-__device__ __forceinline__ f32x4 load4(const E* p, int left, bool vec)
+template <typename E, int C>
+__device__ __forceinline__ void get(const E* p, float (&v)[C], int left)
 {
-    typedef E E4 __attribute__((ext_vector_type(4)));
-    f32x4 v = {0, 0, 0, 0};
-    if (vec && left >= 4) {
-        const E4 w = *(const E4*)p;
+    if (left >= C) {
+        E w[C];
+        __builtin_memcpy(w, p, sizeof(w));
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (float)w[r];
+        for (int r = 0; r < C; ++r) v[r] = (float)w[r];
     } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (r < left) v[r] = (float)p[r];
+        for (int r = 0; r < C; ++r) v[r] = r < left ? (float)p[r] : 0.0f;
     }
-    return v;
 }
 
-// Writes four columns (n .. n + 3, those below N) of row m; z is the batch index.
-template <typename T>
-__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, f32x4 v, bool mirror)
+// Writes C columns from n (those below N) of row m; z is the batch index.
+// Returns the values written in v.
+template <typename T, int C>
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[C])
 {
     typedef typename T::E E;
     const int left = A.N - n;
     const int64_t at = (A.pairs ? 0 : z * A.sc) + (int64_t)m * A.ldc + n;
     void* c = A.c[A.pairs ? z : 0];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] *= A.alpha;
+    for (int r = 0; r < C; ++r) v[r] *= A.alpha;
     if (A.beta != 0.0f) {
         const void* p = A.e[A.pairs ? z : 0];
         const int64_t from = (A.pairs ? 0 : z * A.se) + (int64_t)m * A.lde + n;
-        const f32x4 e = A.out == kOutF32 ? load4((const float*)p + from, left, A.vec)
-                                         : load4((const E*)p + from, left, A.vec);
+        float e[C];
+        if (A.out == kOutF32) get((const float*)p + from, e, left);
+        else get((const E*)p + from, e, left);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] += A.beta * e[r];
+        for (int r = 0; r < C; ++r) v[r] += A.beta * e[r];
     }
     if (A.diag != 0.0f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < C; ++r)
             if (m == n + r) v[r] -= A.diag;
-    if (A.out == kOutF32) store4((float*)c + at, v, left, A.vec);
-    else if (A.out == kOutBf16) store4((__bf16*)c + at, v, left, A.vec);
-    else store4((E*)c + at, v, left, A.vec);
-    if (mirror) {
-        E* q = (E*)c + z * A.sc + (int64_t)n * A.ldc + m;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (r < left) q[(int64_t)r * A.ldc] = (E)v[r];
-    }
+    if (A.out == kOutF32) put((float*)c + at, v, left);
+    else if (A.out == kOutBf16) put((__bf16*)c + at, v, left);
+    else put((E*)c + at, v, left);
 }
 
 // Values kept for the backward pass: the upper 24 bits of a float, 16 in a row
@@ -269,71 +263,74 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
 // 16 bits they would cost the gradients two more roundings of the operands'
 // size (1.8 times the error of one rounding of the result instead of 1.4); the
 // tails are a sixth of the bytes that the pass writes here.
-__device__ __forceinline__ void store24(void* p, const GemmArgs& A, int m, int n, f32x4 v)
+template <int C>
+__device__ __forceinline__ void put24(void* p, const GemmArgs& A, int m, int n, const float (&v)[C])
 {
-    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
     const int64_t at = (int64_t)m * A.ldg + n;
-    U4 head;
-    uint32_t tail = 0;
+    uint16_t head[C];
+    uint8_t tail[C];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < C; ++r) {
         const uint32_t b = __float_as_uint(v[r]);
         head[r] = (uint16_t)(b >> 16);
-        tail |= ((b >> 8) & 0xffu) << (8 * r);
+        tail[r] = (uint8_t)(b >> 8);
     }
-    *(U4*)((uint16_t*)p + at) = head;
-    *(uint32_t*)((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at) = tail;
+    __builtin_memcpy((uint16_t*)p + at, head, sizeof(head));
+    __builtin_memcpy((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, tail, sizeof(tail));
 }
 
-__device__ __forceinline__ f32x4 load24(const void* p, const GemmArgs& A, int m, int n)
+template <int C>
+__device__ __forceinline__ void get24(const void* p, const GemmArgs& A, int m, int n, float (&v)[C])
 {
-    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
     const int64_t at = (int64_t)m * A.ldg + n;
-    const U4 head = *(const U4*)((const uint16_t*)p + at);
-    const uint32_t tail = *(const uint32_t*)((const uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at);
-    f32x4 v;
+    uint16_t head[C];
+    uint8_t tail[C];
+    __builtin_memcpy(head, (const uint16_t*)p + at, sizeof(head));
+    __builtin_memcpy(tail, (const uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, sizeof(tail));
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = __uint_as_float((uint32_t)head[r] << 16 | ((tail >> (8 * r)) & 0xffu) << 8);
-    return v;
+    for (int r = 0; r < C; ++r) v[r] = __uint_as_float((uint32_t)head[r] << 16 | (uint32_t)tail[r] << 8);
 }
 
-// h = act(g) u from the 32-bit sums, rounded to 16 bits as the next product's operand.
-template <typename T>
-__device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, f32x4 g, f32x4 u)
+// h = act(g) u from the 32-bit sums, rounded to 16 bits as the next product's
+// operand.  n and pad are multiples of C's and of 8, so C columns are all
+// inside pad.
+template <typename T, int C>
+__device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, float (&g)[C], float (&u)[C])
 {
     typedef typename T::E E;
-    f32x4 h;
+    float h[C];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < C; ++r) {
         const bool in = n + r < A.N;
         g[r] = in ? g[r] : 0.0f;
         u[r] = in ? u[r] : 0.0f;
         h[r] = in ? act_value(g[r], A.act) * u[r] : 0.0f;
     }
-    store4((E*)A.c[0] + (int64_t)m * A.ldc + n, h, 4, true);
+    put((E*)A.c[0] + (int64_t)m * A.ldc + n, h, C);
     if (A.g) {
-        store24(A.g, A, m, n, g);
-        store24(A.u, A, m, n, u);
+        put24(A.g, A, m, n, g);
+        put24(A.u, A, m, n, u);
     }
 }
 
 // v = the gradient of h = act(g) u:  of g  v u act'(g),  of u  v act(g).
-template <typename T>
-__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, f32x4 v)
+template <typename T, int C>
+__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, const float (&v)[C])
 {
     typedef typename T::E E;
-    const f32x4 g = load24(A.g, A, m, n), u = load24(A.u, A, m, n);
-    f32x4 dg, du;
+    float g[C], u[C], dg[C], du[C];
+    get24(A.g, A, m, n, g);
+    get24(A.u, A, m, n, u);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < C; ++r) {
         const bool in = n + r < A.N;
         float a, d;
         act_both(g[r], A.act, &a, &d);
         du[r] = in ? v[r] * a : 0.0f;
         dg[r] = in ? v[r] * u[r] * d : 0.0f;
     }
-    store4((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, 4, true);
-    store4((E*)A.c[1] + (int64_t)m * A.ldc + n, du, 4, true);
+    put((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, C);
+    put((E*)A.c[1] + (int64_t)m * A.ldc + n, du, C);
 }
 
 // Tile of a block: blocks go to the 8 XCDs in turn, so each XCD gets a run of
@@ -359,9 +356,10 @@ __device__ __forceinline__ void tile_of(int bid, int n_blocks, int tiles_m, int 
 }
 
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, 2) void gemm_kernel(const GemmArgs A)
+__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
 {
     typedef typename P::T T;
+    // separate arrays, so that a fragment read is known not to meet the loads in flight
     __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
@@ -418,95 +416,156 @@ __global__ __launch_bounds__(P::kThreads, 2) void gemm_kernel(const GemmArgs A)
             lb.template fetch<true>(pb, pb1, sb, tid, left);
         }
     };
-    auto multiply = [&](const char* sa, const char* sb) {
+    typename T::V8 fa0[P::FM], fb0[P::FN], fa1[P::FM], fb1[P::FN];    // fragments of the step's halves
+    auto read = [&](const char* sa, const char* sb, int kk, typename T::V8* a, typename T::V8* b) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            typename T::V8 a[P::FM], b[P::FN];
+        for (int j = 0; j < P::FN; ++j) b[j] = fb.get(sb, j, kk);
 #pragma unroll
-            for (int j = 0; j < P::FN; ++j) b[j] = fb.get(sb, j, kk);
-#pragma unroll
-            for (int i = 0; i < P::FM; ++i) a[i] = fa.get(sa, i, kk);
-#pragma unroll
-            for (int i = 0; i < P::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < P::FN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);
-        }
+        for (int i = 0; i < P::FM; ++i) a[i] = fa.get(sa, i, kk);
     };
-    // One step: the loads of this step have landed and every wave is done
-    // with the other buffer (one barrier), then the next step's loads start.
-    auto turn = [&](int step, char* sa, char* sb, char* ta, char* tb) {
-        __syncthreads();
-        if (step + 1 < end) fetch(step + 1, ta, tb);
-        multiply(sa, sb);
-    };
-    if (s < end) fetch(s, sa0, sb0);
-    for (; s < end; s += 2) {
-        turn(s, sa0, sb0, sa1, sb1);
-        if (s + 1 < end) turn(s + 1, sa1, sb1, sa0, sb0);
-    }
-
-    // epilogue: lane holds rows m = .. + (lane & 15), columns 4 (lane >> 4) + 0..3 of each fragment
-    const int mr = m0 + wm * (P::BM / P::WM) + (lane & 15);
-    const int nr = n0 + wn * (P::DUAL ? 32 : P::BN / P::WN) + 4 * (lane >> 4);
-    if (A.splits > 1) {
-        const int64_t plane = (int64_t)A.M * A.N;
-        float* out = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1);
+    auto multiply = [&](const typename T::V8* a, const typename T::V8* b) {
 #pragma unroll
         for (int i = 0; i < P::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < P::FN; ++j) {
-                const bool up = P::DUAL && j >= P::FN / 2;
-                const int m = mr + i * 16, n = nr + (up ? j - P::FN / 2 : j) * 16;
-                if (m < A.M && n < A.N)
-                    store4(out + (up ? plane : 0) + (int64_t)m * A.N + n, acc[i][j], A.N - n, A.N % 4 == 0);
-            }
-        return;
+            for (int j = 0; j < P::FN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);
+    };
+    // Interleaves the fragment reads (and the loads of the next step) of a half
+    // step with the products of the half step before.
+    auto weave = [&](bool loads) {
+        constexpr int reads = P::FM * (P::ATR ? 2 : 1) + P::FN * (P::BTR ? 2 : 1), products = P::FM * P::FN;
+        constexpr int each = products / reads > 0 ? products / reads : 1;
+#pragma unroll
+        for (int i = 0; i < reads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+        }
+        (void)loads;
+    };
+    // One step.  At its barrier this step's loads have landed and every wave
+    // holds its fragments of the step before, so the other buffer is free: the
+    // next step's loads start, and the second half of the step before is
+    // multiplied while this step's first fragments are read.
+    auto turn = [&](int step, char* sa, char* sb, char* ta, char* tb, bool first) {
+        __syncthreads();
+        if (step + 1 < end) fetch(step + 1, ta, tb);
+        __builtin_amdgcn_sched_barrier(0);
+        read(sa, sb, 0, fa0, fb0);
+        if (!first) {
+            multiply(fa1, fb1);
+            weave(true);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        read(sa, sb, 1, fa1, fb1);
+        multiply(fa0, fb0);
+        weave(false);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (s < end) {
+        fetch(s, sa0, sb0);
+        turn(s, sa0, sb0, sa1, sb1, true);
+        for (++s; s < end; s += 2) {
+            turn(s, sa1, sb1, sa0, sb0, false);
+            if (s + 1 < end) turn(s + 1, sa0, sb0, sa1, sb1, false);
+        }
+        multiply(fa1, fb1);
     }
+
+    // Epilogue.  A lane holds row lane & 15 and columns 4 (lane >> 4) + 0..3 of
+    // each fragment; through LDS (a slice of rows at a time, 16-byte pieces
+    // swizzled by row) it gets 8 neighbouring columns, and the wave whole
+    // stretches of rows.  The waves' quarters of the buffers lie in different
+    // arrays or halves of them; a wave reads only what it wrote.
+    constexpr int RW = P::BM / P::WM, CW = P::BN / P::WN, kWaves = P::WM * P::WN;
+    constexpr int kRows = 64, kPer = kWaves / 4;
+    static_assert(kRows * CW * 4 * kPer <= P::BM * 128 && kPer * 4 == kWaves && P::BM == P::BN, "epilogue slices fit");
+    char* const bufs[4] = {sa0, sa1, sb0, sb1};
+    char* const mine = (wave & 2 ? (wave & 1 ? bufs[3] : bufs[2]) : (wave & 1 ? bufs[1] : bufs[0])) +
+                       (wave >> 2) * (kRows * CW * 4);
+    auto piece = [&](int r, int c4) { return (f32x4*)(mine + (r * (CW / 4) + (c4 ^ (r & 15))) * 16); };
+    const int mw = m0 + wm * RW, nw = n0 + wn * (P::DUAL ? CW / 2 : CW);
+    constexpr int kChunks = (P::DUAL ? CW / 2 : CW) / 8;      // of 8 columns a row
+    const bool mirror = A.sym && tm != tn;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < P::FM; ++i) {
-        const int m = mr + i * 16;
-        if (m >= A.M) continue;
-        if constexpr (P::EPI == kGatedFwd) {
+    for (int h = 0; h < RW / kRows; ++h) {
 #pragma unroll
-            for (int j = 0; j < P::FN / 2; ++j) {
-                const int n = nr + j * 16;
-                if (n < A.pad) gated_fwd_out<T>(A, m, n, acc[i][j], acc[i][j + P::FN / 2]);
+        for (int i = 0; i < kRows / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j)
+                *piece(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[h * (kRows / 16) + i][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+        for (int x = lane; x < kRows * kChunks; x += 64) {
+            const int r = x / kChunks, c = x % kChunks;
+            const int m = mw + h * kRows + r, n = nw + c * 8;
+            float v[8], u[8];
+            *(f32x4*)v = *piece(r, 2 * c);
+            *(f32x4*)(v + 4) = *piece(r, 2 * c + 1);
+            if (P::DUAL) {
+                *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
+                *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < P::FN; ++j) {
-                const int n = nr + j * 16;
-                if constexpr (P::EPI == kGatedBwd) {
-                    if (n < A.pad) gated_bwd_out<T>(A, m, n, acc[i][j]);
-                } else if (n < A.N) {
-                    plain_out<T>(A, zb, m, n, acc[i][j], A.sym && tm != tn);
+            if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
+            if (A.splits > 1) {
+                const int64_t plane = (int64_t)A.M * A.N;
+                float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) + (int64_t)m * A.N + n;
+                put(to, v, A.N - n);
+                if (P::DUAL) put(to + plane, u, A.N - n);
+            } else if constexpr (P::EPI == kGatedFwd) {
+                gated_fwd_out<T>(A, m, n, v, u);
+            } else if constexpr (P::EPI == kGatedBwd) {
+                gated_bwd_out<T>(A, m, n, v);
+            } else {
+                plain_out<T>(A, zb, m, n, v);
+                if (mirror) {
+                    *piece(r, 2 * c) = *(f32x4*)v;
+                    *piece(r, 2 * c + 1) = *(f32x4*)(v + 4);
                 }
             }
         }
+        if (P::EPI == kPlain && mirror) {
+            // the transposed tile: 8 rows of a column are 8 columns of its row
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+            for (int x = lane; x < CW * (kRows / 8); x += 64) {
+                const int c = x / (kRows / 8), r0 = x % (kRows / 8) * 8;
+                const int m = mw + h * kRows + r0, n = nw + c;
+                float v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = ((const float*)piece(r0 + r, c >> 2))[c & 3];
+                if (m < A.M && n < A.N)
+                    put((typename T::E*)A.c[0] + zb * A.sc + (int64_t)n * A.ldc + m, v, A.M - m);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
 // Joins the parts of a split product in their order and applies the epilogue;
-// a thread takes four columns of a row.
+// a thread takes eight columns of a row.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A)
 {
-    const int quads = ((EPI == kPlain ? A.N : A.pad) + 3) / 4;
+    const int per = ((EPI == kPlain ? A.N : A.pad) + 7) / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)A.M * quads) return;
-    const int m = (int)(i / quads), n = (int)(i % quads) * 4;
+    if (i >= (int64_t)A.M * per) return;
+    const int m = (int)(i / per), n = (int)(i % per) * 8;
     const int64_t plane = (int64_t)A.M * A.N, each = plane * A.batch * (EPI == kGatedFwd ? 2 : 1);
     const float* p = A.part + (int64_t)blockIdx.y * plane * (EPI == kGatedFwd ? 2 : 1) + (int64_t)m * A.N + n;
-    f32x4 v = {0, 0, 0, 0}, u = {0, 0, 0, 0};
-    const bool vec = A.N % 4 == 0;
-    if (n < A.N)
-        for (int s = 0; s < A.splits; ++s) {
-            v += load4(p + s * each, A.N - n, vec);
-            if (EPI == kGatedFwd) u += load4(p + s * each + plane, A.N - n, vec);
-        }
+    float v[8] = {}, u[8] = {};
+    for (int s = 0; s < A.splits; ++s) {
+        float w[8];
+        get(p + s * each, w, A.N - n);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] += w[r];
+        if (EPI != kGatedFwd) continue;
+        get(p + s * each + plane, w, A.N - n);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) u[r] += w[r];
+    }
     if constexpr (EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
     else if constexpr (EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v);
-    else plain_out<T>(A, blockIdx.y, m, n, v, false);
+    else plain_out<T>(A, blockIdx.y, m, n, v);
 }
 
 // Few rows of A (tokens): nothing of B is used twice, so it goes from memory
@@ -592,10 +651,13 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
             if (DUAL) u += part[q][(NB - 1) * NT + t][lane];
         }
         if (m >= A.M) continue;
+        float fv[4], fu[4];
+        *(f32x4*)fv = v;
+        *(f32x4*)fu = u;
         if constexpr (DUAL) {
-            if (n < A.pad) gated_fwd_out<T>(A, m, n, v, u);
+            if (n < A.pad) gated_fwd_out<T>(A, m, n, fv, fu);
         } else {
-            if (n < A.N) plain_out<T>(A, 0, m, n, v, false);
+            if (n < A.N) plain_out<T>(A, 0, m, n, fv);
         }
     }
 }
@@ -607,8 +669,8 @@ hipError_t launch_tile(const GemmArgs& A, hipStream_t s)
                      P::kThreads, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    const int64_t quads = (int64_t)A.M * (((P::EPI == kPlain ? A.N : A.pad) + 3) / 4);
-    join_kernel<typename P::T, P::EPI><<<dim3((unsigned)((quads + 255) / 256), A.batch), 256, 0, s>>>(A);
+    const int64_t n = (int64_t)A.M * (((P::EPI == kPlain ? A.N : A.pad) + 7) / 8);
+    join_kernel<typename P::T, P::EPI><<<dim3((unsigned)((n + 255) / 256), A.batch), 256, 0, s>>>(A);
     return hipGetLastError();
 }
 
