@@ -7,9 +7,9 @@
 // transposed copies.
 //
 // A block computes a BM x BN tile with WM x WN waves, 64 of k at a time, from
-// two LDS buffers: while one is multiplied, the other is filled by direct
-// global-to-LDS loads.  Those write 16 bytes per lane in lane order, so the
-// bank swizzle sits on the global side (which chunk a lane fetches):
+// two or four LDS buffers: while one is multiplied, the others are filled by
+// direct global-to-LDS loads.  Those write 16 bytes per lane in lane order, so
+// the bank swizzle sits on the global side (which chunk a lane fetches):
 //   k contiguous: row r of 8 chunks; position p holds chunk p ^ (r & 7), and a
 //     fragment read (16 rows, one chunk each) meets every bank once;
 //   m or n contiguous: row k of R / 16 granules of 32 bytes; position q holds
@@ -141,6 +141,7 @@ struct Loader {
         return TR ? q : q + 2 * (int64_t)row0 * ld;
     }
 
+    // TAIL: lanes past the end of k (`left` of it remain) fetch zeros.
     template <bool TAIL>
     __device__ __forceinline__ void fetch(const char* p0, const char* p1, char* lds, int tid, int left) const
     {
@@ -188,14 +189,21 @@ struct Frags {
     }
 };
 
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool ATR_, bool BTR_, int EPI_>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool ATR_, bool BTR_, int EPI_>
 struct Tile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
     static constexpr int EPI = EPI_;
     static constexpr int kThreads = 64 * WM * WN;
-    static constexpr int kWavesEach = BM == 256 ? kThreads / 256 : 2;     // waves a SIMD, for the register limit
+    static constexpr int kStages = STAGES_;
+    // With few blocks on a compute unit a wave that issues its loads in a row
+    // leaves the matrix cores idle (128 x 128, four buffers: 0.72 us a step, woven
+    // between the products 0.54); with many, the others fill the gap and the
+    // comparisons cost more than they bring (8192 x 4096 x 10944: 550 us, woven 582).
+    static constexpr bool kWoven = STAGES_ > 2;
+    // waves a SIMD, for the register limit: one block on a compute unit, or two by their LDS
+    static constexpr int kWavesEach = kThreads / 256 * (kStages * (BM + BN) * 128 <= 81920 ? 2 : 1);
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     static constexpr int kCols = DUAL ? BN / 2 : BN;     // columns of C of a tile
 };
@@ -229,10 +237,50 @@ __device__ __forceinline__ void get(const E* p, float (&v)[C], int left)
     }
 }
 
-// Writes C columns from n (those below N) of row m; z is the batch index.
-// Returns the values written in v.
+// What an epilogue reads from memory for eight columns, apart from using it, so
+// that several reads are in flight.
+template <typename T, int EPI>
+struct Side;
+
+// plain: the added matrix.
+template <typename T>
+struct Side<T, kPlain> {
+    float e[8];
+    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
+    {
+        if (A.beta == 0.0f) return;
+        const void* p = A.e[A.pairs ? z : 0];
+        const int64_t from = (A.pairs ? 0 : z * A.se) + (int64_t)m * A.lde + n;
+        if (A.out == kOutF32) get((const float*)p + from, e, A.N - n);
+        else get((const typename T::E*)p + from, e, A.N - n);
+    }
+};
+
+template <typename T>
+struct Side<T, kGatedFwd> {
+    __device__ __forceinline__ void load(const GemmArgs&, int, int, int) {}
+};
+
+// gated, backward: the heads and tails of the kept gate and up values.
+template <typename T>
+struct Side<T, kGatedBwd> {
+    uint16_t gh[8], uh[8];
+    uint8_t gt[8], ut[8];
+    __device__ __forceinline__ void load(const GemmArgs& A, int, int m, int n)
+    {
+        const int64_t at = (int64_t)m * A.ldg + n, tails = 2 * (int64_t)A.M * A.ldg + at;
+        __builtin_memcpy(gh, (const uint16_t*)A.g + at, sizeof(gh));
+        __builtin_memcpy(uh, (const uint16_t*)A.u + at, sizeof(uh));
+        __builtin_memcpy(gt, (const uint8_t*)A.g + tails, sizeof(gt));
+        __builtin_memcpy(ut, (const uint8_t*)A.u + tails, sizeof(ut));
+    }
+};
+
+// Writes eight (or, of few rows, four) columns from n, those below N, of row m;
+// z is the batch index.  Leaves the values written in v.
 template <typename T, int C>
-__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[C])
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[C],
+                                          const Side<T, kPlain>& side)
 {
     typedef typename T::E E;
     const int left = A.N - n;
@@ -240,15 +288,9 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
     void* c = A.c[A.pairs ? z : 0];
 #pragma unroll
     for (int r = 0; r < C; ++r) v[r] *= A.alpha;
-    if (A.beta != 0.0f) {
-        const void* p = A.e[A.pairs ? z : 0];
-        const int64_t from = (A.pairs ? 0 : z * A.se) + (int64_t)m * A.lde + n;
-        float e[C];
-        if (A.out == kOutF32) get((const float*)p + from, e, left);
-        else get((const E*)p + from, e, left);
+    if (A.beta != 0.0f)
 #pragma unroll
-        for (int r = 0; r < C; ++r) v[r] += A.beta * e[r];
-    }
+        for (int r = 0; r < C; ++r) v[r] += A.beta * side.e[r];
     if (A.diag != 0.0f)
 #pragma unroll
         for (int r = 0; r < C; ++r)
@@ -279,16 +321,9 @@ __device__ __forceinline__ void put24(void* p, const GemmArgs& A, int m, int n, 
     __builtin_memcpy((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, tail, sizeof(tail));
 }
 
-template <int C>
-__device__ __forceinline__ void get24(const void* p, const GemmArgs& A, int m, int n, float (&v)[C])
+__device__ __forceinline__ float from24(uint16_t head, uint8_t tail)
 {
-    const int64_t at = (int64_t)m * A.ldg + n;
-    uint16_t head[C];
-    uint8_t tail[C];
-    __builtin_memcpy(head, (const uint16_t*)p + at, sizeof(head));
-    __builtin_memcpy(tail, (const uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, sizeof(tail));
-#pragma unroll
-    for (int r = 0; r < C; ++r) v[r] = __uint_as_float((uint32_t)head[r] << 16 | (uint32_t)tail[r] << 8);
+    return __uint_as_float((uint32_t)head << 16 | (uint32_t)tail << 8);
 }
 
 // h = act(g) u from the 32-bit sums, rounded to 16 bits as the next product's
@@ -314,23 +349,22 @@ __device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, f
 }
 
 // v = the gradient of h = act(g) u:  of g  v u act'(g),  of u  v act(g).
-template <typename T, int C>
-__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, const float (&v)[C])
+template <typename T>
+__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, const float (&v)[8],
+                                              const Side<T, kGatedBwd>& side)
 {
     typedef typename T::E E;
-    float g[C], u[C], dg[C], du[C];
-    get24(A.g, A, m, n, g);
-    get24(A.u, A, m, n, u);
+    float dg[8], du[8];
 #pragma unroll
-    for (int r = 0; r < C; ++r) {
+    for (int r = 0; r < 8; ++r) {
         const bool in = n + r < A.N;
         float a, d;
-        act_both(g[r], A.act, &a, &d);
+        act_both(from24(side.gh[r], side.gt[r]), A.act, &a, &d);
         du[r] = in ? v[r] * a : 0.0f;
-        dg[r] = in ? v[r] * u[r] * d : 0.0f;
+        dg[r] = in ? v[r] * from24(side.uh[r], side.ut[r]) * d : 0.0f;
     }
-    put((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, C);
-    put((E*)A.c[1] + (int64_t)m * A.ldc + n, du, C);
+    put((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, 8);
+    put((E*)A.c[1] + (int64_t)m * A.ldc + n, du, 8);
 }
 
 // Tile of a block: blocks go to the 8 XCDs in turn, so each XCD gets a run of
@@ -355,15 +389,36 @@ __device__ __forceinline__ void tile_of(int bid, int n_blocks, int tiles_m, int 
     *tn = in / rows;
 }
 
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
+// Waits until at most N of the wave's global loads are in flight, and for all
+// of its LDS reads.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(N < 64, "the counter has six bits");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);
+}
+
 template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
 {
     typedef typename P::T T;
     // separate arrays, so that a fragment read is known not to meet the loads in flight
+    constexpr int kMoreA = P::kStages > 2 ? P::BM * 128 : 16, kMoreB = P::kStages > 2 ? P::BN * 128 : 16;
     __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
     __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
+    __shared__ __attribute__((aligned(16))) char sa2[kMoreA];
+    __shared__ __attribute__((aligned(16))) char sa3[kMoreA];
+    __shared__ __attribute__((aligned(16))) char sb2[kMoreB];
+    __shared__ __attribute__((aligned(16))) char sb3[kMoreB];
+    auto bufa = [&](int i) { return i == 0 ? sa0 : i == 1 ? sa1 : i == 2 ? sa2 : sa3; };
+    auto bufb = [&](int i) { return i == 0 ? sb0 : i == 1 ? sb1 : i == 2 ? sb2 : sb3; };
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
@@ -404,16 +459,19 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
         *pb1 = P::DUAL ? lb.base(A.b[1], 0) + q * lb.step : *pb;
         *left = A.K - q * kBK;
     };
-    auto fetch = [&](int step, char* sa, char* sb) {
+    // The loads of a step, of both operands (which = 3) or one of them.  Woven
+    // between products they may not branch, so every lane compares its k with
+    // the end; otherwise only the last step does.
+    auto fetch = [&](int step, char* sa, char* sb, auto which) {
         const char *pa, *pb, *pb1;
         int left;
         where(step, &pa, &pb, &pb1, &left);
-        if (left >= kBK) {
-            la.template fetch<false>(pa, pa, sa, tid, left);
-            lb.template fetch<false>(pb, pb1, sb, tid, left);
+        if (P::kWoven || left < kBK) {
+            if (which.value & 1) la.template fetch<true>(pa, pa, sa, tid, left);
+            if (which.value & 2) lb.template fetch<true>(pb, pb1, sb, tid, left);
         } else {
-            la.template fetch<true>(pa, pa, sa, tid, left);
-            lb.template fetch<true>(pb, pb1, sb, tid, left);
+            if (which.value & 1) la.template fetch<false>(pa, pa, sa, tid, left);
+            if (which.value & 2) lb.template fetch<false>(pb, pb1, sb, tid, left);
         }
     };
     typename T::V8 fa0[P::FM], fb0[P::FN], fa1[P::FM], fb1[P::FN];    // fragments of the step's halves
@@ -429,44 +487,54 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
 #pragma unroll
             for (int j = 0; j < P::FN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);
     };
-    // Interleaves the fragment reads (and the loads of the next step) of a half
-    // step with the products of the half step before.
-    auto weave = [&](bool loads) {
+    // Interleaves the fragment reads of a half step and its share of the loads
+    // with the products of the half step before.
+    auto weave = [&](auto n_loads) {
         constexpr int reads = P::FM * (P::ATR ? 2 : 1) + P::FN * (P::BTR ? 2 : 1), products = P::FM * P::FN;
-        constexpr int each = products / reads > 0 ? products / reads : 1;
+        constexpr int loads = decltype(n_loads)::value, each = products / reads > 0 ? products / reads : 1;
 #pragma unroll
         for (int i = 0; i < reads; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);          // an LDS read
+            if (i < loads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // a load
+            __builtin_amdgcn_sched_group_barrier(0x008, each, 0);       // products
         }
-        (void)loads;
     };
-    // One step.  At its barrier this step's loads have landed and every wave
-    // holds its fragments of the step before, so the other buffer is free: the
-    // next step's loads start, and the second half of the step before is
+    // One step, from buffer u.  At its barrier this step's loads have landed
+    // (those of later steps are in flight) and every wave holds its
+    // fragments of the step before, so that one's buffer is free: the loads
+    // kStages - 1 steps ahead start, and the second half of the step before is
     // multiplied while this step's first fragments are read.
-    auto turn = [&](int step, char* sa, char* sb, char* ta, char* tb, bool first) {
-        __syncthreads();
-        if (step + 1 < end) fetch(step + 1, ta, tb);
+    constexpr int kAhead = P::kStages - 1, kLoads = la.kChunks + lb.kChunks;
+    auto turn = [&](int step, int u, bool first) {
+        asm volatile("" ::: "memory");
+        wait_loads<(kAhead - 1) * kLoads>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        char* const ta = bufa((u + kAhead) % P::kStages);
+        char* const tb = bufb((u + kAhead) % P::kStages);
+        // woven, past the end the last step is fetched again, into a buffer that nothing reads
+        const int next = P::kWoven ? min(step + kAhead, end - 1) : step + kAhead;
+        if (!P::kWoven && next < end) fetch(next, ta, tb, Int<3>());
         __builtin_amdgcn_sched_barrier(0);
-        read(sa, sb, 0, fa0, fb0);
-        if (!first) {
-            multiply(fa1, fb1);
-            weave(true);
-        }
+        if (P::kWoven) fetch(next, ta, tb, Int<1>());
+        read(bufa(u), bufb(u), 0, fa0, fb0);
+        if (!first) multiply(fa1, fb1);
+        weave(Int<P::kWoven ? la.kChunks : 0>());
         __builtin_amdgcn_sched_barrier(0);
-        read(sa, sb, 1, fa1, fb1);
+        if (P::kWoven) fetch(next, ta, tb, Int<2>());
+        read(bufa(u), bufb(u), 1, fa1, fb1);
         multiply(fa0, fb0);
-        weave(false);
+        weave(Int<P::kWoven ? lb.kChunks : 0>());
         __builtin_amdgcn_sched_barrier(0);
     };
     if (s < end) {
-        fetch(s, sa0, sb0);
-        turn(s, sa0, sb0, sa1, sb1, true);
-        for (++s; s < end; s += 2) {
-            turn(s, sa1, sb1, sa0, sb0, false);
-            if (s + 1 < end) turn(s + 1, sa0, sb0, sa1, sb1, false);
-        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) fetch(min(s + u, end - 1), bufa(u), bufb(u), Int<3>());
+        turn(s, 0, true);
+        for (++s; s < end; s += P::kStages)
+#pragma unroll
+            for (int u = 0; u < P::kStages; ++u)
+                if (s + u < end) turn(s + u, (u + 1) % P::kStages, false);
         multiply(fa1, fb1);
     }
 
@@ -476,12 +544,10 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
     // stretches of rows.  The waves' quarters of the buffers lie in different
     // arrays or halves of them; a wave reads only what it wrote.
     constexpr int RW = P::BM / P::WM, CW = P::BN / P::WN, kWaves = P::WM * P::WN;
-    constexpr int kRows = 64, kPer = kWaves / 4;
+    constexpr int kRows = RW < 64 ? RW : 64, kPer = kWaves / 4;
     static_assert(kRows * CW * 4 * kPer <= P::BM * 128 && kPer * 4 == kWaves && P::BM == P::BN, "epilogue slices fit");
-    char* const bufs[4] = {sa0, sa1, sb0, sb1};
-    char* const mine = (wave & 2 ? (wave & 1 ? bufs[3] : bufs[2]) : (wave & 1 ? bufs[1] : bufs[0])) +
-                       (wave >> 2) * (kRows * CW * 4);
-    auto piece = [&](int r, int c4) { return (f32x4*)(mine + (r * (CW / 4) + (c4 ^ (r & 15))) * 16); };
+    char* const mine = (wave & 2 ? (wave & 1 ? sb1 : sb0) : (wave & 1 ? sa1 : sa0)) + (wave >> 2) * (kRows * CW * 4);
+    auto piece = [&](int r, int c4) { return (f32x4*)(mine + (r * (CW / 4) + (c4 ^ (r & (CW / 4 - 1) & 15))) * 16); };
     const int mw = m0 + wm * RW, nw = n0 + wn * (P::DUAL ? CW / 2 : CW);
     constexpr int kChunks = (P::DUAL ? CW / 2 : CW) / 8;      // of 8 columns a row
     const bool mirror = A.sym && tm != tn;
@@ -494,32 +560,44 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
             for (int j = 0; j < P::FN; ++j)
                 *piece(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[h * (kRows / 16) + i][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // kBatch pieces at a time, what they read from memory first
+        constexpr int kPieces = kRows * kChunks / 64, kBatch = kPieces < 4 ? kPieces : 4;
 #pragma unroll 1
-        for (int x = lane; x < kRows * kChunks; x += 64) {
-            const int r = x / kChunks, c = x % kChunks;
-            const int m = mw + h * kRows + r, n = nw + c * 8;
-            float v[8], u[8];
-            *(f32x4*)v = *piece(r, 2 * c);
-            *(f32x4*)(v + 4) = *piece(r, 2 * c + 1);
-            if (P::DUAL) {
-                *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
-                *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
+        for (int x0 = lane; x0 < kRows * kChunks; x0 += 64 * kBatch) {
+            Side<T, P::EPI> side[kBatch];
+#pragma unroll
+            for (int y = 0; y < kBatch; ++y) {
+                const int x = x0 + 64 * y, m = mw + h * kRows + x / kChunks, n = nw + x % kChunks * 8;
+                if (A.splits == 1 && m < A.M && n < (P::EPI == kPlain ? A.N : A.pad)) side[y].load(A, zb, m, n);
             }
-            if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
-            if (A.splits > 1) {
-                const int64_t plane = (int64_t)A.M * A.N;
-                float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) + (int64_t)m * A.N + n;
-                put(to, v, A.N - n);
-                if (P::DUAL) put(to + plane, u, A.N - n);
-            } else if constexpr (P::EPI == kGatedFwd) {
-                gated_fwd_out<T>(A, m, n, v, u);
-            } else if constexpr (P::EPI == kGatedBwd) {
-                gated_bwd_out<T>(A, m, n, v);
-            } else {
-                plain_out<T>(A, zb, m, n, v);
-                if (mirror) {
-                    *piece(r, 2 * c) = *(f32x4*)v;
-                    *piece(r, 2 * c + 1) = *(f32x4*)(v + 4);
+#pragma unroll
+            for (int y = 0; y < kBatch; ++y) {
+                const int x = x0 + 64 * y, r = x / kChunks, c = x % kChunks;
+                const int m = mw + h * kRows + r, n = nw + c * 8;
+                float v[8], u[8];
+                *(f32x4*)v = *piece(r, 2 * c);
+                *(f32x4*)(v + 4) = *piece(r, 2 * c + 1);
+                if (P::DUAL) {
+                    *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
+                    *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
+                }
+                if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
+                if (A.splits > 1) {
+                    const int64_t plane = (int64_t)A.M * A.N;
+                    float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) +
+                                (int64_t)m * A.N + n;
+                    put(to, v, A.N - n);
+                    if (P::DUAL) put(to + plane, u, A.N - n);
+                } else if constexpr (P::EPI == kGatedFwd) {
+                    gated_fwd_out<T>(A, m, n, v, u);
+                } else if constexpr (P::EPI == kGatedBwd) {
+                    gated_bwd_out<T>(A, m, n, v, side[y]);
+                } else {
+                    plain_out<T>(A, zb, m, n, v, side[y]);
+                    if (mirror) {
+                        *piece(r, 2 * c) = *(f32x4*)v;
+                        *piece(r, 2 * c + 1) = *(f32x4*)(v + 4);
+                    }
                 }
             }
         }
@@ -553,6 +631,9 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A)
     const int64_t plane = (int64_t)A.M * A.N, each = plane * A.batch * (EPI == kGatedFwd ? 2 : 1);
     const float* p = A.part + (int64_t)blockIdx.y * plane * (EPI == kGatedFwd ? 2 : 1) + (int64_t)m * A.N + n;
     float v[8] = {}, u[8] = {};
+    Side<T, EPI> side;
+    side.load(A, blockIdx.y, m, n);
+#pragma unroll 4
     for (int s = 0; s < A.splits; ++s) {
         float w[8];
         get(p + s * each, w, A.N - n);
@@ -564,8 +645,8 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A)
         for (int r = 0; r < 8; ++r) u[r] += w[r];
     }
     if constexpr (EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
-    else if constexpr (EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v);
-    else plain_out<T>(A, blockIdx.y, m, n, v);
+    else if constexpr (EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v, side);
+    else plain_out<T>(A, blockIdx.y, m, n, v, side);
 }
 
 // Few rows of A (tokens): nothing of B is used twice, so it goes from memory
@@ -657,7 +738,7 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
         if constexpr (DUAL) {
             if (n < A.pad) gated_fwd_out<T>(A, m, n, fv, fu);
         } else {
-            if (n < A.N) plain_out<T>(A, 0, m, n, fv);
+            if (n < A.N) plain_out<T>(A, 0, m, n, fv, Side<T, kPlain>());      // nothing is added here
         }
     }
 }
@@ -677,8 +758,13 @@ hipError_t launch_tile(const GemmArgs& A, hipStream_t s)
 template <typename T, bool ATR, bool BTR, int EPI>
 hipError_t launch_layout(const GemmArgs& A, int tile, hipStream_t s)
 {
-    if (tile == 256) return launch_tile<Tile<T, 256, 256, 2, 4, ATR, BTR, EPI>>(A, s);
-    return launch_tile<Tile<T, 128, 128, 2, 2, ATR, BTR, EPI>>(A, s);
+    switch (tile) {
+    case k256: return launch_tile<Tile<T, 256, 256, 2, 4, 2, ATR, BTR, EPI>>(A, s);
+    case k128: return launch_tile<Tile<T, 128, 128, 2, 2, 2, ATR, BTR, EPI>>(A, s);
+    case k128Deep: return launch_tile<Tile<T, 128, 128, 2, 2, 4, ATR, BTR, EPI>>(A, s);
+    case k64: return launch_tile<Tile<T, 64, 64, 2, 2, 4, ATR, BTR, EPI>>(A, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 template <typename T>

@@ -89,37 +89,54 @@ arena_status check_matrix(arena_ctx* c, const char* who, const char* name, const
 
 // ---------------------------------------------------------------- products
 
-// How a product is cut: the tile, and over how many parts of k.
+// How a product is cut: the kind of tile, and over how many parts of k.
 struct Cut {
     int tile, splits, per;
 };
 
-// Time of a product in microseconds as the tiles measured (one MI355X, 64 of k
-// a step): a 256 x 256 tile takes 1.95 us a step, one block a compute unit; a
-// 128 x 128 tile 1.13 us with two on a compute unit, 0.7 us alone; a block's
-// start and epilogue about 4 us; a split's parts are written and read once more.
-double cut_time(int64_t tiles, int64_t steps, int tile, int64_t splits, double part_mb)
+// What a kind of tile costs in microseconds (measured on one MI355X): a step
+// of 64 of k with every slot of the compute units taken and with at most one
+// block on each, a block's start, and how many blocks a compute unit holds.  A
+// compute unit moves about 20 KB of an epilogue's bytes a microsecond.
+struct TileCost {
+    double full, alone, start;
+    int slots;
+};
+constexpr TileCost kTileCost[arena::mm::kTileKinds] = {
+    {1.60, 1.30, 3.5, 1}, {0.90, 0.70, 3.4, 2}, {0.60, 0.55, 4.4, 1}, {0.41, 0.35, 3.0, 2}};
+constexpr double kEpilogueRate = 20e3;
+
+// A product of `tiles` tiles, `steps` of k over `splits` parts; bytes: what the
+// epilogue moves for a value of C; part_mb: megabytes of one part.  A split's
+// parts are written and read once more by a second launch.
+double cut_time(int64_t tiles, int64_t steps, int tile, int64_t splits, double bytes, double part_mb)
 {
+    const TileCost& k = kTileCost[tile];
     const int64_t per = ceil_div(steps, splits), blocks = tiles * splits;
-    if (tile == 256) return ceil_div(blocks, 256) * (per * 1.95 + 6.0);
-    const double step = blocks <= 256 ? 0.7 : 1.13;
-    return ceil_div(blocks, 512) * (per * step + 4.0) + (splits > 1 ? 4.0 + splits * part_mb * 0.5 : 0.0);
+    const bool full = blocks > 256;
+    const double values = (double)arena::mm::kTileSide[tile] * arena::mm::kTileSide[tile];
+    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate * (full ? k.slots : 1);
+    return ceil_div(blocks, 256 * k.slots) * (per * (full ? k.full : k.alone) + k.start + end) +
+           (splits > 1 ? 4.0 + splits * part_mb * 0.5 : 0.0);
 }
 
-// columns of C a tile covers: all of the tile, or half of it where gate and up share it
-Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual)
+// dual: gate and up share a tile, which then covers half as many columns.
+// bytes: what the epilogue moves for a column of the tile.
+Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, double bytes = 2.0)
 {
     const int half = dual ? 2 : 1;
-    const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256 / half) * batch;
-    const int64_t t128 = ceil_div(M, 128) * ceil_div(N, 128 / half) * batch;
     const double mb = 4e-6 * M * N * batch * half;
-    Cut best = {256, 1, (int)steps};
-    double least = cut_time(t256, steps, 256, 1, 0.0);
-    for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
-        const double t = cut_time(t128, steps, 128, s, mb);
-        if (t < least) {
-            least = t;
-            best = {128, s, (int)ceil_div(steps, s)};
+    Cut best = {arena::mm::k256, 1, (int)steps};
+    double least = INFINITY;
+    for (int tile = 0; tile < arena::mm::kTileKinds; ++tile) {
+        const int side = arena::mm::kTileSide[tile];
+        const int64_t tiles = ceil_div(M, side) * ceil_div(N, side / half) * batch;
+        for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
+            const double t = cut_time(tiles, steps, tile, s, bytes, mb);
+            if (t < least) {
+                least = t;
+                best = {tile, s, (int)ceil_div(steps, s)};
+            }
         }
     }
     best.splits = best.per > 0 ? (int)std::max<int64_t>(1, ceil_div(steps, best.per)) : 1;
@@ -133,8 +150,9 @@ int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, bool dua
 
 void set_cut(GemmArgs* A, const Cut& cut, bool dual, void* part)
 {
-    A->tiles_m = (int)ceil_div(A->M, cut.tile);
-    A->tiles_n = (int)ceil_div(A->N, dual ? cut.tile / 2 : cut.tile);
+    const int side = arena::mm::kTileSide[cut.tile];
+    A->tiles_m = (int)ceil_div(A->M, side);
+    A->tiles_n = (int)ceil_div(A->N, dual ? side / 2 : side);
     A->splits = cut.splits;
     A->per = cut.per;
     A->part = (float*)part;
@@ -150,7 +168,6 @@ GemmArgs new_args(int64_t M, int64_t N, int64_t K)
     A.nseg = 1;
     A.batch = 1;
     A.alpha = 1.0f;
-    A.vec = 1;
     return A;
 }
 
@@ -183,11 +200,6 @@ struct Operand {
         return copy ? arena::mm::launch_pack(from, ld_from, copy, ld, rows, cols, s) : hipSuccess;
     }
 };
-
-bool takes_four(const void* p, int64_t ld, int64_t stride, int size)
-{
-    return aligned(p, 4 * (size_t)size) && ld % 4 == 0 && stride % 4 == 0;
-}
 
 // ---------------------------------------------------------------- norms
 
@@ -331,7 +343,7 @@ struct ForwardPlan : FfnPlan {
     void* part;
     ForwardPlan(const arena_ffn_desc* d, void* base) : FfnPlan(d, d->tokens <= arena::mm::kSkinnyRows, base)
     {
-        cut_up = choose_cut(d->tokens, d->inner, ceil_div(d->model, arena::mm::kBK), 1, true);
+        cut_up = choose_cut(d->tokens, d->inner, ceil_div(d->model, arena::mm::kBK), 1, true, d->g ? 4.0 : 1.0);
         cut_down = choose_cut(d->tokens, d->model, ceil_div(d->inner, arena::mm::kBK), 1, false);
         part = w.take(skinny ? 0 : std::max(part_bytes(cut_up, d->tokens, d->inner, 1, true),
                                             part_bytes(cut_down, d->tokens, d->model, 1, false)));
@@ -353,7 +365,7 @@ struct BackwardPlan : FfnPlan {
         dg = w.take(2 * T * ld);
         du = w.take(2 * T * ld);
         pair = g->dw_gate && g->dw_up && g->ld_dw_gate == g->ld_dw_up;
-        cut_dh = choose_cut(T, F, ceil_div(D, bk), 1, false);
+        cut_dh = choose_cut(T, F, ceil_div(D, bk), 1, false, 10.0);
         cut_dx = choose_cut(T, D, 2 * ceil_div(F, bk), 1, false);
         cut_down = choose_cut(D, F, ceil_div(T, bk), 1, false);
         cut_up = choose_cut(F, D, ceil_div(T, bk), pair ? 2 : 1, false);
@@ -499,12 +511,12 @@ struct UpdatePlan {
     static Cut symmetric_cut(int64_t n, int64_t steps, int64_t batch, bool* sym)
     {
         Cut best = choose_cut(n, n, steps, batch, false);
-        const int64_t full = ceil_div(n, best.tile);
-        double least = cut_time(full * full * batch, steps, best.tile, best.splits, 4e-6 * n * n * batch);
+        const int64_t full = ceil_div(n, arena::mm::kTileSide[best.tile]);
+        double least = cut_time(full * full * batch, steps, best.tile, best.splits, 2.0, 4e-6 * n * n * batch);
         *sym = false;
-        for (int tile : {256, 128}) {
-            const int64_t t = ceil_div(n, tile);
-            const double time = cut_time(t * (t + 1) / 2 * batch, steps, tile, 1, 0.0);
+        for (int tile = 0; tile < arena::mm::kTileKinds; ++tile) {
+            const int64_t t = ceil_div(n, arena::mm::kTileSide[tile]);
+            const double time = cut_time(t * (t + 1) / 2 * batch, steps, tile, 1, 4.0, 0.0);
             if (time <= least) {
                 least = time;
                 best = {tile, 1, (int)steps};
@@ -629,7 +641,6 @@ arena_status arena_ffn_forward(arena_ctx* c, const arena_ffn_desc* d, void* stre
     B.a[0] = d->h; B.lda = d->ld_inner;
     B.b[0] = P.down.p; B.ldb = P.down.ld;
     B.c[0] = d->y; B.ldc = d->ld_y;
-    B.vec = takes_four(d->y, d->ld_y, 0, 2);
     set_cut(&B, P.cut_down, false, P.part);
     e = P.skinny ? arena::mm::launch_skinny(B, d->dtype, false, s)
                  : arena::mm::launch_gemm(B, d->dtype, arena::mm::kRowsRows, P.cut_down.tile, s);
@@ -661,7 +672,6 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
     const int64_t T = f->tokens, D = f->model, F = f->inner;
-    const int size = bytes_of(g->grad_dtype);
     const int out = g->grad_dtype == ARENA_F32 ? arena::mm::kOutF32 : arena::mm::kOut16;
     hipError_t e = P.pack(s);
     if (e || (e = P.dy.pack(s))) return hip_error(c, e, "ffn backward copies");
@@ -684,7 +694,6 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
         A.a[0] = P.dg; A.a[1] = P.du; A.lda = P.ld;
         A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld;
         A.c[0] = g->dx; A.ldc = g->ld_dx;
-        A.vec = takes_four(g->dx, g->ld_dx, 0, 2);
         set_cut(&A, P.cut_dx, false, P.part);
         if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kRowsCols, P.cut_dx.tile, s)))
             return hip_error(c, e, "ffn input gradient launch");
@@ -703,7 +712,6 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
             A.beta = 1.0f;
             A.e[0] = c0; A.e[1] = c1; A.lde = ldc;
         }
-        A.vec = takes_four(c0, ldc, 0, size) && takes_four(c1, ldc, 0, size);
         set_cut(&A, cut, false, P.part);
         return arena::mm::launch_gemm(A, f->dtype, arena::mm::kColsCols, cut.tile, s);
     };
@@ -813,7 +821,6 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
             X.beta *= d->scale * inv;
             X.c[0] = d->out; X.ldc = d->ld_out; X.sc = d->stride_out;
             X.out = d->out_dtype == ARENA_BF16 ? arena::mm::kOutBf16 : arena::mm::kOut16;
-            X.vec = takes_four(d->out, d->ld_out, d->batch > 1 ? d->stride_out : 0, 2);
         } else {
             X.c[0] = P.x[at ^ 1]; X.ldc = P.cols; X.sc = sx;
         }

@@ -35,7 +35,6 @@ struct GemmArgs {
     int32_t M, N, K;
     int32_t nseg, pairs, batch;
     int32_t tiles_m, tiles_n, sym;
-    int32_t vec;              // every matrix of the epilogue takes four columns at a time
     // plain: C = alpha * product + beta * e - diag on the diagonal
     const void* e[2];
     int64_t lde, se;
@@ -57,7 +56,13 @@ struct GemmArgs {
 // contiguous) and epilogue.
 enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack };
 
-// tile: 256 or 128.  The host has checked that operands are 16-byte aligned
+// Tiles: 256 x 256 (8 waves, two buffers, one block on a compute unit), 128 x 128
+// (4 waves) with two buffers (two blocks) or four (one block), 64 x 64 (4 waves,
+// four buffers, two blocks).
+enum TileKind { k256 = 0, k128, k128Deep, k64, kTileKinds };
+constexpr int kTileSide[kTileKinds] = {256, 128, 128, 64};
+
+// tile: a TileKind.  The host has checked that operands are 16-byte aligned
 // with strides and batch strides of multiples of 8, and that values between
 // the matrix's edge and the next multiple of 8 along the contiguous axis are
 // readable (and zero where that axis is k).
