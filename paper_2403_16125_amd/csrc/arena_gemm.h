@@ -30,6 +30,7 @@ namespace mm {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 struct Bf16 {
@@ -52,21 +53,24 @@ struct F16 {
     }
 };
 
-// act(z) and act'(z).
-__device__ __forceinline__ float act_value(float z, int act)
+// act(z), and with it act'(z).  Reciprocals and exponentials are the hardware's
+// (one unit in the last place), far inside the 16 bits that results keep.
+template <int ACT>
+__device__ __forceinline__ float act_value(float z)
 {
-    if (act == kSilu) return z / (1.0f + __expf(-z));
-    if (act == kGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (ACT == kSilu) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    if (ACT == kGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     return z > 0.0f ? z : (z == z ? 0.0f : z);
 }
 
-__device__ __forceinline__ void act_both(float z, int act, float* v, float* d)
+template <int ACT>
+__device__ __forceinline__ void act_both(float z, float* v, float* d)
 {
-    if (act == kSilu) {
-        const float s = 1.0f / (1.0f + __expf(-z));
+    if (ACT == kSilu) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
         *v = z * s;
-        *d = s * (1.0f + z * (1.0f - s));
-    } else if (act == kGelu) {
+        *d = s + *v * (1.0f - s);
+    } else if (ACT == kGelu) {
         const float c = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
         *v = z * c;
         *d = c + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
@@ -242,17 +246,39 @@ __device__ __forceinline__ void get(const E* p, float (&v)[C], int left)
 template <typename T, int EPI>
 struct Side;
 
-// plain: the added matrix.
+// plain: the added matrix, as it lies in memory (16-bit values in raw[0]).
 template <typename T>
 struct Side<T, kPlain> {
-    float e[8];
+    u32x4 raw[2];
     __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
     {
         if (A.beta == 0.0f) return;
-        const void* p = A.e[A.pairs ? z : 0];
+        const char* p = (const char*)A.e[A.pairs ? z : 0];
         const int64_t from = (A.pairs ? 0 : z * A.se) + (int64_t)m * A.lde + n;
-        if (A.out == kOutF32) get((const float*)p + from, e, A.N - n);
-        else get((const typename T::E*)p + from, e, A.N - n);
+        const int left = A.N - n;
+        if (A.out == kOutF32) {
+            const uint32_t* q = (const uint32_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 32);
+            else
+#pragma unroll
+                for (int r = 0; r < 8; ++r) raw[r >> 2][r & 3] = r < left ? q[r] : 0;
+        } else {
+            const uint16_t* q = (const uint16_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 16);
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    raw[0][r] = (2 * r < left ? q[2 * r] : 0) | (2 * r + 1 < left ? (uint32_t)q[2 * r + 1] << 16 : 0);
+        }
+    }
+    __device__ __forceinline__ float get(int r, bool f32) const
+    {
+        typedef typename T::E E;
+        if (f32) return __uint_as_float(raw[r >> 2][r & 3]);
+        const uint16_t h = (uint16_t)(raw[0][r >> 1] >> (16 * (r & 1)));
+        E e;
+        __builtin_memcpy(&e, &h, 2);
+        return (float)e;
     }
 };
 
@@ -264,15 +290,20 @@ struct Side<T, kGatedFwd> {
 // gated, backward: the heads and tails of the kept gate and up values.
 template <typename T>
 struct Side<T, kGatedBwd> {
-    uint16_t gh[8], uh[8];
-    uint8_t gt[8], ut[8];
+    u32x4 gh, uh;
+    u32x2 gt, ut;
     __device__ __forceinline__ void load(const GemmArgs& A, int, int m, int n)
     {
         const int64_t at = (int64_t)m * A.ldg + n, tails = 2 * (int64_t)A.M * A.ldg + at;
-        __builtin_memcpy(gh, (const uint16_t*)A.g + at, sizeof(gh));
-        __builtin_memcpy(uh, (const uint16_t*)A.u + at, sizeof(uh));
-        __builtin_memcpy(gt, (const uint8_t*)A.g + tails, sizeof(gt));
-        __builtin_memcpy(ut, (const uint8_t*)A.u + tails, sizeof(ut));
+        gh = *(const u32x4*)((const uint16_t*)A.g + at);
+        uh = *(const u32x4*)((const uint16_t*)A.u + at);
+        gt = *(const u32x2*)((const uint8_t*)A.g + tails);
+        ut = *(const u32x2*)((const uint8_t*)A.u + tails);
+    }
+    static __device__ __forceinline__ float value(u32x4 head, u32x2 tail, int r)
+    {
+        const uint32_t h = (head[r >> 1] >> (16 * (r & 1))) & 0xffff, t = (tail[r >> 2] >> (8 * (r & 3))) & 0xff;
+        return __uint_as_float(h << 16 | t << 8);
     }
 };
 
@@ -290,7 +321,7 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
     for (int r = 0; r < C; ++r) v[r] *= A.alpha;
     if (A.beta != 0.0f)
 #pragma unroll
-        for (int r = 0; r < C; ++r) v[r] += A.beta * side.e[r];
+        for (int r = 0; r < C; ++r) v[r] += A.beta * side.get(r, A.out == kOutF32);
     if (A.diag != 0.0f)
 #pragma unroll
         for (int r = 0; r < C; ++r)
@@ -321,16 +352,11 @@ __device__ __forceinline__ void put24(void* p, const GemmArgs& A, int m, int n, 
     __builtin_memcpy((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, tail, sizeof(tail));
 }
 
-__device__ __forceinline__ float from24(uint16_t head, uint8_t tail)
-{
-    return __uint_as_float((uint32_t)head << 16 | (uint32_t)tail << 8);
-}
-
 // h = act(g) u from the 32-bit sums, rounded to 16 bits as the next product's
 // operand.  n and pad are multiples of C's and of 8, so C columns are all
 // inside pad.
-template <typename T, int C>
-__device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, float (&g)[C], float (&u)[C])
+template <typename T, int ACT, int C>
+__device__ __forceinline__ void gated_fwd(const GemmArgs& A, int m, int n, float (&g)[C], float (&u)[C])
 {
     typedef typename T::E E;
     float h[C];
@@ -339,7 +365,7 @@ __device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, f
         const bool in = n + r < A.N;
         g[r] = in ? g[r] : 0.0f;
         u[r] = in ? u[r] : 0.0f;
-        h[r] = in ? act_value(g[r], A.act) * u[r] : 0.0f;
+        h[r] = in ? act_value<ACT>(g[r]) * u[r] : 0.0f;
     }
     put((E*)A.c[0] + (int64_t)m * A.ldc + n, h, C);
     if (A.g) {
@@ -348,9 +374,17 @@ __device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, f
     }
 }
 
+template <typename T, int C>
+__device__ __forceinline__ void gated_fwd_out(const GemmArgs& A, int m, int n, float (&g)[C], float (&u)[C])
+{
+    if (A.act == kSilu) gated_fwd<T, kSilu>(A, m, n, g, u);
+    else if (A.act == kGelu) gated_fwd<T, kGelu>(A, m, n, g, u);
+    else gated_fwd<T, kRelu>(A, m, n, g, u);
+}
+
 // v = the gradient of h = act(g) u:  of g  v u act'(g),  of u  v act(g).
-template <typename T>
-__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, const float (&v)[8],
+template <typename T, int ACT>
+__device__ __forceinline__ void gated_bwd(const GemmArgs& A, int m, int n, const float (&v)[8],
                                               const Side<T, kGatedBwd>& side)
 {
     typedef typename T::E E;
@@ -359,12 +393,21 @@ __device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, c
     for (int r = 0; r < 8; ++r) {
         const bool in = n + r < A.N;
         float a, d;
-        act_both(from24(side.gh[r], side.gt[r]), A.act, &a, &d);
+        act_both<ACT>(side.value(side.gh, side.gt, r), &a, &d);
         du[r] = in ? v[r] * a : 0.0f;
-        dg[r] = in ? v[r] * from24(side.uh[r], side.ut[r]) * d : 0.0f;
+        dg[r] = in ? v[r] * side.value(side.uh, side.ut, r) * d : 0.0f;
     }
     put((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, 8);
     put((E*)A.c[1] + (int64_t)m * A.ldc + n, du, 8);
+}
+
+template <typename T>
+__device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, const float (&v)[8],
+                                              const Side<T, kGatedBwd>& side)
+{
+    if (A.act == kSilu) gated_bwd<T, kSilu>(A, m, n, v, side);
+    else if (A.act == kGelu) gated_bwd<T, kGelu>(A, m, n, v, side);
+    else gated_bwd<T, kRelu>(A, m, n, v, side);
 }
 
 // Tile of a block: blocks go to the 8 XCDs in turn, so each XCD gets a run of
@@ -474,6 +517,24 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
             if (which.value & 2) lb.template fetch<false>(pb, pb1, sb, tid, left);
         }
     };
+    // What the epilogue reads from memory, in batches of pieces of 8 columns: the
+    // first batch while the products run, each other while the one before is
+    // finished.
+    constexpr int RW = P::BM / P::WM, CW = P::BN / P::WN, kWaves = P::WM * P::WN;
+    constexpr int kRows = RW < 64 ? RW : 64;                  // of a slice through LDS
+    constexpr int kChunks = (P::DUAL ? CW / 2 : CW) / 8;      // pieces of a row
+    constexpr int kPieces = kRows * kChunks / 64, kBatch = kPieces < 4 ? kPieces : 4, kAll = kPieces * (RW / kRows);
+    const int mw = m0 + wm * RW, nw = n0 + wn * (P::DUAL ? CW / 2 : CW);
+    Side<T, P::EPI> side[kBatch], next_side[kBatch];
+    auto ask = [&](int at, Side<T, P::EPI>* to) {
+        if (A.splits > 1 || at >= kAll) return;
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+            const int x = (at + q) * 64 + lane, m = mw + x / kChunks, n = nw + x % kChunks * 8;
+            if (m < A.M && n < (P::EPI == kPlain ? A.N : A.pad)) to[q].load(A, zb, m, n);
+        }
+    };
+
     typename T::V8 fa0[P::FM], fb0[P::FN], fa1[P::FM], fb1[P::FN];    // fragments of the step's halves
     auto read = [&](const char* sa, const char* sb, int kk, typename T::V8* a, typename T::V8* b) {
 #pragma unroll
@@ -527,6 +588,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
         weave(Int<P::kWoven ? lb.kChunks : 0>());
         __builtin_amdgcn_sched_barrier(0);
     };
+    if (P::BM < 256) ask(0, side);
     if (s < end) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) fetch(min(s + u, end - 1), bufa(u), bufb(u), Int<3>());
@@ -543,14 +605,40 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
     // swizzled by row) it gets 8 neighbouring columns, and the wave whole
     // stretches of rows.  The waves' quarters of the buffers lie in different
     // arrays or halves of them; a wave reads only what it wrote.
-    constexpr int RW = P::BM / P::WM, CW = P::BN / P::WN, kWaves = P::WM * P::WN;
-    constexpr int kRows = RW < 64 ? RW : 64, kPer = kWaves / 4;
-    static_assert(kRows * CW * 4 * kPer <= P::BM * 128 && kPer * 4 == kWaves && P::BM == P::BN, "epilogue slices fit");
+    static_assert(kRows * CW * 4 * (kWaves / 4) <= P::BM * 128 && kWaves % 4 == 0 && P::BM == P::BN,
+                  "epilogue slices fit");
     char* const mine = (wave & 2 ? (wave & 1 ? sb1 : sb0) : (wave & 1 ? sa1 : sa0)) + (wave >> 2) * (kRows * CW * 4);
     auto piece = [&](int r, int c4) { return (f32x4*)(mine + (r * (CW / 4) + (c4 ^ (r & (CW / 4 - 1) & 15))) * 16); };
-    const int mw = m0 + wm * RW, nw = n0 + wn * (P::DUAL ? CW / 2 : CW);
-    constexpr int kChunks = (P::DUAL ? CW / 2 : CW) / 8;      // of 8 columns a row
     const bool mirror = A.sym && tm != tn;
+    auto finish = [&](int x, const Side<T, P::EPI>& from) {
+        const int r = x / kChunks % kRows, c = x % kChunks;
+        const int m = mw + x / kChunks, n = nw + c * 8;
+        float v[8], u[8];
+        *(f32x4*)v = *piece(r, 2 * c);
+        *(f32x4*)(v + 4) = *piece(r, 2 * c + 1);
+        if (P::DUAL) {
+            *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
+            *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
+        }
+        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) return;
+        if (A.splits > 1) {
+            const int64_t plane = (int64_t)A.M * A.N;
+            float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) + (int64_t)m * A.N + n;
+            put(to, v, A.N - n);
+            if (P::DUAL) put(to + plane, u, A.N - n);
+        } else if constexpr (P::EPI == kGatedFwd) {
+            gated_fwd_out<T>(A, m, n, v, u);
+        } else if constexpr (P::EPI == kGatedBwd) {
+            gated_bwd_out<T>(A, m, n, v, from);
+        } else {
+            plain_out<T>(A, zb, m, n, v, from);
+            if (mirror) {
+                *piece(r, 2 * c) = *(f32x4*)v;
+                *piece(r, 2 * c + 1) = *(f32x4*)(v + 4);
+            }
+        }
+    };
+    if (P::BM == 256) ask(0, side);      // no registers are left for it before
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < RW / kRows; ++h) {
@@ -560,46 +648,14 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
             for (int j = 0; j < P::FN; ++j)
                 *piece(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[h * (kRows / 16) + i][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        // kBatch pieces at a time, what they read from memory first
-        constexpr int kPieces = kRows * kChunks / 64, kBatch = kPieces < 4 ? kPieces : 4;
 #pragma unroll 1
-        for (int x0 = lane; x0 < kRows * kChunks; x0 += 64 * kBatch) {
-            Side<T, P::EPI> side[kBatch];
+        for (int y = 0; y < kPieces; y += kBatch) {
+            const int at = h * kPieces + y;
+            ask(at + kBatch, next_side);
 #pragma unroll
-            for (int y = 0; y < kBatch; ++y) {
-                const int x = x0 + 64 * y, m = mw + h * kRows + x / kChunks, n = nw + x % kChunks * 8;
-                if (A.splits == 1 && m < A.M && n < (P::EPI == kPlain ? A.N : A.pad)) side[y].load(A, zb, m, n);
-            }
+            for (int q = 0; q < kBatch; ++q) finish((at + q) * 64 + lane, side[q]);
 #pragma unroll
-            for (int y = 0; y < kBatch; ++y) {
-                const int x = x0 + 64 * y, r = x / kChunks, c = x % kChunks;
-                const int m = mw + h * kRows + r, n = nw + c * 8;
-                float v[8], u[8];
-                *(f32x4*)v = *piece(r, 2 * c);
-                *(f32x4*)(v + 4) = *piece(r, 2 * c + 1);
-                if (P::DUAL) {
-                    *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
-                    *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
-                }
-                if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
-                if (A.splits > 1) {
-                    const int64_t plane = (int64_t)A.M * A.N;
-                    float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) +
-                                (int64_t)m * A.N + n;
-                    put(to, v, A.N - n);
-                    if (P::DUAL) put(to + plane, u, A.N - n);
-                } else if constexpr (P::EPI == kGatedFwd) {
-                    gated_fwd_out<T>(A, m, n, v, u);
-                } else if constexpr (P::EPI == kGatedBwd) {
-                    gated_bwd_out<T>(A, m, n, v, side[y]);
-                } else {
-                    plain_out<T>(A, zb, m, n, v, side[y]);
-                    if (mirror) {
-                        *piece(r, 2 * c) = *(f32x4*)v;
-                        *piece(r, 2 * c + 1) = *(f32x4*)(v + 4);
-                    }
-                }
-            }
+            for (int q = 0; q < kBatch; ++q) side[q] = next_side[q];
         }
         if (P::EPI == kPlain && mirror) {
             // the transposed tile: 8 rows of a column are 8 columns of its row

@@ -97,14 +97,14 @@ struct Cut {
 // What a kind of tile costs in microseconds (measured on one MI355X): a step
 // of 64 of k with every slot of the compute units taken and with at most one
 // block on each, a block's start, and how many blocks a compute unit holds.  A
-// compute unit moves about 20 KB of an epilogue's bytes a microsecond.
+// compute unit moves about 40 KB of an epilogue's bytes a microsecond.
 struct TileCost {
     double full, alone, start;
     int slots;
 };
 constexpr TileCost kTileCost[arena::mm::kTileKinds] = {
-    {1.60, 1.30, 3.5, 1}, {0.90, 0.70, 3.4, 2}, {0.60, 0.55, 4.4, 1}, {0.41, 0.35, 3.0, 2}};
-constexpr double kEpilogueRate = 20e3;
+    {1.60, 1.30, 5.0, 1}, {0.90, 0.67, 2.6, 2}, {0.60, 0.55, 3.2, 1}, {0.41, 0.35, 1.0, 2}};
+constexpr double kEpilogueRate = 40e3;
 
 // A product of `tiles` tiles, `steps` of k over `splits` parts; bytes: what the
 // epilogue moves for a value of C; part_mb: megabytes of one part.  A split's
