@@ -410,26 +410,62 @@ __device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, c
     else gated_bwd<T, kRelu>(A, m, n, v, side);
 }
 
-// Tile of a block: blocks go to the 8 XCDs in turn, so each XCD gets a run of
-// consecutive tiles (its L2 then holds the operands that they share), taken in
+// Where the t-th tile of a launch lies; false if it is none (past the edge, or
+// above the diagonal of a symmetric product).  Tiles of the product come in
 // bands of 8 tile rows.
-__device__ __forceinline__ void tile_of(int bid, int n_blocks, int tiles_m, int tiles_n, bool sym, int* tm, int* tn)
+struct Place {
+    int m0, n0, z;
+    bool mirror;         // symmetric and off the diagonal: the transposed tile is written too
+};
+
+// a / b by a reciprocal, corrected: what comes before a block's first load is
+// on the path of a short product.
+__device__ __forceinline__ int quotient(int a, int b)
+{
+    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
+    while (r < 0) { --q; r += b; }
+    while (r >= b) { ++q; r -= b; }
+    return __builtin_amdgcn_readfirstlane(q);
+}
+
+template <typename P>
+__device__ __forceinline__ bool place_of(const GemmArgs& A, int t, Place* at)
+{
+    const int sub = t & ((1 << 2 * A.ratio) - 1);
+    int tile = A.first + (t >> 2 * A.ratio), tm, tn;
+    at->z = 0;
+    if (A.batch > 1) {
+        const int tiles = A.sym ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n;
+        at->z = quotient(tile, tiles);
+        tile -= at->z * tiles;
+    }
+    if (A.sym) {
+        tm = (int)((__builtin_amdgcn_sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+        while (tm * (tm + 1) / 2 > tile) --tm;
+        while ((tm + 1) * (tm + 2) / 2 <= tile) ++tm;
+        tm = __builtin_amdgcn_readfirstlane(tm);
+        tn = tile - tm * (tm + 1) / 2;
+    } else {
+        const int band = 8 * A.tiles_n, b = quotient(tile, band), in = tile - b * band;
+        const int rows = min(8, A.tiles_m - b * 8);
+        tn = quotient(in, rows);
+        tm = b * 8 + in - tn * rows;
+    }
+    tm = (tm << A.ratio) + (sub >> A.ratio);
+    tn = (tn << A.ratio) + (sub & ((1 << A.ratio) - 1));
+    at->m0 = tm * P::BM;
+    at->n0 = tn * P::kCols;
+    at->mirror = A.sym && tm != tn;
+    return at->m0 < A.M && at->n0 < A.N && !(A.sym && tm < tn);
+}
+
+// Blocks go to the 8 XCDs in turn, so each XCD gets a run of consecutive tiles:
+// its L2 then holds the operands that they share.
+__device__ __forceinline__ int tile_of(int bid, int n_blocks)
 {
     const int per = n_blocks >> 3, more = n_blocks & 7;
     const int x = bid & 7, i = bid >> 3;
-    const int t = x * per + min(x, more) + i;
-    if (sym) {
-        int r = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-        while (r * (r + 1) / 2 > t) --r;
-        while ((r + 1) * (r + 2) / 2 <= t) ++r;
-        *tm = r;
-        *tn = t - r * (r + 1) / 2;
-        return;
-    }
-    const int band = 8 * tiles_n, b = t / band, in = t - b * band;
-    const int rows = min(8, tiles_m - b * 8);
-    *tm = b * 8 + in % rows;
-    *tn = in / rows;
+    return x * per + min(x, more) + i;
 }
 
 template <int N>
@@ -465,10 +501,10 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
-    int tm, tn;
-    tile_of(blockIdx.x, gridDim.x, A.tiles_m, A.tiles_n, A.sym, &tm, &tn);
-    const int zb = blockIdx.y;                 // batch index
-    const int m0 = tm * P::BM, n0 = tn * P::kCols;
+    Place at;
+    const int t = tile_of(blockIdx.x, gridDim.x);
+    if (!place_of<P>(A, t, &at)) return;
+    const int zb = at.z, m0 = at.m0, n0 = at.n0;
 
     Loader<P, P::BM, P::ATR, false> la;
     Loader<P, P::BN, P::BTR, P::DUAL> lb;
@@ -488,7 +524,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
     const int sps = (A.K + kBK - 1) / kBK;     // steps of a segment
     int s = 0, end = sps * A.nseg;
     if (A.splits > 1) {
-        s = blockIdx.z * A.per;
+        s = blockIdx.y * A.per;
         end = min(end, s + A.per);
     }
     const int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
@@ -609,7 +645,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
                   "epilogue slices fit");
     char* const mine = (wave & 2 ? (wave & 1 ? sb1 : sb0) : (wave & 1 ? sa1 : sa0)) + (wave >> 2) * (kRows * CW * 4);
     auto piece = [&](int r, int c4) { return (f32x4*)(mine + (r * (CW / 4) + (c4 ^ (r & (CW / 4 - 1) & 15))) * 16); };
-    const bool mirror = A.sym && tm != tn;
+    const bool mirror = at.mirror && A.splits == 1;
     auto finish = [&](int x, const Side<T, P::EPI>& from) {
         const int r = x / kChunks % kRows, c = x % kChunks;
         const int m = mw + x / kChunks, n = nw + c * 8;
@@ -622,11 +658,12 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
         }
         if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) return;
         if (A.splits > 1) {
-            const int64_t plane = (int64_t)A.M * A.N;
-            float* to = A.part + ((int64_t)blockIdx.z * A.batch + zb) * plane * (P::DUAL ? 2 : 1) + (int64_t)m * A.N + n;
-            put(to, v, A.N - n);
-            if (P::DUAL) put(to + plane, u, A.N - n);
-        } else if constexpr (P::EPI == kGatedFwd) {
+            float* to = A.part + ((int64_t)blockIdx.y * gridDim.x + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
+            put(to, v, 8);
+            if (P::DUAL) put(to + P::BM * P::kCols, u, 8);
+            return;
+        }
+        if constexpr (P::EPI == kGatedFwd) {
             gated_fwd_out<T>(A, m, n, v, u);
         } else if constexpr (P::EPI == kGatedBwd) {
             gated_bwd_out<T>(A, m, n, v, from);
@@ -675,34 +712,60 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
     }
 }
 
-// Joins the parts of a split product in their order and applies the epilogue;
-// a thread takes eight columns of a row.
-template <typename T, int EPI>
-__global__ __launch_bounds__(256) void join_kernel(const GemmArgs A)
+// Joins the parts of the tiles of a split product in their order and applies
+// the epilogue.  A block takes 64 rows and up to 64 columns of a tile, a thread
+// one or two pieces of eight columns.
+template <typename P>
+__global__ __launch_bounds__(256) void join_kernel(const GemmArgs A, int n_tiles)
 {
-    const int per = ((EPI == kPlain ? A.N : A.pad) + 7) / 8;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)A.M * per) return;
-    const int m = (int)(i / per), n = (int)(i % per) * 8;
-    const int64_t plane = (int64_t)A.M * A.N, each = plane * A.batch * (EPI == kGatedFwd ? 2 : 1);
-    const float* p = A.part + (int64_t)blockIdx.y * plane * (EPI == kGatedFwd ? 2 : 1) + (int64_t)m * A.N + n;
-    float v[8] = {}, u[8] = {};
-    Side<T, EPI> side;
-    side.load(A, blockIdx.y, m, n);
+    typedef typename P::T T;
+    constexpr int CW = P::kCols < 64 ? P::kCols : 64, kChunks = CW / 8, kAcross = P::kCols / CW;
+    constexpr int kEach = (P::BM / 64) * kAcross;         // blocks of a tile
+    __shared__ float turned[P::EPI == kPlain ? 64 : 1][65];
+    const int t = blockIdx.x / kEach, in = blockIdx.x % kEach;
+    const int r0 = in / kAcross * 64, c0 = in % kAcross * CW;
+    Place at;
+    if (!place_of<P>(A, t, &at)) return;
+    const int64_t each = (int64_t)n_tiles * (P::BM * P::BN);
+    const float* part = A.part + (int64_t)t * (P::BM * P::BN);
+#pragma unroll 1
+    for (int x = threadIdx.x; x < 64 * kChunks; x += 256) {
+        const int r = x / kChunks, c = x % kChunks * 8;
+        const int m = at.m0 + r0 + r, n = at.n0 + c0 + c;
+        const float* p = part + (r0 + r) * P::kCols + c0 + c;
+        float v[8] = {}, u[8] = {};
+        Side<T, P::EPI> side;
+        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
+        side.load(A, at.z, m, n);
 #pragma unroll 4
-    for (int s = 0; s < A.splits; ++s) {
-        float w[8];
-        get(p + s * each, w, A.N - n);
+        for (int s = 0; s < A.splits; ++s) {
+            float w[8];
+            get(p + s * each, w, 8);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] += w[r];
-        if (EPI != kGatedFwd) continue;
-        get(p + s * each + plane, w, A.N - n);
+            for (int q = 0; q < 8; ++q) v[q] += w[q];
+            if (!P::DUAL) continue;
+            get(p + s * each + P::BM * P::kCols, w, 8);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) u[r] += w[r];
+            for (int q = 0; q < 8; ++q) u[q] += w[q];
+        }
+        if constexpr (P::EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
+        else if constexpr (P::EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v, side);
+        else plain_out<T>(A, at.z, m, n, v, side);
+        if (P::EPI == kPlain && at.mirror)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) turned[r][c + q] = v[q];
     }
-    if constexpr (EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
-    else if constexpr (EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v, side);
-    else plain_out<T>(A, blockIdx.y, m, n, v, side);
+    if (P::EPI != kPlain || !at.mirror) return;
+    __syncthreads();
+    for (int x = threadIdx.x; x < CW * 8; x += 256) {
+        const int c = x / 8, r = x % 8 * 8;
+        const int m = at.m0 + r0 + r, n = at.n0 + c0 + c;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = turned[P::EPI == kPlain ? r + q : 0][c];
+        if (m < A.M && n < A.N)
+            put((typename T::E*)A.c[0] + at.z * A.sc + (int64_t)n * A.ldc + m, v, A.M - m);
+    }
 }
 
 // Few rows of A (tokens): nothing of B is used twice, so it goes from memory
@@ -800,38 +863,57 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
 }
 
 template <typename P>
-hipError_t launch_tile(const GemmArgs& A, hipStream_t s)
+hipError_t launch_tile(const GemmArgs& A, int64_t n_tiles, hipStream_t s)
 {
-    gemm_kernel<P><<<dim3(A.sym ? A.tiles_m * (A.tiles_m + 1) / 2 : A.tiles_m * A.tiles_n, A.batch, A.splits),
-                     P::kThreads, 0, s>>>(A);
+    if (n_tiles == 0) return hipSuccess;
+    gemm_kernel<P><<<dim3((unsigned)n_tiles, A.splits), P::kThreads, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    const int64_t n = (int64_t)A.M * (((P::EPI == kPlain ? A.N : A.pad) + 7) / 8);
-    join_kernel<typename P::T, P::EPI><<<dim3((unsigned)((n + 255) / 256), A.batch), 256, 0, s>>>(A);
+    constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
+    join_kernel<P><<<(unsigned)(n_tiles * kEach), 256, 0, s>>>(A, (int)n_tiles);
     return hipGetLastError();
 }
 
 template <typename T, bool ATR, bool BTR, int EPI>
-hipError_t launch_layout(const GemmArgs& A, int tile, hipStream_t s)
+hipError_t launch_kind(const GemmArgs& A, int kind, int64_t n_tiles, hipStream_t s)
 {
-    switch (tile) {
-    case k256: return launch_tile<Tile<T, 256, 256, 2, 4, 2, ATR, BTR, EPI>>(A, s);
-    case k128: return launch_tile<Tile<T, 128, 128, 2, 2, 2, ATR, BTR, EPI>>(A, s);
-    case k128Deep: return launch_tile<Tile<T, 128, 128, 2, 2, 4, ATR, BTR, EPI>>(A, s);
-    case k64: return launch_tile<Tile<T, 64, 64, 2, 2, 4, ATR, BTR, EPI>>(A, s);
+    switch (kind) {
+    case k256: return launch_tile<Tile<T, 256, 256, 2, 4, 2, ATR, BTR, EPI>>(A, n_tiles, s);
+    case k128: return launch_tile<Tile<T, 128, 128, 2, 2, 2, ATR, BTR, EPI>>(A, n_tiles, s);
+    case k128Deep: return launch_tile<Tile<T, 128, 128, 2, 2, 4, ATR, BTR, EPI>>(A, n_tiles, s);
+    case k64: return launch_tile<Tile<T, 64, 64, 2, 2, 4, ATR, BTR, EPI>>(A, n_tiles, s);
     }
     return hipErrorInvalidValue;
 }
 
+template <typename T, bool ATR, bool BTR, int EPI>
+hipError_t launch_layout(GemmArgs A, const Cut& cut, hipStream_t s)
+{
+    const int side = kTileSide[cut.main], cols = EPI == kGatedFwd ? side / 2 : side;
+    A.tiles_m = (A.M + side - 1) / side;
+    A.tiles_n = (A.N + cols - 1) / cols;
+    const int64_t all = (A.sym ? (int64_t)A.tiles_m * (A.tiles_m + 1) / 2 : (int64_t)A.tiles_m * A.tiles_n) * A.batch;
+    A.splits = 1;
+    A.first = 0;
+    A.ratio = 0;
+    const hipError_t e = launch_kind<T, ATR, BTR, EPI>(A, cut.main, cut.first, s);
+    if (e != hipSuccess || cut.first == all) return e;
+    A.splits = cut.splits;
+    A.per = cut.per;
+    A.first = (int)cut.first;
+    while (kTileSide[cut.tail] << A.ratio < side) ++A.ratio;
+    return launch_kind<T, ATR, BTR, EPI>(A, cut.tail, (all - cut.first) << 2 * A.ratio, s);
+}
+
 template <typename T>
-hipError_t launch_gemm_t(const GemmArgs& A, Product what, int tile, hipStream_t s)
+hipError_t launch_gemm_t(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
 {
     switch (what) {
-    case kRowsRows: return launch_layout<T, false, false, kPlain>(A, tile, s);
-    case kRowsCols: return launch_layout<T, false, true, kPlain>(A, tile, s);
-    case kColsCols: return launch_layout<T, true, true, kPlain>(A, tile, s);
-    case kGateUp: return launch_layout<T, false, false, kGatedFwd>(A, tile, s);
-    case kGateUpBack: return launch_layout<T, false, true, kGatedBwd>(A, tile, s);
+    case kRowsRows: return launch_layout<T, false, false, kPlain>(A, cut, s);
+    case kRowsCols: return launch_layout<T, false, true, kPlain>(A, cut, s);
+    case kColsCols: return launch_layout<T, true, true, kPlain>(A, cut, s);
+    case kGateUp: return launch_layout<T, false, false, kGatedFwd>(A, cut, s);
+    case kGateUpBack: return launch_layout<T, false, true, kGatedBwd>(A, cut, s);
     }
     return hipErrorInvalidValue;
 }

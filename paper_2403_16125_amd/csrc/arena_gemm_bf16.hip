@@ -4,12 +4,12 @@
 namespace arena {
 namespace mm {
 
-hipError_t launch_gemm_f16(const GemmArgs& A, Product what, int tile, hipStream_t s);
+hipError_t launch_gemm_f16(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s);
 hipError_t launch_skinny_f16(const GemmArgs& A, bool dual, hipStream_t s);
 
-hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, int tile, hipStream_t s)
+hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s)
 {
-    return dtype == ARENA_BF16 ? launch_gemm_t<Bf16>(A, what, tile, s) : launch_gemm_f16(A, what, tile, s);
+    return dtype == ARENA_BF16 ? launch_gemm_t<Bf16>(A, what, cut, s) : launch_gemm_f16(A, what, cut, s);
 }
 
 hipError_t launch_skinny(const GemmArgs& A, int dtype, bool dual, hipStream_t s)

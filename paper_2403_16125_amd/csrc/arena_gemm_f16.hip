@@ -4,9 +4,9 @@
 namespace arena {
 namespace mm {
 
-hipError_t launch_gemm_f16(const GemmArgs& A, Product what, int tile, hipStream_t s)
+hipError_t launch_gemm_f16(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
 {
-    return launch_gemm_t<F16>(A, what, tile, s);
+    return launch_gemm_t<F16>(A, what, cut, s);
 }
 
 hipError_t launch_skinny_f16(const GemmArgs& A, bool dual, hipStream_t s) { return launch_skinny_t<F16>(A, dual, s); }

@@ -89,10 +89,7 @@ arena_status check_matrix(arena_ctx* c, const char* who, const char* name, const
 
 // ---------------------------------------------------------------- products
 
-// How a product is cut: the kind of tile, and over how many parts of k.
-struct Cut {
-    int tile, splits, per;
-};
+using arena::mm::Cut;
 
 // What a kind of tile costs in microseconds (measured on one MI355X): a step
 // of 64 of k with every slot of the compute units taken and with at most one
@@ -105,57 +102,72 @@ struct TileCost {
 constexpr TileCost kTileCost[arena::mm::kTileKinds] = {
     {1.60, 1.30, 5.0, 1}, {0.90, 0.67, 2.6, 2}, {0.60, 0.55, 3.2, 1}, {0.41, 0.35, 1.0, 2}};
 constexpr double kEpilogueRate = 40e3;
+constexpr double kLaunch = 3.0;             // a launch
+constexpr double kSeam = 8.0;               // and the compute units that idle before it for others' last tiles
+constexpr double kJoin = 4.0, kJoinRate = 2.0;     // joining parts: the launch, and megabytes a microsecond
+constexpr int64_t kUnits = 256;             // compute units
 
-// A product of `tiles` tiles, `steps` of k over `splits` parts; bytes: what the
-// epilogue moves for a value of C; part_mb: megabytes of one part.  A split's
-// parts are written and read once more by a second launch.
-double cut_time(int64_t tiles, int64_t steps, int tile, int64_t splits, double bytes, double part_mb)
+// `tiles` tiles of a kind in one launch, k in `splits` parts.  bytes: what the
+// epilogue moves for a value of the tile.  Whole rounds over the compute units,
+// then one that is not full.
+double launch_time(int64_t tiles, int64_t steps, int kind, int64_t splits, double bytes)
 {
-    const TileCost& k = kTileCost[tile];
-    const int64_t per = ceil_div(steps, splits), blocks = tiles * splits;
-    const bool full = blocks > 256;
-    const double values = (double)arena::mm::kTileSide[tile] * arena::mm::kTileSide[tile];
-    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate * (full ? k.slots : 1);
-    return ceil_div(blocks, 256 * k.slots) * (per * (full ? k.full : k.alone) + k.start + end) +
-           (splits > 1 ? 4.0 + splits * part_mb * 0.5 : 0.0);
+    const TileCost& k = kTileCost[kind];
+    const int64_t per = ceil_div(steps, splits), blocks = tiles * splits, round = kUnits * k.slots;
+    const double values = (double)arena::mm::kTileSide[kind] * arena::mm::kTileSide[kind];
+    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate;
+    const int64_t rounds = blocks / round, rest = blocks % round;
+    double t = kLaunch + rounds * (per * k.full + k.start + end * k.slots);
+    if (rest > kUnits) t += per * k.full + k.start + end * k.slots;
+    else if (rest > 0) t += per * k.alone + k.start + end;
+    return t + (splits > 1 ? kJoin + blocks * values * 4e-6 / kJoinRate : 0.0);
 }
 
+// The cheapest cut of a product: every kind of tile for whole rounds over the
+// compute units or for none, and every smaller kind and split of k for the
+// rest.  A last round that is nearly empty costs as much as a full one: 136
+// tiles of 256 on 256 compute units (the Gram matrix of 4096 rows) would leave
+// half of them idle for the whole product.
 // dual: gate and up share a tile, which then covers half as many columns.
-// bytes: what the epilogue moves for a column of the tile.
-Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, double bytes = 2.0)
+// sym: only the tiles on and below the diagonal.
+Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bool sym, double bytes)
 {
-    const int half = dual ? 2 : 1;
-    const double mb = 4e-6 * M * N * batch * half;
-    Cut best = {arena::mm::k256, 1, (int)steps};
+    using namespace arena::mm;
+    Cut best = {k256, k256, 0, 1, (int)steps};
     double least = INFINITY;
-    for (int tile = 0; tile < arena::mm::kTileKinds; ++tile) {
-        const int side = arena::mm::kTileSide[tile];
-        const int64_t tiles = ceil_div(M, side) * ceil_div(N, side / half) * batch;
-        for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
-            const double t = cut_time(tiles, steps, tile, s, bytes, mb);
-            if (t < least) {
-                least = t;
-                best = {tile, s, (int)ceil_div(steps, s)};
+    for (int main = 0; main < kTileKinds; ++main) {
+        const int64_t side = kTileSide[main], tm = ceil_div(M, side), tn = ceil_div(N, dual ? side / 2 : side);
+        const int64_t all = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch, round = kUnits * kTileCost[main].slots;
+        for (int64_t first : {all / round * round, (int64_t)0}) {
+            const double begin = first ? launch_time(first, steps, main, 1, bytes) + (first < all ? kSeam : 0.0) : 0.0;
+            if (first == all && begin < least) {
+                least = begin;
+                best = {main, main, first, 1, (int)steps};
+            }
+            if (first == all) continue;
+            for (int tail = 0; tail < kTileKinds; ++tail) {
+                if (kTileSide[tail] > side) continue;
+                const int64_t ratio = side / kTileSide[tail], tiles = (all - first) * ratio * ratio;
+                for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
+                    const double t = begin + launch_time(tiles, steps, tail, s, bytes);
+                    if (t < least) {
+                        least = t;
+                        best = {main, tail, first, s, (int)ceil_div(steps, s)};
+                    }
+                }
             }
         }
     }
-    best.splits = best.per > 0 ? (int)std::max<int64_t>(1, ceil_div(steps, best.per)) : 1;
+    if (best.per > 0) best.splits = (int)std::max<int64_t>(1, ceil_div(steps, best.per));
     return best;
 }
 
-int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, bool dual)
+int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, bool dual, bool sym)
 {
-    return cut.splits > 1 ? 4 * (int64_t)cut.splits * M * N * batch * (dual ? 2 : 1) : 0;
-}
-
-void set_cut(GemmArgs* A, const Cut& cut, bool dual, void* part)
-{
-    const int side = arena::mm::kTileSide[cut.tile];
-    A->tiles_m = (int)ceil_div(A->M, side);
-    A->tiles_n = (int)ceil_div(A->N, dual ? side / 2 : side);
-    A->splits = cut.splits;
-    A->per = cut.per;
-    A->part = (float*)part;
+    if (cut.splits == 1) return 0;
+    const int64_t side = arena::mm::kTileSide[cut.main], tm = ceil_div(M, side), tn = ceil_div(N, dual ? side / 2 : side);
+    const int64_t all = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
+    return 4 * cut.splits * (all - cut.first) * side * side;
 }
 
 GemmArgs new_args(int64_t M, int64_t N, int64_t K)
@@ -343,10 +355,10 @@ struct ForwardPlan : FfnPlan {
     void* part;
     ForwardPlan(const arena_ffn_desc* d, void* base) : FfnPlan(d, d->tokens <= arena::mm::kSkinnyRows, base)
     {
-        cut_up = choose_cut(d->tokens, d->inner, ceil_div(d->model, arena::mm::kBK), 1, true, d->g ? 4.0 : 1.0);
-        cut_down = choose_cut(d->tokens, d->model, ceil_div(d->inner, arena::mm::kBK), 1, false);
-        part = w.take(skinny ? 0 : std::max(part_bytes(cut_up, d->tokens, d->inner, 1, true),
-                                            part_bytes(cut_down, d->tokens, d->model, 1, false)));
+        cut_up = choose_cut(d->tokens, d->inner, ceil_div(d->model, arena::mm::kBK), 1, true, false, d->g ? 4.0 : 1.0);
+        cut_down = choose_cut(d->tokens, d->model, ceil_div(d->inner, arena::mm::kBK), 1, false, false, 2.0);
+        part = w.take(skinny ? 0 : std::max(part_bytes(cut_up, d->tokens, d->inner, 1, true, false),
+                                            part_bytes(cut_down, d->tokens, d->model, 1, false, false)));
     }
 };
 
@@ -365,13 +377,15 @@ struct BackwardPlan : FfnPlan {
         dg = w.take(2 * T * ld);
         du = w.take(2 * T * ld);
         pair = g->dw_gate && g->dw_up && g->ld_dw_gate == g->ld_dw_up;
-        cut_dh = choose_cut(T, F, ceil_div(D, bk), 1, false, 10.0);
-        cut_dx = choose_cut(T, D, 2 * ceil_div(F, bk), 1, false);
-        cut_down = choose_cut(D, F, ceil_div(T, bk), 1, false);
-        cut_up = choose_cut(F, D, ceil_div(T, bk), pair ? 2 : 1, false);
-        part = w.take(std::max(std::max(part_bytes(cut_dh, T, F, 1, false), part_bytes(cut_dx, T, D, 1, false)),
-                               std::max(part_bytes(cut_down, D, F, 1, false),
-                                        part_bytes(cut_up, F, D, pair ? 2 : 1, false))));
+        const int pairs = pair ? 2 : 1;
+        const double bytes = bytes_of(g->grad_dtype) * (g->accumulate ? 2.0 : 1.0);
+        cut_dh = choose_cut(T, F, ceil_div(D, bk), 1, false, false, 10.0);
+        cut_dx = choose_cut(T, D, 2 * ceil_div(F, bk), 1, false, false, 2.0);
+        cut_down = choose_cut(D, F, ceil_div(T, bk), 1, false, false, bytes);
+        cut_up = choose_cut(F, D, ceil_div(T, bk), pairs, false, false, bytes);
+        part = w.take(std::max(std::max(part_bytes(cut_dh, T, F, 1, false, false), part_bytes(cut_dx, T, D, 1, false, false)),
+                               std::max(part_bytes(cut_down, D, F, 1, false, false),
+                                        part_bytes(cut_up, F, D, pairs, false, false))));
     }
 };
 
@@ -483,7 +497,6 @@ struct UpdatePlan {
     int blocks;
     void *x[2], *gram, *poly, *sums, *part;
     Cut cut_gram, cut_square, cut_x;
-    bool sym_gram, sym_square;
 
     UpdatePlan(const arena_update_desc* d, void* base) : w(base)
     {
@@ -498,32 +511,12 @@ struct UpdatePlan {
         gram = w.take(2 * n * side * side);
         poly = w.take(2 * n * side * side);
         sums = w.take(8 * n * blocks);
-        cut_gram = symmetric_cut(side, ceil_div(tall ? rows : cols, bk), n, &sym_gram);
-        cut_square = symmetric_cut(side, ceil_div(side, bk), n, &sym_square);
-        cut_x = choose_cut(rows, cols, ceil_div(side, bk), n, false);
-        part = w.take(std::max(std::max(part_bytes(cut_gram, side, side, n, false),
-                                        part_bytes(cut_square, side, side, n, false)),
-                               part_bytes(cut_x, rows, cols, n, false)));
-    }
-
-    // A symmetric product: the tiles on and below the diagonal only, or, where
-    // those leave compute units empty, all tiles with k split.
-    static Cut symmetric_cut(int64_t n, int64_t steps, int64_t batch, bool* sym)
-    {
-        Cut best = choose_cut(n, n, steps, batch, false);
-        const int64_t full = ceil_div(n, arena::mm::kTileSide[best.tile]);
-        double least = cut_time(full * full * batch, steps, best.tile, best.splits, 2.0, 4e-6 * n * n * batch);
-        *sym = false;
-        for (int tile = 0; tile < arena::mm::kTileKinds; ++tile) {
-            const int64_t t = ceil_div(n, arena::mm::kTileSide[tile]);
-            const double time = cut_time(t * (t + 1) / 2 * batch, steps, tile, 1, 4.0, 0.0);
-            if (time <= least) {
-                least = time;
-                best = {tile, 1, (int)steps};
-                *sym = true;
-            }
-        }
-        return best;
+        cut_gram = choose_cut(side, side, ceil_div(tall ? rows : cols, bk), n, false, true, 4.0);
+        cut_square = choose_cut(side, side, ceil_div(side, bk), n, false, true, 6.0);
+        cut_x = choose_cut(rows, cols, ceil_div(side, bk), n, false, false, 4.0);
+        part = w.take(std::max(std::max(part_bytes(cut_gram, side, side, n, false, true),
+                                        part_bytes(cut_square, side, side, n, false, true)),
+                               part_bytes(cut_x, rows, cols, n, false, false)));
     }
 };
 
@@ -632,18 +625,18 @@ arena_status arena_ffn_forward(arena_ctx* c, const arena_ffn_desc* d, void* stre
     A.g = d->g; A.u = d->u; A.ldg = d->ld_inner;
     A.act = d->activation;
     A.pad = (int)pad8(d->inner);
-    set_cut(&A, P.cut_up, true, P.part);
+    A.part = (float*)P.part;
     e = P.skinny ? arena::mm::launch_skinny(A, d->dtype, true, s)
-                 : arena::mm::launch_gemm(A, d->dtype, arena::mm::kGateUp, P.cut_up.tile, s);
+                 : arena::mm::launch_gemm(A, d->dtype, arena::mm::kGateUp, P.cut_up, s);
     if (e) return hip_error(c, e, "ffn gate and up launch");
 
     GemmArgs B = new_args(d->tokens, d->model, d->inner);
     B.a[0] = d->h; B.lda = d->ld_inner;
     B.b[0] = P.down.p; B.ldb = P.down.ld;
     B.c[0] = d->y; B.ldc = d->ld_y;
-    set_cut(&B, P.cut_down, false, P.part);
+    B.part = (float*)P.part;
     e = P.skinny ? arena::mm::launch_skinny(B, d->dtype, false, s)
-                 : arena::mm::launch_gemm(B, d->dtype, arena::mm::kRowsRows, P.cut_down.tile, s);
+                 : arena::mm::launch_gemm(B, d->dtype, arena::mm::kRowsRows, P.cut_down, s);
     return e == hipSuccess ? ARENA_OK : hip_error(c, e, "ffn down launch");
 }
 
@@ -684,8 +677,8 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
         A.c[0] = P.dg; A.c[1] = P.du; A.ldc = P.ld;
         A.act = f->activation;
         A.pad = (int)P.ld;
-        set_cut(&A, P.cut_dh, false, P.part);
-        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kGateUpBack, P.cut_dh.tile, s)))
+        A.part = (float*)P.part;
+        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kGateUpBack, P.cut_dh, s)))
             return hip_error(c, e, "ffn inner gradient launch");
     }
     if (T > 0 && g->dx) {
@@ -694,8 +687,8 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
         A.a[0] = P.dg; A.a[1] = P.du; A.lda = P.ld;
         A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld;
         A.c[0] = g->dx; A.ldc = g->ld_dx;
-        set_cut(&A, P.cut_dx, false, P.part);
-        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kRowsCols, P.cut_dx.tile, s)))
+        A.part = (float*)P.part;
+        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kRowsCols, P.cut_dx, s)))
             return hip_error(c, e, "ffn input gradient launch");
     }
     // weight gradients: C[m, n] = sum over tokens of a(t, m) b(t, n), beside what accumulate keeps
@@ -712,8 +705,8 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
             A.beta = 1.0f;
             A.e[0] = c0; A.e[1] = c1; A.lde = ldc;
         }
-        set_cut(&A, cut, false, P.part);
-        return arena::mm::launch_gemm(A, f->dtype, arena::mm::kColsCols, cut.tile, s);
+        A.part = (float*)P.part;
+        return arena::mm::launch_gemm(A, f->dtype, arena::mm::kColsCols, cut, s);
     };
     if (g->dw_down && (e = weight(P.dy.p, nullptr, P.dy.ld, f->h, f->ld_inner, D, F, g->dw_down, nullptr,
                                   g->ld_dw_down, P.cut_down)))
@@ -777,8 +770,8 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
     auto run = [&](GemmArgs& A, const Cut& cut, bool sym, arena::mm::Product what) {
         A.batch = d->batch;
         A.sym = sym;
-        set_cut(&A, cut, false, P.part);
-        return arena::mm::launch_gemm(A, ARENA_F16, what, cut.tile, s);
+        A.part = (float*)P.part;
+        return arena::mm::launch_gemm(A, ARENA_F16, what, cut, s);
     };
     int at = 0;
     for (int i = 0; i < std::max(1, (int)d->steps); ++i) {
@@ -792,7 +785,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
             A.c[0] = P.gram; A.ldc = P.side; A.sc = sg;
             A.alpha = inv;
             A.diag = (float)(kCentre * kHalfScale);
-            if ((e = run(A, P.cut_gram, P.sym_gram, P.tall ? arena::mm::kColsCols : arena::mm::kRowsRows)))
+            if ((e = run(A, P.cut_gram, true, P.tall ? arena::mm::kColsCols : arena::mm::kRowsRows)))
                 return hip_error(c, e, "update Gram launch");
             // 2^12 ((b + c) C + c C^2); C is symmetric, so its rows serve as columns
             GemmArgs B = new_args(P.side, P.side, P.side);
@@ -801,7 +794,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
             B.e[0] = P.gram; B.lde = P.side; B.se = sg;
             B.alpha = k[2] * inv;
             B.beta = (float)(k[1] + 2.0 * kCentre * k[2]);
-            if ((e = run(B, P.cut_square, P.sym_square, arena::mm::kRowsRows)))
+            if ((e = run(B, P.cut_square, true, arena::mm::kRowsRows)))
                 return hip_error(c, e, "update square launch");
         }
         // 2^12 ((a + b/2 + c/4) X + B X), or X B where X is tall; the last step writes scale times it

@@ -34,7 +34,11 @@ struct GemmArgs {
     int64_t sa, sb, sc;       // batch strides, elements
     int32_t M, N, K;
     int32_t nseg, pairs, batch;
+    // tiles of the product (sym: only those on and below the diagonal) and which
+    // of them, over all batch indices, this launch takes: from `first` on, each
+    // as 2^ratio x 2^ratio tiles of the kernel's size
     int32_t tiles_m, tiles_n, sym;
+    int32_t first, ratio;
     // plain: C = alpha * product + beta * e - diag on the diagonal
     const void* e[2];
     int64_t lde, se;
@@ -47,7 +51,8 @@ struct GemmArgs {
     void *g, *u;
     int64_t ldg;
     int32_t act, pad;
-    // split k: block z of `splits` takes `per` steps and leaves its sums in part
+    // split k: block y of `splits` takes `per` steps and leaves its sums in part,
+    // a place of tile size for each block
     int32_t splits, per;
     float* part;
 };
@@ -62,11 +67,21 @@ enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack };
 enum TileKind { k256 = 0, k128, k128Deep, k64, kTileKinds };
 constexpr int kTileSide[kTileKinds] = {256, 128, 128, 64};
 
-// tile: a TileKind.  The host has checked that operands are 16-byte aligned
+// How a product is cut: tiles of kind `main`, the first `first` of them by
+// themselves, in whole rounds over the compute units; the rest as tiles of kind
+// `tail`, whose side divides main's, with k in `splits` parts of `per` steps.
+struct Cut {
+    int main, tail;
+    int64_t first;
+    int splits, per;
+};
+
+// part: `splits` times the tail's tiles, each of its side squared, if k is
+// split.  The host has checked that operands are 16-byte aligned
 // with strides and batch strides of multiples of 8, and that values between
 // the matrix's edge and the next multiple of 8 along the contiguous axis are
 // readable (and zero where that axis is k).
-hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, int tile, hipStream_t s);
+hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s);
 
 constexpr int kSkinnyRows = 64;         // rows of A (tokens) that the kernel without LDS tiles takes
 
