@@ -130,7 +130,8 @@ double launch_time(int64_t tiles, int64_t steps, int kind, int64_t splits, doubl
 // half of them idle for the whole product.
 // dual: gate and up share a tile, which then covers half as many columns.
 // sym: only the tiles on and below the diagonal.
-Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bool sym, double bytes)
+Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bool sym, double bytes,
+               double* time = nullptr)
 {
     using namespace arena::mm;
     Cut best = {k256, k256, 0, 1, (int)steps};
@@ -146,7 +147,7 @@ Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bo
             }
             if (first == all) continue;
             for (int tail = 0; tail < kTileKinds; ++tail) {
-                if (kTileSide[tail] > side) continue;
+                if (kTileSide[tail] > side || (first == 0 && tail != main)) continue;
                 const int64_t ratio = side / kTileSide[tail], tiles = (all - first) * ratio * ratio;
                 for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
                     const double t = begin + launch_time(tiles, steps, tail, s, bytes);
@@ -159,7 +160,20 @@ Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bo
         }
     }
     if (best.per > 0) best.splits = (int)std::max<int64_t>(1, ceil_div(steps, best.per));
+    if (time) *time = least;
     return best;
+}
+
+// A symmetric product: the tiles on and below the diagonal, each written twice,
+// unless all tiles once are no slower (as where they fit the compute units at
+// once).  bytes: what an epilogue reads and writes for a value written once.
+Cut choose_symmetric(int64_t n, int64_t steps, int64_t batch, double bytes, bool* sym)
+{
+    double all, half;
+    const Cut a = choose_cut(n, n, steps, batch, false, false, bytes, &all);
+    const Cut h = choose_cut(n, n, steps, batch, false, true, bytes + 2.0, &half);
+    *sym = half < all;
+    return *sym ? h : a;
 }
 
 int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, bool dual, bool sym)
@@ -497,6 +511,7 @@ struct UpdatePlan {
     int blocks;
     void *x[2], *gram, *poly, *sums, *part;
     Cut cut_gram, cut_square, cut_x;
+    bool sym_gram, sym_square;
 
     UpdatePlan(const arena_update_desc* d, void* base) : w(base)
     {
@@ -511,11 +526,11 @@ struct UpdatePlan {
         gram = w.take(2 * n * side * side);
         poly = w.take(2 * n * side * side);
         sums = w.take(8 * n * blocks);
-        cut_gram = choose_cut(side, side, ceil_div(tall ? rows : cols, bk), n, false, true, 4.0);
-        cut_square = choose_cut(side, side, ceil_div(side, bk), n, false, true, 6.0);
+        cut_gram = choose_symmetric(side, ceil_div(tall ? rows : cols, bk), n, 2.0, &sym_gram);
+        cut_square = choose_symmetric(side, ceil_div(side, bk), n, 4.0, &sym_square);
         cut_x = choose_cut(rows, cols, ceil_div(side, bk), n, false, false, 4.0);
-        part = w.take(std::max(std::max(part_bytes(cut_gram, side, side, n, false, true),
-                                        part_bytes(cut_square, side, side, n, false, true)),
+        part = w.take(std::max(std::max(part_bytes(cut_gram, side, side, n, false, sym_gram),
+                                        part_bytes(cut_square, side, side, n, false, sym_square)),
                                part_bytes(cut_x, rows, cols, n, false, false)));
     }
 };
@@ -757,7 +772,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
     U.rows = d->rows; U.cols = d->cols; U.batch = d->batch;
     U.nesterov = d->nesterov != 0;
     U.mu = d->mu; U.eps = d->eps;
-    U.x = (_Float16*)P.x[0];
+    U.x = P.x[0];
     U.rows_p = (int)P.rows; U.ld_x = (int)P.cols;
     U.part = (double*)P.sums;
     U.blocks = P.blocks;
@@ -785,7 +800,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
             A.c[0] = P.gram; A.ldc = P.side; A.sc = sg;
             A.alpha = inv;
             A.diag = (float)(kCentre * kHalfScale);
-            if ((e = run(A, P.cut_gram, true, P.tall ? arena::mm::kColsCols : arena::mm::kRowsRows)))
+            if ((e = run(A, P.cut_gram, P.sym_gram, P.tall ? arena::mm::kColsCols : arena::mm::kRowsRows)))
                 return hip_error(c, e, "update Gram launch");
             // 2^12 ((b + c) C + c C^2); C is symmetric, so its rows serve as columns
             GemmArgs B = new_args(P.side, P.side, P.side);
@@ -794,7 +809,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
             B.e[0] = P.gram; B.lde = P.side; B.se = sg;
             B.alpha = k[2] * inv;
             B.beta = (float)(k[1] + 2.0 * kCentre * k[2]);
-            if ((e = run(B, P.cut_square, true, arena::mm::kRowsRows)))
+            if ((e = run(B, P.cut_square, P.sym_square, arena::mm::kRowsRows)))
                 return hip_error(c, e, "update square launch");
         }
         // 2^12 ((a + b/2 + c/4) X + B X), or X B where X is tall; the last step writes scale times it

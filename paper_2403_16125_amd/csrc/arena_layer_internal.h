@@ -130,7 +130,7 @@ struct UpdateArgs {
     int64_t ld_grad, ld_mom, ld_mom_out, s_grad, s_mom, s_mom_out;
     int32_t rows, cols, batch, nesterov;
     float mu, eps;
-    _Float16* x;                  // [batch][rows_p][ld_x], zero past rows and cols
+    void* x;                      // float16 [batch][rows_p][ld_x], zero past rows and cols
     int32_t rows_p, ld_x;
     double* part;                 // [batch][blocks] sums of squares
     int32_t blocks;

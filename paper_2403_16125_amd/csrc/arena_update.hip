@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void update_scale_kernel(const UpdateArgs A)
         _Float16 h[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) h[q] = q < left ? (_Float16)(float)(g[q] * scale) : (_Float16)0.0f;
-        __builtin_memcpy(A.x + (z * (int64_t)A.rows_p + r) * A.ld_x + c, h, sizeof(h));
+        __builtin_memcpy((_Float16*)A.x + (z * (int64_t)A.rows_p + r) * A.ld_x + c, h, sizeof(h));
     }
 }
 
