@@ -292,14 +292,15 @@ NormArgs norm_args(const arena_norm_desc* d)
     return A;
 }
 
-arena_status norm_workspace(arena_ctx* c, const char* who, const arena_norm_desc* d, int64_t* bytes, int* workers,
-                            int* rows_each)
+arena_status norm_workspace(arena_ctx* c, const char* who, const arena_norm_desc* d, int64_t* bytes, int64_t* sums,
+                            int* workers, int* rows_each)
 {
     arena_status s = check_norm(c, who, d, true);
     if (s) return s;
     const NormArgs A = norm_args(d);
     arena::norm_plan(A.tokens, A.gate_rows, A.width, workers, rows_each);
-    *bytes = pad256((int64_t)*workers * arena::kNormSums * A.width * 4);
+    *sums = pad256((int64_t)*workers * arena::kNormSums * A.width * 4);
+    *bytes = *sums + (A.width > arena::kNormSumsWidth ? pad256(A.tokens * 8) : 0);
     return ARENA_OK;
 }
 
@@ -556,8 +557,9 @@ arena_status arena_norm_backward_workspace(arena_ctx* c, const arena_norm_desc* 
     if (!c) return ARENA_ERR_INVALID_ARG;
     ctx_clear(c);
     if (!bytes) return ctx_fail(c, ARENA_ERR_INVALID_ARG, "norm backward: bytes is NULL");
+    int64_t sums;
     int workers, rows;
-    return norm_workspace(c, "norm backward", f, bytes, &workers, &rows);
+    return norm_workspace(c, "norm backward", f, bytes, &sums, &workers, &rows);
 }
 
 arena_status arena_norm_backward(arena_ctx* c, const arena_norm_desc* f, const arena_norm_grads* g, void* stream)
@@ -565,9 +567,9 @@ arena_status arena_norm_backward(arena_ctx* c, const arena_norm_desc* f, const a
     if (!c) return ARENA_ERR_INVALID_ARG;
     ctx_clear(c);
     const char* who = "norm backward";
-    int64_t need;
+    int64_t need, sums_bytes;
     int workers, rows;
-    arena_status s = norm_workspace(c, who, f, &need, &workers, &rows);
+    arena_status s = norm_workspace(c, who, f, &need, &sums_bytes, &workers, &rows);
     if (s) return s;
     if (!g) return ctx_fail(c, ARENA_ERR_INVALID_ARG, "%s: gradient descriptor is NULL", who);
     const size_t size = bytes_of(f->dtype), wide = bytes_of(f->stream_dtype);
@@ -600,6 +602,7 @@ arena_status arena_norm_backward(arena_ctx* c, const arena_norm_desc* f, const a
     A.dw_post = g->dw_post; A.db_post = g->db_post;
     A.dw_pre = g->dw_pre; A.db_pre = g->db_pre;
     A.part = (float*)g->workspace;
+    A.means = (float*)((char*)g->workspace + sums_bytes);
     A.workers = workers;
     A.rows_each = rows;
     DeviceScope scope(arena::ctx_device(c));

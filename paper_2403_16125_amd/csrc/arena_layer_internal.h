@@ -110,6 +110,7 @@ struct NormArgs {
     void *dx, *dy;
     void *dgate, *dw_post, *db_post, *dw_pre, *db_pre;
     float* part;                  // workers' column sums, see norm_plan
+    float* means;                 // [tokens][2], rows wider than kNormSumsWidth
     int32_t workers, rows_each;   // workers of the backward, tokens of each
 };
 
@@ -117,6 +118,7 @@ struct NormArgs {
 // first and last gate row's dgate.
 constexpr int kNormSums = 6;
 constexpr int kNormMaxWidth = 16384;
+constexpr int kNormSumsWidth = 8192;       // wider rows' column sums take a pass of their own
 
 void norm_plan(int64_t tokens, int64_t gate_rows, int width, int* workers, int* rows_each);
 hipError_t launch_norm_forward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s);

@@ -23,37 +23,62 @@
 namespace arena {
 namespace {
 
-// Eight neighbouring values of a row.
+template <typename E>
+__device__ __forceinline__ float half_value(uint16_t h)
+{
+    E e;
+    __builtin_memcpy(&e, &h, 2);
+    return (float)e;
+}
+template <>
+__device__ __forceinline__ float half_value<float>(uint16_t)
+{
+    return 0.0f;      // floats are taken whole
+}
+
+// Eight neighbouring values of a row as they lie in memory.
 template <typename E>
 struct Eight {
-    E v[8];
+    static constexpr int kWords = sizeof(E) * 2;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if (sizeof(E) == 4) return __uint_as_float(w[i]);
+        const uint16_t h = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        return half_value<E>(h);
+    }
 };
 
-// `left` values lie inside the row; the others read as zero.  Rows may start
-// on any value: the 16-byte accesses are unaligned where they do not.
+// Eight values from column c of the row that starts at `row` values from base (the
+// same in all lanes, so it stays in scalar registers).  `left` of them lie
+// inside the row; the others read as zero.  Rows may start on any value: the
+// 16-byte accesses are unaligned where they do not.
 template <typename E>
-__device__ __forceinline__ Eight<E> get8(const void* base, int64_t at, int left)
+__device__ __forceinline__ Eight<E> get8(const void* base, int64_t row, int c, int left)
 {
-    const E* p = (const E*)base + at;
+    const char* p = (const char*)base + row * (int64_t)sizeof(E) + (uint32_t)(c * (int)sizeof(E));
     Eight<E> w;
     if (left >= 8) {
-        __builtin_memcpy(&w, p, sizeof(w));
+        __builtin_memcpy(w.w, p, sizeof(w.w));
     } else {
+        const uint16_t* h = (const uint16_t*)p;
+        const int n = left * (int)(sizeof(E) / 2);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w.v[i] = i < left ? p[i] : (E)0.0f;
+        for (int i = 0; i < Eight<E>::kWords; ++i)
+            w.w[i] = (2 * i < n ? h[2 * i] : 0) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0);
     }
     return w;
 }
 
 template <typename E>
-__device__ __forceinline__ void put8(void* base, int64_t at, int left, const float* v)
+__device__ __forceinline__ void put8(void* base, int64_t row, int c, int left, const float* v)
 {
-    E* p = (E*)base + at;
+    E* p = (E*)((char*)base + row * (int64_t)sizeof(E) + (uint32_t)(c * (int)sizeof(E)));
     if (left >= 8) {
-        Eight<E> w;
+        E w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w.v[i] = (E)v[i];
-        __builtin_memcpy(p, &w, sizeof(w));
+        for (int i = 0; i < 8; ++i) w[i] = (E)v[i];
+        __builtin_memcpy(p, w, sizeof(w));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -78,9 +103,9 @@ __device__ __forceinline__ void worker_sum(float (&v)[N], float (*lds)[WV][N], i
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        v[i] = lds[slot][0][i];
+        v[i] = lds[slot][threadIdx.x & (WV - 1)][i];
 #pragma unroll
-        for (int w = 1; w < WV; ++w) v[i] += lds[slot][w][i];
+        for (int d = WV / 2; d >= 1; d >>= 1) v[i] += __shfl_xor(v[i], d, 64);
     }
     slot ^= 1;
 }
@@ -95,7 +120,7 @@ struct Row {
     }
     static __device__ __forceinline__ int64_t worker()
     {
-        return (int64_t)blockIdx.x * kWorkers + (WV == 1 ? threadIdx.x >> 6 : 0);
+        return (int64_t)blockIdx.x * kWorkers + (WV == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
     }
 };
 
@@ -142,17 +167,17 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_forward_kernel(c
     float mu2 = 0.0f, rs2 = 0.0f, mu1 = 0.0f, rs1 = 0.0f;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-        const Eight<TX> x = get8<TX>(A.x, t * A.ld_x + R::col(it), A.width - R::col(it));
+        const Eight<TX> x = get8<TX>(A.x, t * A.ld_x, R::col(it), A.width - R::col(it));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[it][i] = (float)x.v[i];
+        for (int i = 0; i < 8; ++i) r[it][i] = x[i];
     }
     if (A.y) {
         float y[IT][8];
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-            const Eight<TY> w = get8<TY>(A.y, t * A.ld_y + R::col(it), A.width - R::col(it));
+            const Eight<TY> w = get8<TY>(A.y, t * A.ld_y, R::col(it), A.width - R::col(it));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[it][i] = (float)w.v[i];
+            for (int i = 0; i < 8; ++i) y[it][i] = w[i];
         }
         moments<WV, IT>(y, A.width, A.layer, A.eps, lds, slot, &mu2, &rs2);
         const int64_t row = t / A.gate_rows;
@@ -160,18 +185,18 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_forward_kernel(c
         for (int it = 0; it < IT; ++it) {
             const int c = R::col(it), left = A.width - c;
             Eight<TY> w, b, g;
-            if (A.w_post) w = get8<TY>(A.w_post, c, left);
-            if (A.b_post) b = get8<TY>(A.b_post, c, left);
-            if (A.gate) g = get8<TY>(A.gate, row * A.ld_gate + c, left);
+            if (A.w_post) w = get8<TY>(A.w_post, 0, c, left);
+            if (A.b_post) b = get8<TY>(A.b_post, 0, c, left);
+            if (A.gate) g = get8<TY>(A.gate, row * A.ld_gate, c, left);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float v = (y[it][i] - mu2) * rs2;
-                if (A.w_post) v *= (float)w.v[i];
-                if (A.b_post) v += (float)b.v[i];
-                r[it][i] += A.scale * (A.gate ? (float)g.v[i] : 1.0f) * v;
+                if (A.w_post) v *= w[i];
+                if (A.b_post) v += b[i];
+                r[it][i] += A.scale * (A.gate ? g[i] : 1.0f) * v;
                 if (i >= left) r[it][i] = 0.0f;
             }
-            put8<TX>(A.r, t * A.ld_r + c, left, r[it]);
+            put8<TX>(A.r, t * A.ld_r, c, left, r[it]);
         }
     }
     if (A.n) {
@@ -180,16 +205,16 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_forward_kernel(c
         for (int it = 0; it < IT; ++it) {
             const int c = R::col(it), left = A.width - c;
             Eight<TY> w, b;
-            if (A.w_pre) w = get8<TY>(A.w_pre, c, left);
-            if (A.b_pre) b = get8<TY>(A.b_pre, c, left);
+            if (A.w_pre) w = get8<TY>(A.w_pre, 0, c, left);
+            if (A.b_pre) b = get8<TY>(A.b_pre, 0, c, left);
             float n[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 n[i] = (r[it][i] - mu1) * rs1;
-                if (A.w_pre) n[i] *= (float)w.v[i];
-                if (A.b_pre) n[i] += (float)b.v[i];
+                if (A.w_pre) n[i] *= w[i];
+                if (A.b_pre) n[i] += b[i];
             }
-            put8<TY>(A.n, t * A.ld_n + c, left, n);
+            put8<TY>(A.n, t * A.ld_n, c, left, n);
         }
     }
     if (A.stats && (WV == 1 ? (threadIdx.x & 63) == 0 : threadIdx.x == 0)) {
@@ -201,126 +226,182 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_forward_kernel(c
     }
 }
 
-// A worker goes down rows_each rows.
+// What the backward pass reads of a row.
+template <typename TY, typename TX, int WV, int IT>
+struct BackRow {
+    Eight<TY> dn[IT], y[IT];
+    Eight<TX> res[IT], dr[IT];
+    float st[4];
+    __device__ __forceinline__ void load(const NormArgs& A, int64_t t)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st[i] = A.stats[t * 4 + i];
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int c = Row<WV, IT>::col(it), left = A.width - c;
+            if (A.dn) {
+                dn[it] = get8<TY>(A.dn, t * A.ld_dn, c, left);
+                res[it] = get8<TX>(A.res, t * A.ld_res, c, left);
+            }
+            if (A.y) y[it] = get8<TY>(A.y, t * A.ld_y, c, left);
+            if (A.dr) dr[it] = get8<TX>(A.dr, t * A.ld_dr, c, left);
+        }
+    }
+};
+
+// A worker goes down rows_each rows.  With 8 values a thread (AHEAD) the next
+// row's are on their way while it works on one, and the weights stay in
+// registers.  With more it reads each value where it uses it, twice from a
+// cache.  With 32 (past 8192 columns) the column sums have no place either (a
+// form that kept them spilled up to 1.3 KB a thread, 4096 x 12288 501 us): then
+// the rows' means are left for norm_sums_kernel, which reads four of the six
+// matrices once more.
 template <typename TY, typename TX, int WV, int IT, bool BIAS>
 __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_backward_kernel(const NormArgs A)
 {
     typedef Row<WV, IT> R;
+    constexpr bool AHEAD = IT == 1, SUMS = IT <= 2;
     __shared__ float lds[2][WV][2];
     const int64_t me = R::worker();
     if (me >= A.workers) return;
     const int64_t t0 = me * A.rows_each, t1 = min(t0 + A.rows_each, A.tokens);
     int slot = 0;
-    float s_w1[IT][8], s_w2[IT][8], s_g[IT][8], s_b1[BIAS ? IT : 1][8], s_b2[BIAS ? IT : 1][8];
+    constexpr int SB = BIAS && SUMS ? IT : 1, SI = SUMS ? IT : 1;
+    float s_w1[SI][8], s_w2[SI][8], s_g[SI][8], s_b1[SB][8], s_b2[SB][8];
+    if (SUMS)
 #pragma unroll
-    for (int it = 0; it < IT; ++it)
+        for (int it = 0; it < SI; ++it)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s_w1[it][i] = s_w2[it][i] = s_g[it][i] = 0.0f;
-            if (BIAS) s_b1[it][i] = s_b2[it][i] = 0.0f;
-        }
-    Eight<TY> w1[IT], w2[IT], gt[IT];
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        const int c = R::col(it), left = A.width - c;
-        if (A.w_pre) w1[it] = get8<TY>(A.w_pre, c, left);
-        if (A.w_post) w2[it] = get8<TY>(A.w_post, c, left);
-    }
+            for (int i = 0; i < 8; ++i) {
+                s_w1[it][i] = s_w2[it][i] = s_g[it][i] = 0.0f;
+                if (BIAS) s_b1[it % SB][i] = s_b2[it % SB][i] = 0.0f;
+            }
     const float inv = 1.0f / A.width;
     const int64_t first = t0 / A.gate_rows;
     int64_t row = -1;
+    Eight<TY> w1[IT], w2[IT], gt[IT];
+    auto read_w1 = [&](int it) { if (A.w_pre) w1[it] = get8<TY>(A.w_pre, 0, R::col(it), A.width - R::col(it)); };
+    auto read_w2 = [&](int it) { if (A.w_post) w2[it] = get8<TY>(A.w_post, 0, R::col(it), A.width - R::col(it)); };
+    auto read_gate = [&](int it) {
+        if (A.gate) gt[it] = get8<TY>(A.gate, row * A.ld_gate, R::col(it), A.width - R::col(it));
+    };
+    if (AHEAD)
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            read_w1(it);
+            read_w2(it);
+        }
     // dgate of the gate row that ends here: to its place if the worker saw all of its tokens
     auto flush = [&]() {
         const bool whole = row * A.gate_rows >= t0 && min((row + 1) * A.gate_rows, A.tokens) <= t1;
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
+        for (int it = 0; it < SI; ++it) {
             const int c = R::col(it), left = A.width - c;
             if (whole) {
-                put8<TY>(A.dgate, row * A.width + c, left, s_g[it]);
+                put8<TY>(A.dgate, row * A.width, c, left, s_g[it]);
             } else {
-                put8<float>(A.part, (me * kNormSums + (row == first ? 4 : 5)) * A.width + c, left, s_g[it]);
+                put8<float>(A.part, (me * kNormSums + (row == first ? 4 : 5)) * A.width, c, left, s_g[it]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) s_g[it][i] = 0.0f;
         }
     };
+    BackRow<TY, TX, WV, IT> now, ahead;
+    if (AHEAD) ahead.load(A, t0);
     for (int64_t t = t0; t < t1; ++t) {
         if (A.gate && t / A.gate_rows != row) {
-            if (row >= 0 && A.dgate) flush();
+            if (SUMS && row >= 0 && A.dgate) flush();
             row = t / A.gate_rows;
+            if (AHEAD)
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
-                gt[it] = get8<TY>(A.gate, row * A.ld_gate + R::col(it), A.width - R::col(it));
+                for (int it = 0; it < IT; ++it) read_gate(it);
         }
-        const float* st = A.stats + t * 4;
-        const float mu2 = st[0], rs2 = st[1], mu1 = st[2], rs1 = st[3];
-        float d[IT][8];            // gradient of r
-        Eight<TX> res[IT];
-        Eight<TY> dn[IT], y[IT];
+        if (AHEAD) {
+            now = ahead;
+            if (t + 1 < t1) ahead.load(A, t + 1);
+        } else {
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
+            for (int i = 0; i < 4; ++i) now.st[i] = A.stats[t * 4 + i];
+        }
+        const float mu2 = now.st[0], rs2 = now.st[1], mu1 = now.st[2], rs1 = now.st[3];
+        auto read_n = [&](int it) {
             const int c = R::col(it), left = A.width - c;
-            if (A.dn) {
-                dn[it] = get8<TY>(A.dn, t * A.ld_dn + c, left);
-                res[it] = get8<TX>(A.res, t * A.ld_res + c, left);
-            }
-            if (A.y) y[it] = get8<TY>(A.y, t * A.ld_y + c, left);
-            Eight<TX> w;
-            if (A.dr) w = get8<TX>(A.dr, t * A.ld_dr + c, left);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[it][i] = A.dr ? (float)w.v[i] : 0.0f;
-        }
+            if (AHEAD) return;
+            now.dn[it] = get8<TY>(A.dn, t * A.ld_dn, c, left);
+            now.res[it] = get8<TX>(A.res, t * A.ld_res, c, left);
+            read_w1(it);
+        };
+        auto read_y = [&](int it) {
+            const int c = R::col(it);
+            if (AHEAD) return;
+            now.y[it] = get8<TY>(A.y, t * A.ld_y, c, A.width - c);
+        };
+        float d[IT][8];            // gradient of r
+        float mz = 0.0f, mq = 0.0f;
         if (A.dn) {
             float m[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 const int left = A.width - R::col(it);
+                read_n(it);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float g = (float)dn[it].v[i], z = ((float)res[it].v[i] - mu1) * rs1;
-                    const float q = A.w_pre ? g * (float)w1[it].v[i] : g;
+                    const float g = now.dn[it][i], z = (now.res[it][i] - mu1) * rs1;
+                    const float q = A.w_pre ? g * w1[it][i] : g;
                     if (i < left) {
                         m[0] += q * z;
                         m[1] += q;
                     }
-                    s_w1[it][i] += g * z;
-                    if (BIAS) s_b1[it][i] += g;
+                    if (SUMS) s_w1[it % SI][i] += g * z;
+                    if (SUMS && BIAS) s_b1[it % SB][i] += g;
                 }
             }
             worker_sum<WV, 2>(m, lds, slot);
-            const float mz = m[0] * inv, mq = A.layer ? m[1] * inv : 0.0f;
+            mz = m[0] * inv;
+            mq = A.layer ? m[1] * inv : 0.0f;
+        }
+        if (!SUMS && threadIdx.x == 0) {
+            A.means[t * 2] = mz;
+            A.means[t * 2 + 1] = mq;
+        }
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
+        for (int it = 0; it < IT; ++it) {
+            const int c = R::col(it), left = A.width - c;
+            if (!AHEAD && A.dr) now.dr[it] = get8<TX>(A.dr, t * A.ld_dr, c, left);
+            if (A.dn) read_n(it);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float g = (float)dn[it].v[i], z = ((float)res[it].v[i] - mu1) * rs1;
-                    const float q = A.w_pre ? g * (float)w1[it].v[i] : g;
+            for (int i = 0; i < 8; ++i) {
+                d[it][i] = A.dr ? now.dr[it][i] : 0.0f;
+                if (A.dn) {
+                    const float g = now.dn[it][i], z = (now.res[it][i] - mu1) * rs1;
+                    const float q = A.w_pre ? g * w1[it][i] : g;
                     d[it][i] += rs1 * (q - z * mz - mq);
                 }
+            }
+            if (A.dx) put8<TX>(A.dx, t * A.ld_dx, c, left, d[it]);
         }
-        if (A.dx)
-#pragma unroll
-            for (int it = 0; it < IT; ++it)
-                put8<TX>(A.dx, t * A.ld_dx + R::col(it), A.width - R::col(it), d[it]);
         if (!A.y) continue;
-        Eight<TY> b2[IT];
-        if (BIAS && A.b_post)
-#pragma unroll
-            for (int it = 0; it < IT; ++it) b2[it] = get8<TY>(A.b_post, R::col(it), A.width - R::col(it));
         float m[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             const int left = A.width - R::col(it);
+            Eight<TY> b2;
+            if (SUMS && BIAS && A.b_post) b2 = get8<TY>(A.b_post, 0, R::col(it), left);
+            read_y(it);
+            if (!AHEAD) {
+                read_w2(it);
+                read_gate(it);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float z = ((float)y[it].v[i] - mu2) * rs2;
-                const float w = A.w_post ? (float)w2[it].v[i] : 1.0f;
-                const float b = BIAS && A.b_post ? (float)b2[it].v[i] : 0.0f;
+                const float z = (now.y[it][i] - mu2) * rs2;
+                const float w = A.w_post ? w2[it][i] : 1.0f;
+                const float b = SUMS && BIAS && A.b_post ? b2[i] : 0.0f;
                 const float sd = A.scale * d[it][i];
-                s_g[it][i] += sd * (z * w + b);
-                const float dv = A.gate ? sd * (float)gt[it].v[i] : sd;
-                s_w2[it][i] += dv * z;
-                if (BIAS) s_b2[it][i] += dv;
+                if (SUMS) s_g[it % SI][i] += sd * (z * w + b);
+                const float dv = A.gate ? sd * gt[it][i] : sd;
+                if (SUMS) s_w2[it % SI][i] += dv * z;
+                if (SUMS && BIAS) s_b2[it % SB][i] += dv;
                 const float q = dv * w;
                 d[it][i] = q;
                 if (i < left) {
@@ -330,39 +411,110 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_backward_kernel(
             }
         }
         worker_sum<WV, 2>(m, lds, slot);
-        const float mz = m[0] * inv, mq = A.layer ? m[1] * inv : 0.0f;
+        mz = m[0] * inv;
+        mq = A.layer ? m[1] * inv : 0.0f;
         if (A.dy)
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
+                read_y(it);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float z = ((float)y[it].v[i] - mu2) * rs2;
+                    const float z = (now.y[it][i] - mu2) * rs2;
                     d[it][i] = rs2 * (d[it][i] - z * mz - mq);
                 }
-                put8<TY>(A.dy, t * A.ld_dy + R::col(it), A.width - R::col(it), d[it]);
+                put8<TY>(A.dy, t * A.ld_dy, R::col(it), A.width - R::col(it), d[it]);
             }
     }
+    if (!SUMS) return;
     if (A.dgate && row >= 0) flush();
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
+    for (int it = 0; it < SI; ++it) {
         const int c = R::col(it), left = A.width - c;
-        const int64_t at = me * kNormSums * A.width + c;
-        if (A.dw_pre) put8<float>(A.part, at, left, s_w1[it]);
-        if (BIAS && A.db_pre) put8<float>(A.part, at + A.width, left, s_b1[it]);
-        if (A.dw_post) put8<float>(A.part, at + 2 * (int64_t)A.width, left, s_w2[it]);
-        if (BIAS && A.db_post) put8<float>(A.part, at + 3 * (int64_t)A.width, left, s_b2[it]);
+        const int64_t at = me * kNormSums * A.width;
+        if (A.dw_pre) put8<float>(A.part, at, c, left, s_w1[it]);
+        if (BIAS && A.db_pre) put8<float>(A.part, at + A.width, c, left, s_b1[it % SB]);
+        if (A.dw_post) put8<float>(A.part, at + 2 * (int64_t)A.width, c, left, s_w2[it]);
+        if (BIAS && A.db_post) put8<float>(A.part, at + 3 * (int64_t)A.width, c, left, s_b2[it % SB]);
     }
 }
 
+// The workers' column sums of wide rows, from the means of dn w_pre rhat (and of
+// dn w_pre) that the rows' pass left: a thread owns 8 columns and goes down a
+// worker's rows.  Where dx was written over dr, the gradient of r is read from it.
+template <typename TY, typename TX, bool BIAS>
+__global__ __launch_bounds__(256) void norm_sums_kernel(const NormArgs A)
+{
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 8, left = A.width - c;
+    if (left <= 0) return;
+    const int64_t me = blockIdx.y, t0 = me * A.rows_each, t1 = min(t0 + A.rows_each, A.tokens);
+    float s_w1[8] = {}, s_w2[8] = {}, s_g[8] = {}, s_b1[8] = {}, s_b2[8] = {};
+    Eight<TY> w1, w2, b2, gt;
+    if (A.w_pre) w1 = get8<TY>(A.w_pre, 0, c, left);
+    if (A.w_post) w2 = get8<TY>(A.w_post, 0, c, left);
+    if (BIAS && A.b_post) b2 = get8<TY>(A.b_post, 0, c, left);
+    const bool over = A.dr && A.dr == A.dx;
+    const int64_t first = t0 / A.gate_rows;
+    int64_t row = -1;
+    auto flush = [&]() {
+        const bool whole = row * A.gate_rows >= t0 && min((row + 1) * A.gate_rows, A.tokens) <= t1;
+        if (whole) put8<TY>(A.dgate, row * A.width, c, left, s_g);
+        else put8<float>(A.part, (me * kNormSums + (row == first ? 4 : 5)) * A.width, c, left, s_g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_g[i] = 0.0f;
+    };
+#pragma unroll 2
+    for (int64_t t = t0; t < t1; ++t) {
+        if (A.gate && t / A.gate_rows != row) {
+            if (row >= 0 && A.dgate) flush();
+            row = t / A.gate_rows;
+            gt = get8<TY>(A.gate, row * A.ld_gate, c, left);
+        }
+        const float *st = A.stats + t * 4, *means = A.means + t * 2;
+        const float mu2 = st[0], rs2 = st[1], mu1 = st[2], rs1 = st[3], mz = means[0], mq = means[1];
+        Eight<TY> dn, y;
+        Eight<TX> res, dr;
+        if (A.dn) {
+            dn = get8<TY>(A.dn, t * A.ld_dn, c, left);
+            res = get8<TX>(A.res, t * A.ld_res, c, left);
+        }
+        if (A.y) y = get8<TY>(A.y, t * A.ld_y, c, left);
+        if (A.dr) dr = get8<TX>(A.dr, t * A.ld_dr, c, left);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float d = A.dr ? dr[i] : 0.0f;
+            if (A.dn) {
+                const float g = dn[i], z = (res[i] - mu1) * rs1, q = A.w_pre ? g * w1[i] : g;
+                if (!over) d += rs1 * (q - z * mz - mq);
+                s_w1[i] += g * z;
+                if (BIAS) s_b1[i] += g;
+            }
+            if (!A.y) continue;
+            const float z = (y[i] - mu2) * rs2, sd = A.scale * d;
+            s_g[i] += sd * (z * (A.w_post ? w2[i] : 1.0f) + (BIAS && A.b_post ? b2[i] : 0.0f));
+            const float dv = A.gate ? sd * gt[i] : sd;
+            s_w2[i] += dv * z;
+            if (BIAS) s_b2[i] += dv;
+        }
+    }
+    if (A.dgate && row >= 0) flush();
+    const int64_t at = me * kNormSums * A.width;
+    if (A.dw_pre) put8<float>(A.part, at, c, left, s_w1);
+    if (BIAS && A.db_pre) put8<float>(A.part, at + A.width, c, left, s_b1);
+    if (A.dw_post) put8<float>(A.part, at + 2 * (int64_t)A.width, c, left, s_w2);
+    if (BIAS && A.db_post) put8<float>(A.part, at + 3 * (int64_t)A.width, c, left, s_b2);
+}
+
 // Joins the workers' column sums: blockIdx.y < 4 the weights and biases, above
-// that the gate rows that several workers share.  64 columns a block, 16 waves
-// over the workers.
-template <typename TY>
+// that the gate rows that several workers share.  A block takes COLS columns,
+// its threads share the workers: 16 columns where rows are narrow, so that
+// enough blocks are at work (16384 x 512: 36 us with 64).
+template <typename TY, int COLS>
 __global__ __launch_bounds__(1024) void norm_join_kernel(const NormArgs A)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
+    constexpr int kShare = 1024 / COLS;
+    __shared__ float lds[kShare][COLS];
+    const int lane = threadIdx.x % COLS, part = threadIdx.x / COLS;
+    const int c = blockIdx.x * COLS + lane;
     TY* out;
     int64_t w0 = 0, w1 = A.workers, row = 0;
     if (blockIdx.y < 4) {
@@ -382,20 +534,21 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormArgs A)
     if (!out) return;
     float s = 0.0f;
     if (c < A.width)
-        for (int64_t w = w0 + wave; w < w1; w += 16) {
+#pragma unroll 8
+        for (int64_t w = w0 + part; w < w1; w += kShare) {
             const int which = blockIdx.y < 4 ? blockIdx.y : (w * A.rows_each / A.gate_rows == row ? 4 : 5);
             s += A.part[(w * kNormSums + which) * A.width + c];
         }
-    lds[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < A.width) {
-        for (int w = 1; w < 16; ++w) s += lds[w][lane];
-        out[c] = (TY)s;
+    lds[part][lane] = s;
+    for (int half = kShare / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (part < half) lds[part][lane] += lds[part + half][lane];
     }
+    if (part == 0 && c < A.width) out[c] = (TY)lds[0][lane];
 }
 
-// Waves and chunks a thread by width.
-int waves_of(int width) { return width <= 512 ? 1 : width <= 4096 ? 4 : width <= 8192 ? 8 : 16; }
+// Waves of a worker by width: 8 values a thread up to 4096, then 16, past 8192 32.
+int waves_of(int width) { return width <= 512 ? 1 : width <= 2048 ? 4 : 8; }
 
 template <typename TY, typename TX>
 hipError_t forward(const NormArgs& A, hipStream_t s)
@@ -403,12 +556,11 @@ hipError_t forward(const NormArgs& A, hipStream_t s)
     const int64_t n = A.tokens;
     switch (waves_of(A.width)) {
     case 1: norm_forward_kernel<TY, TX, 1, 1><<<(unsigned)((n + 3) / 4), 256, 0, s>>>(A); break;
-    case 4:
-        if (A.width <= 2048) norm_forward_kernel<TY, TX, 4, 1><<<(unsigned)n, 256, 0, s>>>(A);
-        else norm_forward_kernel<TY, TX, 4, 2><<<(unsigned)n, 256, 0, s>>>(A);
-        break;
-    case 8: norm_forward_kernel<TY, TX, 8, 2><<<(unsigned)n, 512, 0, s>>>(A); break;
-    default: norm_forward_kernel<TY, TX, 16, 2><<<(unsigned)n, 1024, 0, s>>>(A); break;
+    case 4: norm_forward_kernel<TY, TX, 4, 1><<<(unsigned)n, 256, 0, s>>>(A); break;
+    default:
+        if (A.width <= 4096) norm_forward_kernel<TY, TX, 8, 1><<<(unsigned)n, 512, 0, s>>>(A);
+        else if (A.width <= 8192) norm_forward_kernel<TY, TX, 8, 2><<<(unsigned)n, 512, 0, s>>>(A);
+        else norm_forward_kernel<TY, TX, 8, 4><<<(unsigned)n, 512, 0, s>>>(A);
     }
     return hipGetLastError();
 }
@@ -419,19 +571,23 @@ hipError_t backward(const NormArgs& A, hipStream_t s)
     const unsigned n = (unsigned)A.workers;
     if (n) switch (waves_of(A.width)) {
     case 1: norm_backward_kernel<TY, TX, 1, 1, BIAS><<<(n + 3) / 4, 256, 0, s>>>(A); break;
-    case 4:
-        if (A.width <= 2048) norm_backward_kernel<TY, TX, 4, 1, BIAS><<<n, 256, 0, s>>>(A);
-        else norm_backward_kernel<TY, TX, 4, 2, BIAS><<<n, 256, 0, s>>>(A);
-        break;
-    case 8: norm_backward_kernel<TY, TX, 8, 2, BIAS><<<n, 512, 0, s>>>(A); break;
-    default: norm_backward_kernel<TY, TX, 16, 2, BIAS><<<n, 1024, 0, s>>>(A); break;
+    case 4: norm_backward_kernel<TY, TX, 4, 1, BIAS><<<n, 256, 0, s>>>(A); break;
+    default:
+        if (A.width <= 4096) norm_backward_kernel<TY, TX, 8, 1, BIAS><<<n, 512, 0, s>>>(A);
+        else if (A.width <= kNormSumsWidth) norm_backward_kernel<TY, TX, 8, 2, BIAS><<<n, 512, 0, s>>>(A);
+        else norm_backward_kernel<TY, TX, 8, 4, BIAS><<<n, 512, 0, s>>>(A);
     }
+    if (n && A.width > kNormSumsWidth)
+        norm_sums_kernel<TY, TX, BIAS><<<dim3((A.width + 2047) / 2048, n), 256, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // rows_each is a multiple of gate_rows or less than it: only then gate rows are shared
     const int64_t rows = !A.dgate ? 0 : A.tokens == 0 ? 1
                          : A.gate_rows > A.rows_each ? (A.tokens + A.gate_rows - 1) / A.gate_rows : 0;
-    norm_join_kernel<TY><<<dim3((A.width + 63) / 64, (unsigned)(4 + rows)), 1024, 0, s>>>(A);
+    if (A.width <= 2048)
+        norm_join_kernel<TY, 16><<<dim3((A.width + 15) / 16, (unsigned)(4 + rows)), 1024, 0, s>>>(A);
+    else
+        norm_join_kernel<TY, 64><<<dim3((A.width + 63) / 64, (unsigned)(4 + rows)), 1024, 0, s>>>(A);
     return hipGetLastError();
 }
 
@@ -447,7 +603,7 @@ hipError_t backward_any(const NormArgs& A, hipStream_t s)
 // leave more sums to join.
 void norm_plan(int64_t tokens, int64_t gate_rows, int width, int* workers, int* rows_each)
 {
-    const int64_t most = width <= 512 ? 2048 : 512;
+    const int64_t most = width <= 512 ? 2048 : width <= kNormSumsWidth ? 512 : 256;
     int64_t each = (tokens + most - 1) / most;
     if (each < 1) each = 1;
     if (gate_rows <= each) each = (each + gate_rows - 1) / gate_rows * gate_rows;
