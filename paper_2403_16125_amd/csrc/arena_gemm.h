@@ -808,7 +808,7 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0, 0, 0, 0};
 
-    constexpr int U = NT >= 4 ? 2 : 4;          // steps of 32 in flight
+    constexpr int U = 4;          // steps of 32 in flight
     const int steps = (A.K + 31) / 32, per = (steps + WAVES - 1) / WAVES;
     int k = wave * per * 32;
     const int end = min(A.K, k + per * 32);
@@ -918,20 +918,21 @@ hipError_t launch_gemm_t(const GemmArgs& A, Product what, const Cut& cut, hipStr
     return hipErrorInvalidValue;
 }
 
-template <typename T, bool DUAL>
+template <typename T, bool DUAL, int WAVES>
 hipError_t launch_skinny_n(const GemmArgs& A, hipStream_t s)
 {
     const int blocks = (A.N + 15) / 16;
-    if (A.M <= 16) skinny_kernel<T, 1, DUAL, 8><<<blocks, 512, 0, s>>>(A);
-    else if (A.M <= 32) skinny_kernel<T, 2, DUAL, 8><<<blocks, 512, 0, s>>>(A);
-    else skinny_kernel<T, 4, DUAL, 8><<<blocks, 512, 0, s>>>(A);
+    if (A.M <= 16) skinny_kernel<T, 1, DUAL, WAVES><<<blocks, 64 * WAVES, 0, s>>>(A);
+    else skinny_kernel<T, 2, DUAL, WAVES><<<blocks, 64 * WAVES, 0, s>>>(A);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_skinny_t(const GemmArgs& A, bool dual, hipStream_t s)
 {
-    return dual ? launch_skinny_n<T, true>(A, s) : launch_skinny_n<T, false>(A, s);
+    if (dual) return launch_skinny_n<T, true, 8>(A, s);
+    // few columns: 16 waves a block, so that the compute units have enough to wait for
+    return A.N <= 4096 ? launch_skinny_n<T, false, 16>(A, s) : launch_skinny_n<T, false, 8>(A, s);
 }
 
 }  // namespace mm

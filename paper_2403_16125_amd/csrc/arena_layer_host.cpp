@@ -365,10 +365,19 @@ struct FfnPlan {
     }
 };
 
+// Whether a forward pass takes the kernel for few tokens, which streams the
+// weights past them.  Past 16 tokens it reads as much of the tokens as of the
+// weights, and the tiled products are faster where the weights are large (24
+// tokens, 4096 x 10944: 87 us against 75; 4096 x 1368: 23 us against 27).
+bool few_tokens(const arena_ffn_desc* d)
+{
+    return d->tokens <= 16 || (d->tokens <= arena::mm::kSkinnyRows && (int64_t)d->model * d->inner <= 1 << 23);
+}
+
 struct ForwardPlan : FfnPlan {
     Cut cut_up, cut_down;
     void* part;
-    ForwardPlan(const arena_ffn_desc* d, void* base) : FfnPlan(d, d->tokens <= arena::mm::kSkinnyRows, base)
+    ForwardPlan(const arena_ffn_desc* d, void* base) : FfnPlan(d, few_tokens(d), base)
     {
         cut_up = choose_cut(d->tokens, d->inner, ceil_div(d->model, arena::mm::kBK), 1, true, false, d->g ? 4.0 : 1.0);
         cut_down = choose_cut(d->tokens, d->model, ceil_div(d->inner, arena::mm::kBK), 1, false, false, 2.0);

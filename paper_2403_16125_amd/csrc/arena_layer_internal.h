@@ -83,7 +83,7 @@ struct Cut {
 // readable (and zero where that axis is k).
 hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s);
 
-constexpr int kSkinnyRows = 64;         // rows of A (tokens) that the kernel without LDS tiles takes
+constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel without LDS tiles takes
 
 // C = A B^T with both operands' k contiguous, M <= kSkinnyRows; dual: the gated
 // forward product.
