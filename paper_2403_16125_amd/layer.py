@@ -76,9 +76,10 @@ _bound = None
 def load():
     """The library with the layer operators' signatures; raises if it has not been built."""
     global _bound
-    lib = arena.load()
-    if _bound is lib:
+    lib = arena._lib
+    if lib is not None and _bound is lib:
         return lib
+    lib = arena.load()
     P, out = ctypes.POINTER, ctypes.POINTER(_i64)
     signatures = {
         "arena_norm_forward": [_vp, P(NormDesc), _vp],
@@ -183,6 +184,7 @@ class LayerOps:
         load()
         self.ctx = arena.arena_create(device)
         self._alive = True
+        self._index, self._new, self._current = int(device), torch.empty, torch.cuda.current_stream
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
     def close(self) -> None:
@@ -207,35 +209,38 @@ class LayerOps:
     def _matrix(self, name, t, shape, dtype):
         """Address and row stride of a 2-D tensor; a tensor of more axes is
         taken as its rows where they lie evenly."""
-        if t.device != self.dev:
-            raise ValueError(f"{name} is on {t.device}, not on {self.dev}")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} is on {t.device}, not on {self.dev}")
         if t.dim() != 2:
             try:
-                t = t.view(-1, t.shape[-1])
+                t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(-1, t.shape[-1])
             except RuntimeError:
                 raise ValueError(f"{name}: the rows of shape {tuple(t.shape)}, strides {t.stride()} do not lie evenly")\
                     from None
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-        rows, cols = t.shape
-        if cols > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}: the last axis has stride {t.stride(1)}, not 1")
-        ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+        rows, cols = shape
+        ld, unit = t.stride()
+        if unit != 1 and cols > 1:
+            raise ValueError(f"{name}: the last axis has stride {unit}, not 1")
         if ld < cols:
-            raise ValueError(f"{name}: rows overlap (stride {ld}, width {cols})")
+            if rows > 1:
+                raise ValueError(f"{name}: rows overlap (stride {ld}, width {cols})")
+            ld = cols
         return t.data_ptr(), ld
 
     def _vector(self, name, t, width, dtype):
         if t is None:
             return None
-        if t.device != self.dev or t.dtype != dtype or tuple(t.shape) != (width,) or (width > 1 and t.stride(0) != 1):
+        if t.get_device() != self._index or t.dtype is not dtype or t.shape != (width,) or \
+                (width > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous {dtype} vector of {width} on {self.dev}")
         return t.data_ptr()
 
     def _empty(self, shape, dtype):
-        return self.torch.empty(shape, dtype=dtype, device=self.dev)
+        return self._new(shape, dtype=dtype, device=self.dev)
 
     def _workspace(self, desc, nbytes):
         """Workspace of a call: freed to the stream's pool when the caller drops it."""
@@ -246,19 +251,12 @@ class LayerOps:
         desc.workspace, desc.workspace_bytes = None, 0
         return None
 
-    def _on(self, stream):
-        """(stream handle, context manager that makes it current for allocations)."""
-        torch = self.torch
+    def _run(self, stream, body, *args):
+        """body(stream handle, *args), allocating on that stream."""
         if stream is None:
-            return torch.cuda.current_stream(self.dev).cuda_stream, None
-        return stream.cuda_stream, torch.cuda.stream(stream)
-
-    def _run(self, stream, body):
-        handle, scope = self._on(stream)
-        if scope is None:
-            return body(handle)
-        with scope:
-            return body(handle)
+            return body(self._current(self._index).cuda_stream, *args)
+        with self.torch.cuda.stream(stream):
+            return body(stream.cuda_stream, *args)
 
     # -- norms around a block
 
@@ -294,8 +292,8 @@ class LayerOps:
         row t // gate_rows for token t (gate_rows 0: one row).  dtype: n's type
         where y is None (x's by default).  next_norm=False leaves n out (None).
         Returns (r, n), with save=True (r, n, stats) for norm_backward."""
-        return self._run(stream, lambda h: self._norm_forward(
-            h, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps, dtype, next_norm, save))
+        return self._run(stream, self._norm_forward, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind,
+                         eps, dtype, next_norm, save)
 
     def _norm_forward(self, handle, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps, dtype,
                       next_norm, save):
@@ -324,8 +322,8 @@ class LayerOps:
         the forward's r, y (None: no block before), stats and parameters.
         Returns a dict of dx, dy, dgate, dw_post, db_post, dw_pre and db_pre,
         None where there is no such input."""
-        return self._run(stream, lambda h: self._norm_backward(
-            h, dn, dr, r, y, stats, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps))
+        return self._run(stream, self._norm_backward, dn, dr, r, y, stats, gate, gate_rows, scale, w_post, b_post, w_pre,
+                         b_pre, kind, eps)
 
     def _norm_backward(self, handle, dn, dr, r, y, stats, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind,
                        eps):
@@ -383,7 +381,7 @@ class LayerOps:
         """y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [..., model], w_gate
         and w_up [inner, model], w_down [model, inner], bfloat16 or float16.
         Returns y, with save=True (y, FfnSaved) for ffn_backward."""
-        return self._run(stream, lambda h: self._ffn_forward(h, x, w_gate, w_up, w_down, activation, save, out))
+        return self._run(stream, self._ffn_forward, x, w_gate, w_up, w_down, activation, save, out)
 
     def _ffn_forward(self, handle, x, w_gate, w_up, w_down, activation, save, out):
         d = self._ffn_desc(x, w_gate, w_up, w_down, activation)
@@ -407,8 +405,7 @@ class LayerOps:
         """(dx, dw_gate, dw_up, dw_down) from dy, with the forward's inputs and
         `saved`.  grads: three tensors for the weights' gradients, of x's type
         or float32, which accumulate=True adds to."""
-        return self._run(stream, lambda h: self._ffn_backward(h, dy, x, w_gate, w_up, w_down, saved, activation, grads,
-                                                              accumulate))
+        return self._run(stream, self._ffn_backward, dy, x, w_gate, w_up, w_down, saved, activation, grads, accumulate)
 
     def _ffn_backward(self, handle, dy, x, w_gate, w_up, w_down, saved, activation, grads, accumulate):
         d = self._ffn_desc(x, w_gate, w_up, w_down, activation)
@@ -447,8 +444,8 @@ class LayerOps:
         momentum: float32 of grad's shape, updated in place, or into
         momentum_out.  coefficients: (a, b, c) for every step, or one such triple a
         step.  dtype: of the result (bfloat16 by default, or out's)."""
-        return self._run(stream, lambda h: self._orthogonal_update(
-            h, grad, momentum, momentum_out, mu, nesterov, coefficients, steps, eps, scale, dtype, out))
+        return self._run(stream, self._orthogonal_update, grad, momentum, momentum_out, mu, nesterov, coefficients,
+                         steps, eps, scale, dtype, out)
 
     def _stack(self, name, t, shape, dtype):
         """Address, row stride and matrix stride of a tensor of two or three axes."""
