@@ -6,7 +6,7 @@
  * a layer's forward and backward pass, its parameter, activation and boundary
  * bytes (the profiled operators of Sec. 3.4 of the paper).  The operators here
  * are such a layer's parts as kernels of this library, so the rows of a job can
- * be measured on the machine (paper_2403_16125_amd/layer.py: profile_layer).
+ * be measured on the machine (paper_2403_16125_amd/layer_profile.py).
  *
  *   arena_norm_forward, arena_norm_backward    norms before and after a block,
  *                                              its gate and the residual scale

@@ -1,13 +1,10 @@
 """Python binding of the layer operators (include/arena_layer.h): the training
-step of a gated feed-forward sub-layer on the library's own kernels, and the
-measurement of such layers as rows of an estimator's job tables.
+step of a gated feed-forward sub-layer on the library's own kernels.
 
 The raw functions carry the C ABI's names.  `LayerOps` wraps them for torch
 tensors: it checks shapes and types, makes outputs and workspaces, and enqueues
-on the current stream (or the one given).  `profile_layer` times a sub-layer's
-forward and backward pass and `measured_jobs` turns the times into jobs that
-`workloads.from_lists` and `arena.Estimator` take (the paper's profiler, Sec.
-3.4, measures a job's operators on one GPU).
+on the current stream (or the one given).  layer_profile.py runs them together
+and measures jobs for the estimator.
 
 If the library is not built this module raises: there is no fallback.
 """
@@ -23,7 +20,7 @@ F32, BF16, F16 = 0, 1, 2
 NORM_KINDS = {"rms": 0, "layer": 1}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 NORM_MAX_WIDTH = 16384
-# five steps of the quintic polynomial that Muon uses
+# the quintic polynomial of the Muon optimiser's five steps
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 EXPORTED = (
