@@ -482,27 +482,37 @@ __device__ __forceinline__ void wait_loads()
     __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);
 }
 
+// The LDS buffers of a block: separate arrays, so that a fragment read is known
+// not to meet the loads in flight.
+struct Buffers {
+    char *a0, *a1, *b0, *b1, *a2, *a3, *b2, *b3;
+};
+
+#define ARENA_TILE_BUFFERS(P, name)                                                                        \
+    constexpr int kMoreA = P::kStages > 2 ? P::BM * 128 : 16, kMoreB = P::kStages > 2 ? P::BN * 128 : 16;  \
+    __shared__ __attribute__((aligned(16))) char sa0_[P::BM * 128];                                        \
+    __shared__ __attribute__((aligned(16))) char sa1_[P::BM * 128];                                        \
+    __shared__ __attribute__((aligned(16))) char sb0_[P::BN * 128];                                        \
+    __shared__ __attribute__((aligned(16))) char sb1_[P::BN * 128];                                        \
+    __shared__ __attribute__((aligned(16))) char sa2_[kMoreA];                                             \
+    __shared__ __attribute__((aligned(16))) char sa3_[kMoreA];                                             \
+    __shared__ __attribute__((aligned(16))) char sb2_[kMoreB];                                             \
+    __shared__ __attribute__((aligned(16))) char sb3_[kMoreB];                                             \
+    const Buffers name = {sa0_, sa1_, sb0_, sb1_, sa2_, sa3_, sb2_, sb3_}
+
+// Tile t of a launch's n_tiles; part: which of the splits of k.
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
+__device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, const int n_tiles, const int part,
+                                             const Buffers& lds)
 {
     typedef typename P::T T;
-    // separate arrays, so that a fragment read is known not to meet the loads in flight
-    constexpr int kMoreA = P::kStages > 2 ? P::BM * 128 : 16, kMoreB = P::kStages > 2 ? P::BN * 128 : 16;
-    __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
-    __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
-    __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
-    __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
-    __shared__ __attribute__((aligned(16))) char sa2[kMoreA];
-    __shared__ __attribute__((aligned(16))) char sa3[kMoreA];
-    __shared__ __attribute__((aligned(16))) char sb2[kMoreB];
-    __shared__ __attribute__((aligned(16))) char sb3[kMoreB];
-    auto bufa = [&](int i) { return i == 0 ? sa0 : i == 1 ? sa1 : i == 2 ? sa2 : sa3; };
-    auto bufb = [&](int i) { return i == 0 ? sb0 : i == 1 ? sb1 : i == 2 ? sb2 : sb3; };
+    char *const sa0 = lds.a0, *const sa1 = lds.a1, *const sb0 = lds.b0, *const sb1 = lds.b1;
+    auto bufa = [&](int i) { return i == 0 ? lds.a0 : i == 1 ? lds.a1 : i == 2 ? lds.a2 : lds.a3; };
+    auto bufb = [&](int i) { return i == 0 ? lds.b0 : i == 1 ? lds.b1 : i == 2 ? lds.b2 : lds.b3; };
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
     Place at;
-    const int t = tile_of(blockIdx.x, gridDim.x);
     if (!place_of<P>(A, t, &at)) return;
     const int zb = at.z, m0 = at.m0, n0 = at.n0;
 
@@ -524,7 +534,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
     const int sps = (A.K + kBK - 1) / kBK;     // steps of a segment
     int s = 0, end = sps * A.nseg;
     if (A.splits > 1) {
-        s = blockIdx.y * A.per;
+        s = part * A.per;
         end = min(end, s + A.per);
     }
     const int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
@@ -658,7 +668,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
         }
         if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) return;
         if (A.splits > 1) {
-            float* to = A.part + ((int64_t)blockIdx.y * gridDim.x + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
+            float* to = A.part + ((int64_t)part * n_tiles + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
             put(to, v, 8);
             if (P::DUAL) put(to + P::BM * P::kCols, u, 8);
             return;
@@ -709,6 +719,31 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const 
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+template <typename P>
+__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
+{
+    ARENA_TILE_BUFFERS(P, lds);
+    tile_product<P>(A, tile_of(blockIdx.x, gridDim.x), gridDim.x, blockIdx.y, lds);
+}
+
+// Two independent products in one launch: blocks below n1 * A.splits belong to
+// the first, the rest to the second.  Of medium sizes neither fills the compute
+// units by itself.
+template <typename P, typename Q>
+__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void pair_kernel(const GemmArgs A, int n1, const GemmArgs B,
+                                                                          int n2)
+{
+    static_assert(P::BM == Q::BM && P::kThreads == Q::kThreads && P::kStages == Q::kStages, "one shape of tile");
+    ARENA_TILE_BUFFERS(P, lds);
+    const int first = n1 * A.splits, i = blockIdx.x;
+    if (i < first) {
+        const int part = quotient(i, n1);
+        tile_product<P>(A, tile_of(i - part * n1, n1), n1, part, lds);
+    } else {
+        tile_product<Q>(B, tile_of(i - first, n2), n2, 0, lds);
     }
 }
 
@@ -905,6 +940,28 @@ hipError_t launch_layout(GemmArgs A, const Cut& cut, hipStream_t s)
     return launch_kind<T, ATR, BTR, EPI>(A, cut.tail, (all - cut.first) << 2 * A.ratio, s);
 }
 
+// Both products on 128 x 128 tiles, k of the first in cut.splits parts.
+template <typename T, int EPI>
+hipError_t launch_pair_t(GemmArgs A, GemmArgs B, const Cut& cut, hipStream_t s)
+{
+    typedef Tile<T, 128, 128, 2, 2, 2, false, true, EPI> P;
+    typedef Tile<T, 128, 128, 2, 2, 2, true, true, kPlain> Q;
+    for (GemmArgs* g : {&A, &B}) {
+        g->tiles_m = (g->M + 127) / 128;
+        g->tiles_n = (g->N + 127) / 128;
+        g->first = g->ratio = 0;
+        g->splits = 1;
+    }
+    A.splits = cut.splits;
+    A.per = cut.per;
+    const int n1 = A.tiles_m * A.tiles_n * A.batch, n2 = B.tiles_m * B.tiles_n * B.batch;
+    pair_kernel<P, Q><<<n1 * A.splits + n2, P::kThreads, 0, s>>>(A, n1, B, n2);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || A.splits == 1) return e;
+    join_kernel<P><<<n1 * 4, 256, 0, s>>>(A, n1);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_gemm_t(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
 {
@@ -916,6 +973,12 @@ hipError_t launch_gemm_t(const GemmArgs& A, Product what, const Cut& cut, hipStr
     case kGateUpBack: return launch_layout<T, false, true, kGatedBwd>(A, cut, s);
     }
     return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_pair_of(const GemmArgs& A, Product what, const GemmArgs& B, const Cut& cut, hipStream_t s)
+{
+    return what == kGateUpBack ? launch_pair_t<T, kGatedBwd>(A, B, cut, s) : launch_pair_t<T, kPlain>(A, B, cut, s);
 }
 
 template <typename T, bool DUAL, int WAVES>

@@ -9,6 +9,11 @@ hipError_t launch_gemm_f16(const GemmArgs& A, Product what, const Cut& cut, hipS
     return launch_gemm_t<F16>(A, what, cut, s);
 }
 
+hipError_t launch_pair_f16(const GemmArgs& A, Product what, const GemmArgs& B, const Cut& cut, hipStream_t s)
+{
+    return launch_pair_of<F16>(A, what, B, cut, s);
+}
+
 hipError_t launch_skinny_f16(const GemmArgs& A, bool dual, hipStream_t s) { return launch_skinny_t<F16>(A, dual, s); }
 
 }  // namespace mm

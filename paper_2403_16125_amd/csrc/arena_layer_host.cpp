@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "arena_layer.h"
 #include "arena_layer_internal.h"
@@ -164,6 +165,43 @@ Cut choose_cut(int64_t M, int64_t N, int64_t steps, int64_t batch, bool dual, bo
     return best;
 }
 
+// Whether two independent products are faster in one launch, and over how many
+// parts of the first one's k (the cut's splits; 0: they are not).  The blocks of
+// 128 x 128 share the compute units: their work over all slots and the longest
+// block's end bound the time.  first, second: what each takes by itself.
+struct Half {
+    int64_t M, N, steps, batch;
+    double bytes, alone;
+};
+
+Cut choose_pair(const Half& a, const Half& b)
+{
+    using namespace arena::mm;
+    Cut best = {k128, k128, 0, 0, 0};
+    double least = a.alone + b.alone;
+    const TileCost& k = kTileCost[k128];
+    const int64_t na = ceil_div(a.M, 128) * ceil_div(a.N, 128) * a.batch;
+    const int64_t nb = ceil_div(b.M, 128) * ceil_div(b.N, 128) * b.batch, slots = kUnits * k.slots;
+    const double value = 128.0 * 128.0 / kEpilogueRate * k.slots;
+    if (na + nb > (1 << 20)) return best;
+    for (int s = 1; s <= 16 && (s == 1 || s * 4 <= a.steps); ++s) {
+        const int64_t per = ceil_div(a.steps, s), blocks = na * ceil_div(a.steps, per);
+        const double step = blocks + nb > kUnits ? k.full : k.alone;
+        const double ta = per * step + k.start + value * (s > 1 ? 4.0 : a.bytes);
+        const double tb = b.steps * step + k.start + value * b.bytes;
+        const double work = (blocks * ta + nb * tb) / slots, longest = std::max(ta, tb);
+        // a last round is on average half idle
+        const double t = kLaunch + std::max(longest, work + (blocks + nb > slots ? 0.5 * longest : 0.0)) +
+                         (s > 1 ? kJoin + blocks * 128.0 * 128.0 * 4e-6 / kJoinRate : 0.0);
+        if (t < least) {
+            least = t;
+            best = {k128, k128, 0, s, (int)per};
+        }
+    }
+    if (best.splits > 0) best.splits = (int)ceil_div(a.steps, best.per);
+    return best;
+}
+
 // A symmetric product: the tiles on and below the diagonal, each written twice,
 // unless all tiles once are no slower (as where they fit the compute units at
 // once).  bytes: what an epilogue reads and writes for a value written once.
@@ -178,7 +216,7 @@ Cut choose_symmetric(int64_t n, int64_t steps, int64_t batch, double bytes, bool
 
 int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, bool dual, bool sym)
 {
-    if (cut.splits == 1) return 0;
+    if (cut.splits <= 1) return 0;
     const int64_t side = arena::mm::kTileSide[cut.main], tm = ceil_div(M, side), tn = ceil_div(N, dual ? side / 2 : side);
     const int64_t all = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
     return 4 * cut.splits * (all - cut.first) * side * side;
@@ -221,11 +259,18 @@ struct Operand {
         p = copy;
     }
 
-    hipError_t pack(hipStream_t s) const
-    {
-        return copy ? arena::mm::launch_pack(from, ld_from, copy, ld, rows, cols, s) : hipSuccess;
-    }
 };
+
+// Fills the copies among some operands.
+hipError_t pack(std::initializer_list<const Operand*> operands, hipStream_t s)
+{
+    arena::mm::Pack packs[arena::mm::kMaxPacks];
+    int n = 0;
+    for (const Operand* o : operands)
+        if (o->copy && n < arena::mm::kMaxPacks)
+            packs[n++] = {o->from, o->copy, o->ld_from, o->ld, o->rows, o->cols};
+    return n ? arena::mm::launch_packs(packs, n, s) : hipSuccess;
+}
 
 // ---------------------------------------------------------------- norms
 
@@ -357,12 +402,6 @@ struct FfnPlan {
           down(w, d->w_down, d->ld_down, d->model, d->inner, skinny || Operand::direct(d->w_down, d->ld_down, d->inner))
     {
     }
-    hipError_t pack(hipStream_t s) const
-    {
-        hipError_t e;
-        if ((e = x.pack(s)) || (e = gate.pack(s)) || (e = up.pack(s)) || (e = down.pack(s))) return e;
-        return hipSuccess;
-    }
 };
 
 // Whether a forward pass takes the kernel for few tokens, which streams the
@@ -392,6 +431,7 @@ struct BackwardPlan : FfnPlan {
     void *dg, *du, *part;
     bool pair;                // both weight gradients of the first products in one launch
     Cut cut_dh, cut_dx, cut_down, cut_up;
+    Cut pair_dh, pair_dx;     // the inner gradient with dw_down, dx with dw_gate and dw_up, if splits > 0
     BackwardPlan(const arena_ffn_desc* d, const arena_ffn_grads* g, void* base)
         : FfnPlan(d, false, base),
           dy(w, g->dy, g->ld_dy, d->tokens, d->model, Operand::direct(g->dy, g->ld_dy, d->model))
@@ -403,13 +443,26 @@ struct BackwardPlan : FfnPlan {
         pair = g->dw_gate && g->dw_up && g->ld_dw_gate == g->ld_dw_up;
         const int pairs = pair ? 2 : 1;
         const double bytes = bytes_of(g->grad_dtype) * (g->accumulate ? 2.0 : 1.0);
-        cut_dh = choose_cut(T, F, ceil_div(D, bk), 1, false, false, 10.0);
-        cut_dx = choose_cut(T, D, 2 * ceil_div(F, bk), 1, false, false, 2.0);
-        cut_down = choose_cut(D, F, ceil_div(T, bk), 1, false, false, bytes);
-        cut_up = choose_cut(F, D, ceil_div(T, bk), pairs, false, false, bytes);
-        part = w.take(std::max(std::max(part_bytes(cut_dh, T, F, 1, false, false), part_bytes(cut_dx, T, D, 1, false, false)),
-                               std::max(part_bytes(cut_down, D, F, 1, false, false),
-                                        part_bytes(cut_up, F, D, pairs, false, false))));
+        Half dh = {T, F, ceil_div(D, bk), 1, 10.0, 0.0}, dx = {T, D, 2 * ceil_div(F, bk), 1, 2.0, 0.0};
+        Half down = {D, F, ceil_div(T, bk), 1, bytes, 0.0}, up = {F, D, ceil_div(T, bk), pairs, bytes, 0.0};
+        auto alone = [](Half& h) { return choose_cut(h.M, h.N, h.steps, h.batch, false, false, h.bytes, &h.alone); };
+        cut_dh = alone(dh);
+        cut_dx = alone(dx);
+        cut_down = alone(down);
+        cut_up = alone(up);
+        pair_dh = pair_dx = Cut{arena::mm::k128, arena::mm::k128, 0, 0, 0};
+        const bool inner_grad = g->dx || g->dw_gate || g->dw_up;
+        if (T > 0 && inner_grad && g->dw_down) pair_dh = choose_pair(dh, down);
+        if (T > 0 && g->dx && pair) pair_dx = choose_pair(dx, up);
+        int64_t most = 0;
+        auto need = [&](const Half& h, const Cut& cut) {
+            most = std::max(most, part_bytes(cut, h.M, h.N, h.batch, false, false));
+        };
+        need(dh, pair_dh.splits ? pair_dh : cut_dh);
+        need(dx, pair_dx.splits ? pair_dx : cut_dx);
+        if (!pair_dh.splits) need(down, cut_down);
+        if (!pair_dx.splits) need(up, cut_up);
+        part = w.take(most);
     }
 };
 
@@ -642,7 +695,7 @@ arena_status arena_ffn_forward(arena_ctx* c, const arena_ffn_desc* d, void* stre
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
-    hipError_t e = P.pack(s);
+    hipError_t e = pack({&P.x, &P.gate, &P.up, &P.down}, s);
     if (e) return hip_error(c, e, "ffn forward copies");
 
     GemmArgs A = new_args(d->tokens, d->inner, d->model);
@@ -693,34 +746,27 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
     hipStream_t s = (hipStream_t)stream;
     const int64_t T = f->tokens, D = f->model, F = f->inner;
     const int out = g->grad_dtype == ARENA_F32 ? arena::mm::kOutF32 : arena::mm::kOut16;
-    hipError_t e = P.pack(s);
-    if (e || (e = P.dy.pack(s))) return hip_error(c, e, "ffn backward copies");
+    hipError_t e = pack({&P.x, &P.gate, &P.up, &P.down, &P.dy}, s);
+    if (e) return hip_error(c, e, "ffn backward copies");
 
-    if (T > 0 && (g->dx || g->dw_gate || g->dw_up)) {
-        GemmArgs A = new_args(T, F, D);
-        A.a[0] = P.dy.p; A.lda = P.dy.ld;
-        A.b[0] = P.down.p; A.ldb = P.down.ld;
-        A.g = f->g; A.u = f->u; A.ldg = f->ld_inner;
-        A.c[0] = P.dg; A.c[1] = P.du; A.ldc = P.ld;
-        A.act = f->activation;
-        A.pad = (int)P.ld;
-        A.part = (float*)P.part;
-        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kGateUpBack, P.cut_dh, s)))
-            return hip_error(c, e, "ffn inner gradient launch");
-    }
-    if (T > 0 && g->dx) {
-        GemmArgs A = new_args(T, D, F);
-        A.nseg = 2;
-        A.a[0] = P.dg; A.a[1] = P.du; A.lda = P.ld;
-        A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld;
-        A.c[0] = g->dx; A.ldc = g->ld_dx;
-        A.part = (float*)P.part;
-        if ((e = arena::mm::launch_gemm(A, f->dtype, arena::mm::kRowsCols, P.cut_dx, s)))
-            return hip_error(c, e, "ffn input gradient launch");
-    }
-    // weight gradients: C[m, n] = sum over tokens of a(t, m) b(t, n), beside what accumulate keeps
+    // the inner gradient, dx, and the weight gradients C[m, n] = sum over tokens
+    // of a(t, m) b(t, n) beside what accumulate keeps
+    GemmArgs H = new_args(T, F, D);
+    H.a[0] = P.dy.p; H.lda = P.dy.ld;
+    H.b[0] = P.down.p; H.ldb = P.down.ld;
+    H.g = f->g; H.u = f->u; H.ldg = f->ld_inner;
+    H.c[0] = P.dg; H.c[1] = P.du; H.ldc = P.ld;
+    H.act = f->activation;
+    H.pad = (int)P.ld;
+    H.part = (float*)P.part;
+    GemmArgs X = new_args(T, D, F);
+    X.nseg = 2;
+    X.a[0] = P.dg; X.a[1] = P.du; X.lda = P.ld;
+    X.b[0] = P.gate.p; X.b[1] = P.up.p; X.ldb = P.gate.ld;
+    X.c[0] = g->dx; X.ldc = g->ld_dx;
+    X.part = (float*)P.part;
     auto weight = [&](const void* a0, const void* a1, int64_t lda, const void* b, int64_t ldb, int64_t M, int64_t N,
-                      void* c0, void* c1, int64_t ldc, const Cut& cut) {
+                      void* c0, void* c1, int64_t ldc) {
         GemmArgs A = new_args(M, N, T);
         A.pairs = c1 != nullptr;
         A.batch = c1 ? 2 : 1;
@@ -733,22 +779,39 @@ arena_status arena_ffn_backward(arena_ctx* c, const arena_ffn_desc* f, const are
             A.e[0] = c0; A.e[1] = c1; A.lde = ldc;
         }
         A.part = (float*)P.part;
-        return arena::mm::launch_gemm(A, f->dtype, arena::mm::kColsCols, cut, s);
+        return A;
     };
-    if (g->dw_down && (e = weight(P.dy.p, nullptr, P.dy.ld, f->h, f->ld_inner, D, F, g->dw_down, nullptr,
-                                  g->ld_dw_down, P.cut_down)))
-        return hip_error(c, e, "ffn down gradient launch");
+    const GemmArgs down = weight(P.dy.p, nullptr, P.dy.ld, f->h, f->ld_inner, D, F, g->dw_down, nullptr, g->ld_dw_down);
+    const bool inner_grad = T > 0 && (g->dx || g->dw_gate || g->dw_up);
+    using namespace arena::mm;
+    if (P.pair_dh.splits) {
+        if ((e = launch_pair(H, f->dtype, kGateUpBack, down, P.pair_dh, s)))
+            return hip_error(c, e, "ffn inner and down gradients launch");
+    } else {
+        if (inner_grad && (e = launch_gemm(H, f->dtype, kGateUpBack, P.cut_dh, s)))
+            return hip_error(c, e, "ffn inner gradient launch");
+        if (g->dw_down && (e = launch_gemm(down, f->dtype, kColsCols, P.cut_down, s)))
+            return hip_error(c, e, "ffn down gradient launch");
+    }
     if (P.pair) {
-        if ((e = weight(P.dg, P.du, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, g->dw_up, g->ld_dw_gate, P.cut_up)))
+        const GemmArgs up = weight(P.dg, P.du, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, g->dw_up, g->ld_dw_gate);
+        if (P.pair_dx.splits) {
+            if ((e = launch_pair(X, f->dtype, kRowsCols, up, P.pair_dx, s)))
+                return hip_error(c, e, "ffn input, gate and up gradients launch");
+            return ARENA_OK;
+        }
+        if ((e = launch_gemm(up, f->dtype, kColsCols, P.cut_up, s)))
             return hip_error(c, e, "ffn gate and up gradient launch");
     } else {
-        if (g->dw_gate && (e = weight(P.dg, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, nullptr, g->ld_dw_gate,
-                                      P.cut_up)))
+        if (g->dw_gate && (e = launch_gemm(weight(P.dg, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, nullptr,
+                                                  g->ld_dw_gate), f->dtype, kColsCols, P.cut_up, s)))
             return hip_error(c, e, "ffn gate gradient launch");
-        if (g->dw_up && (e = weight(P.du, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_up, nullptr, g->ld_dw_up,
-                                    P.cut_up)))
+        if (g->dw_up && (e = launch_gemm(weight(P.du, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_up, nullptr,
+                                                g->ld_dw_up), f->dtype, kColsCols, P.cut_up, s)))
             return hip_error(c, e, "ffn up gradient launch");
     }
+    if (T > 0 && g->dx && (e = launch_gemm(X, f->dtype, kRowsCols, P.cut_dx, s)))
+        return hip_error(c, e, "ffn input gradient launch");
     return ARENA_OK;
 }
 

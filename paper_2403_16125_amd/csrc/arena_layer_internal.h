@@ -83,15 +83,26 @@ struct Cut {
 // readable (and zero where that axis is k).
 hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s);
 
+// Two independent products in one launch, both on 128 x 128 tiles: A of layout
+// rows x cols (what: kGateUpBack or kRowsCols) with k in cut.splits parts, B of
+// layout cols x cols.
+hipError_t launch_pair(const GemmArgs& A, int dtype, Product what, const GemmArgs& B, const Cut& cut, hipStream_t s);
+
 constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel without LDS tiles takes
 
 // C = A B^T with both operands' k contiguous, M <= kSkinnyRows; dual: the gated
 // forward product.
 hipError_t launch_skinny(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
 
-// Copies rows x cols 16-bit values with zeros in columns cols .. ld_to - 1.
-hipError_t launch_pack(const void* from, int64_t ld_from, void* to, int64_t ld_to, int64_t rows, int64_t cols,
-                       hipStream_t s);
+// Copies of matrices of 16-bit values, rows x cols, with zeros in columns cols ..
+// ld_to - 1; one launch.
+struct Pack {
+    const void* from;
+    void* to;
+    int64_t ld_from, ld_to, rows, cols;
+};
+constexpr int kMaxPacks = 5;
+hipError_t launch_packs(const Pack* packs, int n, hipStream_t s);
 
 }  // namespace mm
 
