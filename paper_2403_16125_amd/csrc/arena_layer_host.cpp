@@ -105,7 +105,7 @@ constexpr TileCost kTileCost[arena::mm::kTileKinds] = {
 constexpr double kEpilogueRate = 40e3;
 constexpr double kLaunch = 3.0;             // a launch
 constexpr double kSeam = 8.0;               // and the compute units that idle before it for others' last tiles
-constexpr double kJoin = 4.0, kJoinRate = 2.0;     // joining parts: the launch, and megabytes a microsecond
+constexpr double kJoin = 4.0, kJoinRate = 3.0;     // joining parts: the launch, and megabytes a microsecond
 constexpr int64_t kUnits = 256;             // compute units
 
 // `tiles` tiles of a kind in one launch, k in `splits` parts.  bytes: what the
@@ -190,8 +190,8 @@ Cut choose_pair(const Half& a, const Half& b)
         const double ta = per * step + k.start + value * (s > 1 ? 4.0 : a.bytes);
         const double tb = b.steps * step + k.start + value * b.bytes;
         const double work = (blocks * ta + nb * tb) / slots, longest = std::max(ta, tb);
-        // a last round is on average half idle
-        const double t = kLaunch + std::max(longest, work + (blocks + nb > slots ? 0.5 * longest : 0.0)) +
+        // a last round leaves some slots idle, fewer than of equal blocks
+        const double t = kLaunch + std::max(longest, work + (blocks + nb > slots ? 0.25 * longest : 0.0)) +
                          (s > 1 ? kJoin + blocks * 128.0 * 128.0 * 4e-6 / kJoinRate : 0.0);
         if (t < least) {
             least = t;
