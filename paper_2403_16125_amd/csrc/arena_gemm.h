@@ -833,7 +833,7 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_kernel(const GemmArgs A)
     const E* w[NB];
     const E* x[NT];
     w[0] = (const E*)A.b[0] + (int64_t)row * A.ldb + kc;
-    if (DUAL) w[NB - 1] = (const E*)A.b[1] + (int64_t)row * A.ldb + kc;
+    if (DUAL) w[NB - 1] = (const E*)A.b[1] + (int64_t)row * A.ldb1 + kc;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
         x[t] = (const E*)A.a[0] + (int64_t)min(t * 16 + (lane & 15), A.M - 1) * A.lda + kc;

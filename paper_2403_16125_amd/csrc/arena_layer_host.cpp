@@ -397,8 +397,8 @@ struct FfnPlan {
           gate_ok(Operand::direct(d->w_gate, d->ld_gate, d->model) && Operand::direct(d->w_up, d->ld_up, d->model) &&
                   d->ld_gate == d->ld_up),
           x(w, d->x, d->ld_x, d->tokens, d->model, skinny || Operand::direct(d->x, d->ld_x, d->model)),
-          gate(w, d->w_gate, d->ld_gate, d->inner, d->model, (skinny && d->ld_gate == d->ld_up) || gate_ok),
-          up(w, d->w_up, d->ld_up, d->inner, d->model, (skinny && d->ld_gate == d->ld_up) || gate_ok),
+          gate(w, d->w_gate, d->ld_gate, d->inner, d->model, skinny || gate_ok),
+          up(w, d->w_up, d->ld_up, d->inner, d->model, skinny || gate_ok),
           down(w, d->w_down, d->ld_down, d->model, d->inner, skinny || Operand::direct(d->w_down, d->ld_down, d->inner))
     {
     }
@@ -700,7 +700,7 @@ arena_status arena_ffn_forward(arena_ctx* c, const arena_ffn_desc* d, void* stre
 
     GemmArgs A = new_args(d->tokens, d->inner, d->model);
     A.a[0] = P.x.p; A.lda = P.x.ld;
-    A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld;
+    A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld; A.ldb1 = P.up.ld;
     A.c[0] = d->h; A.ldc = d->ld_inner;
     A.g = d->g; A.u = d->u; A.ldg = d->ld_inner;
     A.act = d->activation;

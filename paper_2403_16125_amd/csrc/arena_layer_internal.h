@@ -31,6 +31,7 @@ struct GemmArgs {
     const void* b[2];
     void* c[2];
     int64_t lda, ldb, ldc;    // elements
+    int64_t ldb1;             // few tokens: of b[1]
     int64_t sa, sb, sc;       // batch strides, elements
     int32_t M, N, K;
     int32_t nseg, pairs, batch;
@@ -112,7 +113,8 @@ struct NormArgs {
     int64_t ld_x, ld_y, ld_gate, ld_r, ld_n;
     void *r, *n;
     float* stats;                 // [tokens][4]: mean and 1/deviation of the block's output, then of the stream
-    int64_t tokens, gate_rows;    // gate_rows: tokens of one gate row (all of them: tokens, at least 1)
+    int64_t first_token, tokens;  // rows first_token .. tokens - 1 (the backward: from 0)
+    int64_t gate_rows;            // tokens of one gate row (all of them: tokens, at least 1)
     int32_t width, layer;         // layer: subtract the mean
     float eps, scale;
     // backward

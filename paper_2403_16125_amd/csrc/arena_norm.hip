@@ -160,7 +160,7 @@ __global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_forward_kernel(c
 {
     typedef Row<WV, IT> R;
     __shared__ float lds[2][WV][1];
-    const int64_t t = R::worker();
+    const int64_t t = A.first_token + R::worker();
     if (WV == 1 && t >= A.tokens) return;
     int slot = 0;
     float r[IT][8];
@@ -553,7 +553,7 @@ int waves_of(int width) { return width <= 512 ? 1 : width <= 2048 ? 4 : 8; }
 template <typename TY, typename TX>
 hipError_t forward(const NormArgs& A, hipStream_t s)
 {
-    const int64_t n = A.tokens;
+    const int64_t n = A.tokens - A.first_token;
     switch (waves_of(A.width)) {
     case 1: norm_forward_kernel<TY, TX, 1, 1><<<(unsigned)((n + 3) / 4), 256, 0, s>>>(A); break;
     case 4: norm_forward_kernel<TY, TX, 4, 1><<<(unsigned)n, 256, 0, s>>>(A); break;
@@ -611,12 +611,30 @@ void norm_plan(int64_t tokens, int64_t gate_rows, int width, int* workers, int* 
     *workers = (int)((tokens + each - 1) / each);
 }
 
-hipError_t launch_norm_forward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s)
+namespace {
+
+hipError_t forward_any(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s)
 {
     if (dtype == ARENA_F32) return forward<float, float>(A, s);
     if (dtype == ARENA_BF16)
         return stream_dtype == ARENA_F32 ? forward<__bf16, float>(A, s) : forward<__bf16, __bf16>(A, s);
     return stream_dtype == ARENA_F32 ? forward<_Float16, float>(A, s) : forward<_Float16, _Float16>(A, s);
+}
+
+}  // namespace
+
+hipError_t launch_norm_forward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s)
+{
+    // a launch holds less than 2^32 threads
+    constexpr int64_t kMost = 1 << 22;
+    NormArgs part = A;
+    for (int64_t t = 0; t < A.tokens; t += kMost) {
+        part.first_token = t;
+        part.tokens = A.tokens - t < kMost ? A.tokens : t + kMost;
+        const hipError_t e = forward_any(part, dtype, stream_dtype, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_norm_backward(const NormArgs& A, int dtype, int stream_dtype, hipStream_t s)

@@ -293,6 +293,45 @@ def test_norm_large_mean(ops):
     inside("n", n, want, torch.full_like(want, 1000 * 2.0 ** -22))
 
 
+def test_norm_wide_rows_in_place(ops):
+    """Past 8192 columns the sums have a pass of their own, which then finds dx where dr was."""
+    T, D = 30, 9000
+    t = norm_inputs(T, D, BF16, F32, 7)
+    given = dict(gate=t["gate"], gate_rows=7, w_post=t["w_post"], w_pre=t["w_pre"], scale=0.5)
+    r, n, stats = ops.norm_forward(t["x"], t["y"], save=True, **given)
+    want = ops.norm_backward(t["dn"], t["dr"], r, t["y"], stats, **given)
+    dr = t["dr"].clone()
+    dgate, dw2, dw1 = torch.empty_like(t["gate"]), torch.empty_like(t["w_post"]), torch.empty_like(t["w_pre"])
+    d = layer.NormDesc(dtype=1, stream_dtype=0, kind=0, width=D, tokens=T, gate_rows=7, eps=1e-6, scale=0.5,
+                       y=t["y"].data_ptr(), ld_y=D, gate=t["gate"].data_ptr(), ld_gate=D, w_post=t["w_post"].data_ptr(),
+                       w_pre=t["w_pre"].data_ptr(), r=r.data_ptr(), ld_r=D, stats=stats.data_ptr())
+    need = layer.arena_norm_backward_workspace(ops.ctx, d)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    g = layer.NormGrads(dn=t["dn"].data_ptr(), ld_dn=D, dr=dr.data_ptr(), ld_dr=D, dx=dr.data_ptr(), ld_dx=D,
+                        dgate=dgate.data_ptr(), dw_post=dw2.data_ptr(), dw_pre=dw1.data_ptr(), workspace=ws.data_ptr(),
+                        workspace_bytes=need)
+    layer.arena_norm_backward(ops.ctx, d, g, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(dr, want["dx"])
+    sizes = ref.block_back(t["dn"], t["dr"], r, t["y"], stats, t["gate"], 7, 0.5, t["w_post"], None, t["w_pre"], "rms")
+    for name, got in (("dgate", dgate), ("dw_post", dw2), ("dw_pre", dw1)):
+        near_sums(name, got, sizes[name], sizes["_" + name])
+
+
+def test_norm_many_rows(ops):
+    """More rows than a launch's workers."""
+    x = normal((4200000, 6), BF16, 12)
+    r, n = ops.norm_forward(x, x, kind="layer", eps=1e-3)
+    wr, wn = ref.block(x, x, None, 0, 1.0, None, None, None, None, "layer", 1e-3)
+    near_rows("r", r, wr)
+    near_rows("n", n, wn)
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_ffn_gate_and_up_with_strides_of_their_own(ops, T):
+    x, wg, wu, wd, dy = ffn_inputs(T, 64, 96, BF16)
+    check_ffn(ops, (x, strided(wg, 8, 0), strided(wu, 24, 8), wd, dy), "gelu", BF16)
+
+
 def test_norm_in_place(ops):
     """r over x and dx over dr, as the header allows."""
     t = norm_inputs(40, 520, BF16, F32, 0)
