@@ -249,18 +249,20 @@ struct BackRow {
     }
 };
 
-// A worker goes down rows_each rows.  With 8 values a thread (AHEAD) the next
-// row's are on their way while it works on one, and the weights stay in
-// registers.  With more it reads each value where it uses it, twice from a
-// cache.  With 32 (past 8192 columns) the column sums have no place either (a
-// form that kept them spilled up to 1.3 KB a thread, 4096 x 12288 501 us): then
-// the rows' means are left for norm_sums_kernel, which reads four of the six
-// matrices once more.
+// A worker goes down rows_each rows.  AHEAD: the next row's values are on their
+// way while it works on one, and the weights stay in registers.  Otherwise it
+// reads each value where it uses it, twice from a cache: with 16 waves there are
+// 128 registers a thread, and two blocks of 8 waves on a compute unit need as few
+// (16384 x 4096: 225 us with 135 registers and one block, 190 with 128).
+// Past 8192 columns the column sums have no place either (a form that kept them
+// spilled up to 1.3 KB a thread, 4096 x 12288 501 us; 289 so): the rows' means
+// are left for norm_sums_kernel, which reads four of the six matrices once more.
 template <typename TY, typename TX, int WV, int IT, bool BIAS>
-__global__ __launch_bounds__((Row<WV, IT>::kThreads)) void norm_backward_kernel(const NormArgs A)
+__global__ __launch_bounds__((Row<WV, IT>::kThreads), (WV == 16 || (WV == 8 && IT == 1 && !BIAS && sizeof(TY) == 2) ? 4 : 2))
+void norm_backward_kernel(const NormArgs A)
 {
     typedef Row<WV, IT> R;
-    constexpr bool AHEAD = IT == 1, SUMS = IT <= 2;
+    constexpr bool AHEAD = IT == 1 && WV < 16, SUMS = IT == 1 || WV < 16;
     __shared__ float lds[2][WV][2];
     const int64_t me = R::worker();
     if (me >= A.workers) return;
@@ -547,7 +549,10 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormArgs A)
     if (part == 0 && c < A.width) out[c] = (TY)lds[0][lane];
 }
 
-// Waves of a worker by width: 8 values a thread up to 4096, then 16, past 8192 32.
+// Waves of a worker by width, 8 values a thread up to 4096 columns.  Past that the
+// forward takes 16 or 32 a thread; the backward 16 waves (of 8 or 16 values), or 8 of
+// 16 values where two more sums or 32-bit values would not fit 128 registers
+// (8192 x 8192 with biases: 560 us with 16 waves, 474 with 8; without 249 and 311).
 int waves_of(int width) { return width <= 512 ? 1 : width <= 2048 ? 4 : 8; }
 
 template <typename TY, typename TX>
@@ -574,8 +579,9 @@ hipError_t backward(const NormArgs& A, hipStream_t s)
     case 4: norm_backward_kernel<TY, TX, 4, 1, BIAS><<<n, 256, 0, s>>>(A); break;
     default:
         if (A.width <= 4096) norm_backward_kernel<TY, TX, 8, 1, BIAS><<<n, 512, 0, s>>>(A);
-        else if (A.width <= kNormSumsWidth) norm_backward_kernel<TY, TX, 8, 2, BIAS><<<n, 512, 0, s>>>(A);
-        else norm_backward_kernel<TY, TX, 8, 4, BIAS><<<n, 512, 0, s>>>(A);
+        else if (A.width > kNormSumsWidth) norm_backward_kernel<TY, TX, 16, 2, BIAS><<<n, 1024, 0, s>>>(A);
+        else if constexpr (BIAS || sizeof(TY) == 4) norm_backward_kernel<TY, TX, 8, 2, BIAS><<<n, 512, 0, s>>>(A);
+        else norm_backward_kernel<TY, TX, 16, 1, BIAS><<<n, 1024, 0, s>>>(A);
     }
     if (n && A.width > kNormSumsWidth)
         norm_sums_kernel<TY, TX, BIAS><<<dim3((A.width + 2047) / 2048, n), 256, 0, s>>>(A);

@@ -225,6 +225,13 @@ def test_norm_without_parameters(ops, use):
     check_norm(ops, norm_inputs(20, 200, BF16, BF16, 0), 0, "rms", use=use)
 
 
+@pytest.mark.parametrize("typ,stream", [(BF16, BF16), (F16, F32), (F32, F32)])
+@pytest.mark.parametrize("T,D", [(50, 1500), (9, 3000), (700, 5000), (40, 8000), (600, 9000)])
+def test_norm_without_biases(ops, T, D, typ, stream):
+    """The rows' shapes by width, where two fewer sums leave other forms of the backward."""
+    check_norm(ops, norm_inputs(T, D, typ, stream, 300), 300, "rms", use=("gate", "w_post", "w_pre"))
+
+
 @pytest.mark.parametrize("T,D,rows", [(4100, 512, 1000), (3001, 520, 7), (2500, 96, 1), (1500, 3000, 600)])
 def test_norm_gate_rows_across_workers(ops, T, D, rows):
     """Gate rows shared by workers, several to a worker, one token each."""
