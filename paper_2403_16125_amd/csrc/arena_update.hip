@@ -4,7 +4,9 @@
 //
 // The norm has to be known before X0 can be rounded, so U is formed twice: by
 // the sum of squares (which stores M') and by the scaling.  Both are bound by
-// memory, and small beside the products that follow.
+// memory, and small beside the products that follow: 10944 x 4096 in float32 with
+// momentum 112 us (538 MB, 4.8 TB/s) and 77 us (448 MB, 5.8 TB/s, part of it from
+// the cache) of 3200.
 //
 // X0 is held in float16 times 2^12.  Its entries are at most 1 in magnitude
 // and about 1 / sqrt(rows cols) in size, and the products' operands keep 11

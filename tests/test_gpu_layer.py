@@ -361,6 +361,46 @@ def test_norm_in_place(ops):
     assert torch.equal(dr, want["dx"])
 
 
+@pytest.mark.parametrize("D", [2, 5, 7, 8, 9, 15, 505, 513, 519, 1366, 2047, 2053, 4099, 8197, 9001])
+def test_norm_rows_of_all_ends(ops, D):
+    """Rows that end inside eight values: what lies past them is neither used nor written, in place or not."""
+    T, gap = 21, 11
+    t = norm_inputs(T, D, BF16, F32, 0)
+    given = dict(gate=t["gate"], w_post=t["w_post"], w_pre=t["w_pre"], scale=0.5, kind="layer", eps=1e-3)
+    r, n, stats = ops.norm_forward(t["x"], t["y"], save=True, **given)
+    want = ops.norm_backward(t["dn"], t["dr"], r, t["y"], stats, **given)
+
+    def wide(v, fill):
+        w = torch.full((T, D + gap), fill, dtype=v.dtype, device="cuda")
+        w[:, :D] = v
+        return w
+    nan = float("nan")
+    x, y, dn, dr = wide(t["x"], nan), wide(t["y"], nan), wide(t["dn"], nan), wide(t["dr"], nan)
+    n2 = wide(torch.zeros_like(n), 7.0)
+    s2 = torch.empty_like(stats)
+    dw2, dw1 = torch.empty_like(t["w_post"]), torch.empty_like(t["w_pre"])
+    dgate = torch.empty_like(t["gate"])
+    stream, L = torch.cuda.current_stream().cuda_stream, D + gap
+    d = layer.NormDesc(dtype=1, stream_dtype=0, kind=1, width=D, tokens=T, eps=1e-3, scale=0.5, x=x.data_ptr(), ld_x=L,
+                       y=y.data_ptr(), ld_y=L, gate=t["gate"].data_ptr(), ld_gate=D, w_post=t["w_post"].data_ptr(),
+                       w_pre=t["w_pre"].data_ptr(), r=x.data_ptr(), ld_r=L, n=n2.data_ptr(), ld_n=L, stats=s2.data_ptr())
+    layer.arena_norm_forward(ops.ctx, d, stream)
+    assert torch.equal(x[:, :D], r) and bool(x[:, D:].isnan().all())
+    assert torch.equal(n2[:, :D], n) and bool((n2[:, D:] == 7.0).all()) and torch.equal(s2, stats)
+    need = layer.arena_norm_backward_workspace(ops.ctx, d)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    dy = wide(torch.zeros_like(t["y"]), 7.0)
+    g = layer.NormGrads(dn=dn.data_ptr(), ld_dn=L, dr=dr.data_ptr(), ld_dr=L, dx=dr.data_ptr(), ld_dx=L,
+                        dy=dy.data_ptr(), ld_dy=L, dgate=dgate.data_ptr(), dw_post=dw2.data_ptr(),
+                        dw_pre=dw1.data_ptr(), workspace=ws.data_ptr(), workspace_bytes=need)
+    layer.arena_norm_backward(ops.ctx, d, g, stream)
+    assert torch.equal(dr[:, :D], want["dx"]) and bool(dr[:, D:].isnan().all())
+    assert torch.equal(dy[:, :D], want["dy"]) and bool((dy[:, D:] == 7.0).all())
+    sizes = ref.block_back(t["dn"], t["dr"], r, t["y"], stats, t["gate"], 0, 0.5, t["w_post"], None, t["w_pre"], "layer")
+    for name, got in (("dgate", dgate), ("dw_post", dw2), ("dw_pre", dw1)):
+        near_sums(name, got, sizes[name].reshape(got.shape), sizes["_" + name].reshape(got.shape))
+
+
 # ---------------------------------------------------------------- orthogonalised update
 
 def check_update(ops, grad, steps=5, coefficients=COEF, scale=1.5, momentum=None, mu=0.9, nesterov=True, dtype=BF16,
