@@ -493,8 +493,10 @@ constexpr double kHalfMost = 15.5;         // magnitudes that holds, with room f
 // error against 64 bits fell from 1.3-1.9e-3 to 0.7-1.1e-3 (64 to 1000 rows).
 constexpr double kCentre = 0.5;
 
-// Whether every matrix of the iteration stays within kHalfMost: bounds on the
-// singular values, at the ends and the stationary points of the polynomials.
+// Whether every matrix of the iteration stays within kHalfMost: bounds over the
+// singular values from 0 (a normalised matrix of some size has nearly all of them
+// there, the padding of a small one exactly) to their largest, at both ends and the
+// stationary points of the polynomials.
 bool polynomial_holds(const float* k, int steps)
 {
     double s = 1.0;
@@ -503,7 +505,7 @@ bool polynomial_holds(const float* k, int steps)
         const double t = s * s;
         auto B = [&](double v) { return std::fabs((b + 2.0 * c * kCentre) * (v - kCentre) + c * (v - kCentre) * (v - kCentre)); };
         auto X = [&](double v) { return std::sqrt(v) * std::fabs(a + b * v + c * v * v); };
-        double most_b = B(t), most_x = X(t);
+        double most_b = std::max(B(0.0), B(t)), most_x = X(t);
         if (c != 0.0) {
             const double v = -b / (2.0 * c);
             if (v > 0.0 && v < t) most_b = std::max(most_b, B(v));
