@@ -630,7 +630,8 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
         asm volatile("" ::: "memory");
         char* const ta = bufa((u + kAhead) % P::kStages);
         char* const tb = bufb((u + kAhead) % P::kStages);
-        // woven, past the end the last step is fetched again, into a buffer that nothing reads
+        // woven, past the end the last step is fetched again, into buffers that no step
+        // reads; the epilogue waits for them
         const int next = P::kWoven ? min(step + kAhead, end - 1) : step + kAhead;
         if (!P::kWoven && next < end) fetch(next, ta, tb, Int<3>());
         __builtin_amdgcn_sched_barrier(0);
@@ -696,6 +697,10 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             }
         }
     };
+    // Loads into LDS may still be in flight here, and a wave's land in slices that
+    // others write: each waits for its own before the barrier, which does not.
+    asm volatile("" ::: "memory");
+    wait_loads<0>();
     if (P::BM == 256) ask(0, side);      // no registers are left for it before
     __syncthreads();
 #pragma unroll
