@@ -248,11 +248,21 @@ class LayerOps:
         desc.workspace, desc.workspace_bytes = None, 0
         return None
 
-    def _run(self, stream, body, *args):
-        """body(stream handle, *args), allocating on that stream."""
-        if stream is None:
-            return body(self._current(self._index).cuda_stream, *args)
-        with self.torch.cuda.stream(stream):
+    def _run(self, stream, tensors, body, *args):
+        """body(stream handle, *args), allocating on that stream.  tensors: all that
+        the call is given, some of them None."""
+        current = self._current(self._index)
+        if stream is None or stream == current:
+            return body(current.cuda_stream, *args)
+        cuda = self.torch.cuda
+        outside = not cuda.is_current_stream_capturing()
+        with cuda.stream(stream):
+            # a stream under capture cannot wait for one outside of it
+            if not (outside and cuda.is_current_stream_capturing()):
+                stream.wait_stream(current)
+            for t in tensors:
+                if t is not None and t.is_cuda:
+                    t.record_stream(stream)
             return body(stream.cuda_stream, *args)
 
     # -- norms around a block
@@ -289,8 +299,8 @@ class LayerOps:
         row t // gate_rows for token t (gate_rows 0: one row).  dtype: n's type
         where y is None (x's by default).  next_norm=False leaves n out (None).
         Returns (r, n), with save=True (r, n, stats) for norm_backward."""
-        return self._run(stream, self._norm_forward, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind,
-                         eps, dtype, next_norm, save)
+        return self._run(stream, (x, y, gate, w_post, b_post, w_pre, b_pre), self._norm_forward, x, y, gate, gate_rows,
+                         scale, w_post, b_post, w_pre, b_pre, kind, eps, dtype, next_norm, save)
 
     def _norm_forward(self, handle, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps, dtype,
                       next_norm, save):
@@ -319,8 +329,8 @@ class LayerOps:
         the forward's r, y (None: no block before), stats and parameters.
         Returns a dict of dx, dy, dgate, dw_post, db_post, dw_pre and db_pre,
         None where there is no such input."""
-        return self._run(stream, self._norm_backward, dn, dr, r, y, stats, gate, gate_rows, scale, w_post, b_post, w_pre,
-                         b_pre, kind, eps)
+        return self._run(stream, (dn, dr, r, y, stats, gate, w_post, b_post, w_pre, b_pre), self._norm_backward, dn, dr, r,
+                         y, stats, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps)
 
     def _norm_backward(self, handle, dn, dr, r, y, stats, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind,
                        eps):
@@ -378,7 +388,8 @@ class LayerOps:
         """y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [..., model], w_gate
         and w_up [inner, model], w_down [model, inner], bfloat16 or float16.
         Returns y, with save=True (y, FfnSaved) for ffn_backward."""
-        return self._run(stream, self._ffn_forward, x, w_gate, w_up, w_down, activation, save, out)
+        return self._run(stream, (x, w_gate, w_up, w_down, out), self._ffn_forward, x, w_gate, w_up, w_down, activation,
+                         save, out)
 
     def _ffn_forward(self, handle, x, w_gate, w_up, w_down, activation, save, out):
         d = self._ffn_desc(x, w_gate, w_up, w_down, activation)
@@ -402,7 +413,8 @@ class LayerOps:
         """(dx, dw_gate, dw_up, dw_down) from dy, with the forward's inputs and
         `saved`.  grads: three tensors for the weights' gradients, of x's type
         or float32, which accumulate=True adds to."""
-        return self._run(stream, self._ffn_backward, dy, x, w_gate, w_up, w_down, saved, activation, grads, accumulate)
+        return self._run(stream, (dy, x, w_gate, w_up, w_down, saved.buffer, *(() if grads is None else grads)),
+                         self._ffn_backward, dy, x, w_gate, w_up, w_down, saved, activation, grads, accumulate)
 
     def _ffn_backward(self, handle, dy, x, w_gate, w_up, w_down, saved, activation, grads, accumulate):
         d = self._ffn_desc(x, w_gate, w_up, w_down, activation)
@@ -441,8 +453,8 @@ class LayerOps:
         momentum: float32 of grad's shape, updated in place, or into
         momentum_out.  coefficients: (a, b, c) for every step, or one such triple a
         step.  dtype: of the result (bfloat16 by default, or out's)."""
-        return self._run(stream, self._orthogonal_update, grad, momentum, momentum_out, mu, nesterov, coefficients,
-                         steps, eps, scale, dtype, out)
+        return self._run(stream, (grad, momentum, momentum_out, out), self._orthogonal_update, grad, momentum,
+                         momentum_out, mu, nesterov, coefficients, steps, eps, scale, dtype, out)
 
     def _stack(self, name, t, shape, dtype):
         """Address, row stride and matrix stride of a tensor of two or three axes."""
