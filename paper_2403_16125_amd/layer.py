@@ -251,6 +251,11 @@ class LayerOps:
     def _run(self, stream, tensors, body, *args):
         """body(stream handle, *args), allocating on that stream.  tensors: all that
         the call is given, some of them None."""
+        if self.torch.is_grad_enabled():
+            for t in tensors:
+                if t is not None and t.requires_grad:
+                    raise ValueError(f"a tensor of shape {tuple(t.shape)} requires a gradient, which these calls do not "
+                                     "record: detach it, or call under torch.no_grad()")
         current = self._current(self._index)
         if stream is None or stream == current:
             return body(current.cuda_stream, *args)
