@@ -198,10 +198,13 @@ class LayerOps:
     # -- checks
 
     def _type(self, t) -> int:
+        return self._code(t.dtype)
+
+    def _code(self, dtype) -> int:
         try:
-            return self._types[t.dtype]
+            return self._types[dtype]
         except KeyError:
-            raise ValueError(f"type {t.dtype} is not supported") from None
+            raise ValueError(f"type {dtype} is not supported") from None
 
     def _matrix(self, name, t, shape, dtype):
         """Address and row stride of a 2-D tensor; a tensor of more axes is
@@ -276,7 +279,7 @@ class LayerOps:
         if kind not in NORM_KINDS:
             raise ValueError(f"kind must be one of {sorted(NORM_KINDS)}")
         tokens, width = x_shape
-        d = NormDesc(dtype=self._types[dtype], stream_dtype=self._types[stream_dtype], kind=NORM_KINDS[kind],
+        d = NormDesc(dtype=self._code(dtype), stream_dtype=self._code(stream_dtype), kind=NORM_KINDS[kind],
                      width=width, tokens=tokens, gate_rows=int(gate_rows), eps=eps, scale=scale)
         if gate is not None:
             rows = -(-tokens // gate_rows) if gate_rows else 1
@@ -310,7 +313,6 @@ class LayerOps:
     def _norm_forward(self, handle, x, y, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps, dtype,
                       next_norm, save):
         dtype = y.dtype if y is not None else dtype or x.dtype
-        self._type(x)
         shape = self._rows(x)
         d = self._norm_desc(shape, dtype, x.dtype, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps)
         d.x, d.ld_x = self._matrix("x", x, shape, x.dtype)
@@ -343,7 +345,6 @@ class LayerOps:
             raise ValueError("norm_backward needs dn or dr")
         shape = self._rows(r)
         dtype = y.dtype if y is not None else dn.dtype if dn is not None else r.dtype
-        self._type(r)
         d = self._norm_desc(shape, dtype, r.dtype, gate, gate_rows, scale, w_post, b_post, w_pre, b_pre, kind, eps)
         g = NormGrads()
         p, ld = self._matrix("r", r, shape, r.dtype)
