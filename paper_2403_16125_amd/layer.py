@@ -186,8 +186,8 @@ class LayerOps:
 
     def close(self) -> None:
         if getattr(self, "_alive", False):
-            arena.arena_destroy(self.ctx)
-            self._alive = False
+            ctx, self.ctx, self._alive = self.ctx, None, False      # later calls are refused
+            arena.arena_destroy(ctx)
 
     def __del__(self):
         try:

@@ -25,3 +25,18 @@ def test_types_that_no_norm_takes(ops, typ):
     for args in ((x, x, odd, x, stats), (odd, x, x, None, stats), (x, x, x, odd, stats)):
         with pytest.raises(ValueError, match=f"type {typ} is not supported"):
             ops._norm_backward(0, *args, *none)
+
+
+def test_calls_after_close_are_refused():
+    """The context is gone: nothing is handed to the library, whatever the call."""
+    o = layer.LayerOps()
+    o.close()
+    assert o.ctx is None
+    with pytest.raises(arena.ArenaError) as e:
+        layer.arena_norm_forward(o.ctx, layer.NormDesc())
+    assert e.value.status == 1
+    for query in (lambda: layer.arena_ffn_forward_workspace(o.ctx, layer.FfnDesc()),
+                  lambda: layer.arena_orthogonal_update_workspace(o.ctx, layer.UpdateDesc())):
+        with pytest.raises(arena.ArenaError):
+            query()
+    o.close()
