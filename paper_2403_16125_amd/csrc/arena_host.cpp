@@ -10,7 +10,6 @@
 #include <map>
 #include <numeric>
 #include <new>
-#include <string>
 #include <utility>
 #include <vector>
 
@@ -23,9 +22,18 @@ using arena::TypeDev;
 static_assert(ARENA_NOALLOC_SCRATCH_BYTES == arena::kNoallocScratchBytes, "scratch size of the header and the kernels");
 static_assert(ARENA_EXACT_T_MAX_LAYERS == arena::kExactTMaxLayers, "exact-T layer limit of the header and the kernels");
 
+// Why the last call failed.  No memory is taken for it: a refusal must not end in
+// an exception, which a C caller cannot catch.
+struct ErrorText {
+    char text[512] = "";
+    void clear() { text[0] = 0; }
+    const char* c_str() const { return text; }
+    void print(const char* fmt, va_list ap) { vsnprintf(text, sizeof(text), fmt, ap); }
+};
+
 struct arena_ctx {
     int device = 0;
-    std::string err;
+    ErrorText err;
 
     // jobs (host copies of per-job scalars; device pointers are the caller's)
     bool jobs_bound = false;
@@ -121,12 +129,10 @@ namespace {
 arena_status fail(arena_ctx* c, arena_status s, const char* fmt, ...)
 {
     if (c) {
-        char buf[512];
         va_list ap;
         va_start(ap, fmt);
-        vsnprintf(buf, sizeof(buf), fmt, ap);
+        c->err.print(fmt, ap);
         va_end(ap);
-        c->err = buf;
     }
     return s;
 }
@@ -1359,12 +1365,10 @@ void ctx_clear(arena_ctx* c) { c->err.clear(); }
 
 arena_status ctx_fail(arena_ctx* c, arena_status s, const char* fmt, ...)
 {
-    char buf[512];
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
+    c->err.print(fmt, ap);
     va_end(ap);
-    c->err = buf;
     return s;
 }
 
