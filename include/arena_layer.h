@@ -93,7 +93,7 @@ arena_status arena_norm_forward(arena_ctx* ctx, const arena_norm_desc* d, void* 
  * where y is NULL; stats is required).  Given dn and dr, the gradients of n and
  * r (either may be NULL: none), writes those of x (dx, of stream_dtype), y, the
  * gate (dense rows of `width`), weights and biases (of dtype); NULL outputs are
- * not computed.  dx may be dr itself. */
+ * not computed.  dx may be dr itself (same pointer and stride), with the same bits. */
 typedef struct arena_norm_grads {
     const void* dn; int64_t ld_dn;
     const void* dr; int64_t ld_dr;

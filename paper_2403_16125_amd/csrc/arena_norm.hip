@@ -417,7 +417,7 @@ void norm_backward_kernel(const NormArgs A)
                     d[it][i] += rs1 * (q - z * mz - mq);
                 }
             }
-            if (A.dx) put8<TX>(A.dx, t * A.ld_dx, c, lo, d[it]);
+            if (A.dx && (SUMS || A.dx != A.dr)) put8<TX>(A.dx, t * A.ld_dx, c, lo, d[it]);
         }
         if (!A.y) continue;
         float m[2] = {0.0f, 0.0f};
@@ -479,7 +479,8 @@ void norm_backward_kernel(const NormArgs A)
 
 // The workers' column sums of wide rows, from the means of dn w_pre rhat (and of
 // dn w_pre) that the rows' pass left: a thread owns 8 columns and goes down a
-// worker's rows.  Where dx was written over dr, the gradient of r is read from it.
+// worker's rows.  dx over dr is written here and not by the rows' pass: the sums
+// take the gradient of r as it is before it is rounded, so they need dr.
 template <typename TY, typename TX, bool BIAS>
 __global__ __launch_bounds__(256) void norm_sums_kernel(const NormArgs A)
 {
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormArgs A)
     if (A.w_pre) w1 = get8<TY, 16>(A.w_pre, 0, c, lo, A.width);
     if (A.w_post) w2 = get8<TY, 16>(A.w_post, 0, c, lo, A.width);
     if (BIAS && A.b_post) b2 = get8<TY, 16>(A.b_post, 0, c, lo, A.width);
-    const bool over = A.dr && A.dr == A.dx;
+    const bool over = A.dx && A.dx == A.dr;
     const int64_t first = t0 / A.gate_rows;
     int64_t row = -1;
     auto flush = [&]() {
@@ -519,15 +520,17 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormArgs A)
         }
         if (A.y) y = get8<TY, 16>(A.y, t * A.ld_y, c, lo, A.width);
         if (A.dr) dr = get8<TX, 16>(A.dr, t * A.ld_dr, c, lo, A.width);
+        float dx[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float d = A.dr ? dr[i] : 0.0f;
             if (A.dn) {
                 const float g = dn[i], z = (res[i] - mu1) * rs1, q = A.w_pre ? g * w1[i] : g;
-                if (!over) d += rs1 * (q - z * mz - mq);
+                d += rs1 * (q - z * mz - mq);
                 s_w1[i] += g * z;
                 if (BIAS) s_b1[i] += g;
             }
+            dx[i] = d;
             if (!A.y) continue;
             const float z = (y[i] - mu2) * rs2, sd = A.scale * d;
             s_g[i] += sd * (z * (A.w_post ? w2[i] : 1.0f) + (BIAS && A.b_post ? b2[i] : 0.0f));
@@ -535,6 +538,7 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormArgs A)
             s_w2[i] += dv * z;
             if (BIAS) s_b2[i] += dv;
         }
+        if (over) put8<TX>(A.dx, t * A.ld_dx, c, lo, dx);
     }
     if (A.dgate && row >= 0) flush();
     const int64_t at = me * kNormSums * A.width;
