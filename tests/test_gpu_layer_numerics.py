@@ -54,3 +54,42 @@ def test_norm_backward_in_place_gives_the_same_bits(ops, T, D, rows, typ, kind):
     layer.arena_norm_backward(ops.ctx, d, g, torch.cuda.current_stream().cuda_stream)
     for k in got:
         assert torch.equal(got[k], want[k]), k
+
+
+@pytest.mark.parametrize("typ", [BF16, F16])
+@pytest.mark.parametrize("T", [1, 70])
+@pytest.mark.parametrize("act,low", [("gelu", -8.0), ("silu", -80.0)])
+def test_activations_far_below_zero(ops, act, low, T, typ):
+    """Gates of exact values down to `low`, where the activation is a small difference
+    or a small exponential.  One rounding of h (du, dg), and 2^-16 of the value for
+    the arithmetic: an exponent e carries e 2^-24 of rounding into it (46 and 80
+    at most, times two units), the functions a few units more."""
+    F = 128
+    z = torch.linspace(low, 2.0, F, device="cuda").to(typ)
+    x, wg, wu = torch.zeros(T, 8, dtype=typ, device="cuda"), *(torch.zeros(F, 8, dtype=typ, device="cuda") for _ in range(2))
+    x[:, 0], wg[:, 0], wu[:, 0] = 1.0, z, 1024.0       # g = z, u = 1024
+    wd = torch.zeros(8, F, dtype=typ, device="cuda")
+    y, saved = ops.ffn_forward(x, wg, wu, wd, activation=act, save=True)
+    h = saved.buffer[:2 * T * F].view(typ).view(T, F).double()
+    g = z.double()
+    if act == "gelu":
+        c, p = torch.erfc(-g / 2 ** 0.5) / 2, torch.exp(-g * g / 2) / (2 * torch.pi) ** 0.5
+        value, slope, size = g * c, c + g * p, c + g.abs() * p
+    else:
+        s = 1 / (1 + torch.exp(-g))
+        value, slope, size = g * s, s + g * s * (1 - s), s + g.abs() * s * (1 - s)
+    rounding = ref.U[typ] + 2.0 ** -16
+    off = (h - 1024 * value).abs() - 1024 * value.abs() * rounding - ref.TINY[typ]
+    assert off.max() <= 0, (g[off.amax(0).argmax()].item(), off.max().item())
+    # dh = 1 for every feature: the gradients of the weights are T times du and dg
+    wd[0] = 1.0
+    dy = torch.zeros(T, 8, dtype=typ, device="cuda")
+    dy[:, 0] = 1.0
+    grads = [torch.empty(w.shape, device="cuda") for w in (wg, wu, wd)]
+    ops.ffn_backward(dy, x, wg, wu, wd, saved, activation=act, grads=grads)
+    du, dg = grads[1][:, 0].double() / T, grads[0][:, 0].double() / T
+    rounding = ref.U[typ] + 2.0 ** -15                # and the sum over tokens
+    off = (du - value).abs() - value.abs() * rounding - ref.TINY[typ]
+    assert off.max() <= 0, (g[off.argmax()].item(), off.max().item())
+    off = (dg - 1024 * slope).abs() - 1024 * (ref.U[typ] * slope.abs() + 2.0 ** -15 * size) - ref.TINY[typ]
+    assert off.max() <= 0, (g[off.argmax()].item(), off.max().item())
