@@ -329,7 +329,9 @@ NormArgs norm_args(const arena_norm_desc* d)
     A.n = d->n; A.ld_n = d->ld_n;
     A.stats = d->stats;
     A.tokens = d->tokens;
-    A.gate_rows = d->gate_rows > 0 ? d->gate_rows : std::max<int64_t>(1, d->tokens);
+    // a gate row of more tokens than there are is one of all of them
+    const int64_t all = std::max<int64_t>(1, d->tokens);
+    A.gate_rows = d->gate_rows > 0 ? std::min(d->gate_rows, all) : all;
     A.width = d->width;
     A.layer = d->kind == ARENA_NORM_LAYER;
     A.eps = d->eps;

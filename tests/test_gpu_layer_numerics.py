@@ -93,3 +93,21 @@ def test_activations_far_below_zero(ops, act, low, T, typ):
     assert off.max() <= 0, (g[off.argmax()].item(), off.max().item())
     off = (dg - 1024 * slope).abs() - 1024 * (ref.U[typ] * slope.abs() + 2.0 ** -15 * size) - ref.TINY[typ]
     assert off.max() <= 0, (g[off.argmax()].item(), off.max().item())
+
+
+@pytest.mark.parametrize("gate_rows", [40, 41, 1 << 40, (1 << 63) - 40, (1 << 63) - 1])
+def test_gate_rows_past_the_tokens_are_one_row(ops, gate_rows):
+    """However many tokens a gate row would take, up to the largest number that the
+    descriptor holds: its gradient is the sum over all that there are."""
+    T, D = 40, 64
+    x, y, dr = normal((T, D), F32, 1), normal((T, D), BF16, 2), normal((T, D), F32, 3)
+    gate = normal((1, D), BF16, 4, 0.3, 0.5)
+    r, _, stats = ops.norm_forward(x, y, gate=gate, save=True)
+    r2, _, _ = ops.norm_forward(x, y, gate=gate, gate_rows=gate_rows, save=True)
+    assert torch.equal(r, r2)
+    want = ops.norm_backward(None, dr, r, y, stats, gate=gate)
+    junk = torch.full((4096,), float("nan"), device="cuda")       # what a gradient left out would hold
+    del junk
+    got = ops.norm_backward(None, dr, r, y, stats, gate=gate, gate_rows=gate_rows)
+    for k in ("dx", "dy", "dgate"):
+        assert torch.equal(got[k], want[k]), k
