@@ -166,7 +166,9 @@ arena_status arena_ffn_backward(arena_ctx* ctx, const arena_ffn_desc* f, const a
  *   X = U / (|U|_F + eps);  `steps` times  X <- a X + (b A + c A^2) X, A = X X^T
  *   out = scale X
  * with (a, b, c) = coefficients[step].  A is formed on the smaller side.  The
- * products' operands are float16 scaled by 2^12; polynomials whose iterates can
+ * products' operands are float16 scaled by 2^12, whatever the gradient's type; what
+ * rounding takes off X goes along beside it (but for the last two steps), as its
+ * share on small singular values would grow by `a` a step.  Polynomials whose iterates can
  * leave the magnitudes that holds (15, starting from singular values of at most
  * 1) are refused as UNSUPPORTED.  Out of bfloat16 or float16 type
  * (a float16 out overflows past 65504, as any conversion). */

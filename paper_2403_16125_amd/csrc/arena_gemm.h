@@ -345,6 +345,36 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
     else put((E*)c + at, v, left);
 }
 
+// Plain, with the part of the added matrix that its 16 bits left out: the next step's
+// product takes C in 16 bits, and the rest goes on beside it.
+template <typename T>
+struct Side<T, kPlainRest> : Side<T, kPlain> {
+    u32x4 rest;
+    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
+    {
+        Side<T, kPlain>::load(A, z, m, n);
+        rest = *(const u32x4*)((const typename T::E*)A.rest + z * A.se + (int64_t)m * A.lde + n);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[8],
+                                          const Side<T, kPlainRest>& side)
+{
+    typedef typename T::E E;
+    E w[8], c[8];
+    __builtin_memcpy(w, &side.rest, sizeof(w));
+    const int64_t at = z * A.sc + (int64_t)m * A.ldc + n;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        v[r] = A.alpha * v[r] + A.beta * side.get(r, false) + A.rest_in * (float)w[r];
+        c[r] = (E)v[r];
+        w[r] = (E)((v[r] - (float)c[r]) * 2048.0f);
+    }
+    __builtin_memcpy((E*)A.c[0] + at, c, sizeof(c));
+    if (A.rest_out) __builtin_memcpy((E*)A.rest + at, w, sizeof(w));
+}
+
 // Values kept for the backward pass: the upper 24 bits of a float, 16 in a row
 // of heads and 8 in a row of tails (all rows of heads, then all of tails).  In
 // 16 bits they would cost the gradients two more roundings of the operands'
@@ -992,8 +1022,8 @@ hipError_t launch_gemm_t(const GemmArgs& A, Product what, const Cut& cut, hipStr
     case kColsCols: return launch_layout<T, true, true, kPlain>(A, cut, s);
     case kGateUp: return launch_layout<T, false, false, kGatedFwd>(A, cut, s);
     case kGateUpBack: return launch_layout<T, false, true, kGatedBwd>(A, cut, s);
+    default: return hipErrorInvalidValue;
     }
-    return hipErrorInvalidValue;
 }
 
 template <typename T>

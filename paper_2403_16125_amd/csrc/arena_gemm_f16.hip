@@ -6,6 +6,8 @@ namespace mm {
 
 hipError_t launch_gemm_f16(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
 {
+    if (what == kRowsRowsRest) return launch_layout<F16, false, false, kPlainRest>(A, cut, s);
+    if (what == kRowsColsRest) return launch_layout<F16, false, true, kPlainRest>(A, cut, s);
     return launch_gemm_t<F16>(A, what, cut, s);
 }
 

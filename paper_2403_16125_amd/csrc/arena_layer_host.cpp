@@ -571,12 +571,15 @@ arena_status check_update(arena_ctx* c, const char* who, const arena_update_desc
     return ARENA_OK;
 }
 
+// Whether step i adds what rounding took off its X: all but the last two do.
+bool keeps_rest(const arena_update_desc* d, int i) { return i + 2 < d->steps; }
+
 struct UpdatePlan {
     Pieces w;
     int64_t rows, cols, side;       // padded to multiples of 8
     bool tall;                      // more rows than columns: the Gram matrix is X^T X
     int blocks;
-    void *x[2], *gram, *poly, *sums, *part;
+    void *x[2], *rest, *gram, *poly, *sums, *part;
     Cut cut_gram, cut_square, cut_x;
     bool sym_gram, sym_square;
 
@@ -590,6 +593,7 @@ struct UpdatePlan {
         const int64_t values = (int64_t)d->rows * pad8(d->cols) / 8;
         blocks = (int)std::max<int64_t>(1, std::min<int64_t>(arena::kUpdateBlocks, ceil_div(values, 1024)));
         for (void*& p : x) p = w.take(2 * n * rows * cols);
+        rest = w.take(keeps_rest(d, 0) ? 2 * n * rows * cols : 0);
         gram = w.take(2 * n * side * side);
         poly = w.take(2 * n * side * side);
         sums = w.take(8 * n * blocks);
@@ -852,6 +856,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
     U.nesterov = d->nesterov != 0;
     U.mu = d->mu; U.eps = d->eps;
     U.x = P.x[0];
+    U.rest = keeps_rest(d, 0) ? P.rest : nullptr;
     U.rows_p = (int)P.rows; U.ld_x = (int)P.cols;
     U.part = (double*)P.sums;
     U.blocks = P.blocks;
@@ -903,6 +908,14 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
         X.e[0] = x; X.lde = P.cols; X.se = sx;
         X.alpha = inv;
         X.beta = k ? (float)(k[0] + kCentre * k[1] + kCentre * kCentre * k[2]) : 1.0f;
+        arena::mm::Product what = P.tall ? arena::mm::kRowsRows : arena::mm::kRowsCols;
+        if (keeps_rest(d, i)) {
+            what = P.tall ? arena::mm::kRowsRowsRest : arena::mm::kRowsColsRest;
+            X.rest = P.rest;
+            X.rest_in = k[0] * (1.0f / 2048.0f);
+            X.rest_out = keeps_rest(d, i + 1);
+            X.pad = X.N;
+        }
         if (last) {
             X.alpha *= d->scale * inv;
             X.beta *= d->scale * inv;
@@ -911,7 +924,7 @@ arena_status arena_orthogonal_update(arena_ctx* c, const arena_update_desc* d, v
         } else {
             X.c[0] = P.x[at ^ 1]; X.ldc = P.cols; X.sc = sx;
         }
-        if ((e = run(X, P.cut_x, false, P.tall ? arena::mm::kRowsRows : arena::mm::kRowsCols)))
+        if ((e = run(X, P.cut_x, false, what)))
             return hip_error(c, e, "update product launch");
         at ^= 1;
     }

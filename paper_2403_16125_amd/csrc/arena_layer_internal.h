@@ -19,7 +19,7 @@ namespace mm {
 constexpr int kBK = 64;                 // k per step
 constexpr int kMaxLd = 1 << 22;         // row stride limit, elements: 256 rows stay within 32-bit byte offsets
 
-enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2 };
+enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2, kPlainRest = 3 };
 enum Out { kOut16 = 0, kOutF32 = 1, kOutBf16 = 2 };   // the operands' own type, float, bf16
 enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
 
@@ -45,6 +45,12 @@ struct GemmArgs {
     int64_t lde, se;
     float alpha, beta, diag;
     int32_t out;
+    // plain with a rest: what rounding took off e, times 2^11, laid out as e and C;
+    // `rest_in` times it is added, and with rest_out C's own takes its place.  C is of
+    // the operands' type, N a multiple of 8 and pad = N
+    void* rest;
+    float rest_in;
+    int32_t rest_out;
     // gated, forward: c[0] = act(g) u, and g, u unless null; backward: c[0] and
     // c[1] the gradients of g and u.  Rows of ldc elements (c) and ldg values of
     // 24 bits (g, u: M rows of 16-bit heads, then M rows of 8-bit tails);
@@ -59,8 +65,8 @@ struct GemmArgs {
 };
 
 // Products by the layouts of their operands (rows: k contiguous; cols: m or n
-// contiguous) and epilogue.
-enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack };
+// contiguous) and epilogue; those with a rest in float16 only.
+enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack, kRowsRowsRest, kRowsColsRest };
 
 // Tiles: 256 x 256 (8 waves, two buffers, one block on a compute unit), 128 x 128
 // (4 waves) with two buffers (two blocks) or four (one block), 64 x 64 (4 waves,
@@ -146,6 +152,7 @@ struct UpdateArgs {
     int32_t rows, cols, batch, nesterov;
     float mu, eps;
     void* x;                      // float16 [batch][rows_p][ld_x], zero past rows and cols
+    void* rest;                   // nullable: 2^11 times what rounding took off x, laid out as x
     int32_t rows_p, ld_x;
     double* part;                 // [batch][blocks] sums of squares
     int32_t blocks;

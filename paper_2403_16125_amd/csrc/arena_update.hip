@@ -14,6 +14,15 @@
 // the small entries of X, X X^T and its polynomial out of float16's subnormals
 // (magnitudes up to 15 are representable, which the host checks for the
 // polynomial).
+//
+// What falls on small singular values grows by `a` in each step, the rounding of X
+// with it, and a spectrum that decays leaves little beside it: with singular values
+// of i^-2 (512 x 768, five steps of the usual polynomial) the result was off by 2.1e-2.  So
+// what rounding takes off X is kept too (11 more bits, times 2^11), and the next step
+// adds `a` times it, to first order what the polynomial makes of it there: 2.2e-3.
+// The last two steps do without: little growth is left, and where singular values
+// are large the polynomial makes less of it than a.  Costs 2 to 5 % of an update (10944
+// x 4096: 3255 -> 3350 us).
 #include "arena_layer_internal.h"
 
 namespace arena {
@@ -104,10 +113,16 @@ __global__ __launch_bounds__(256) void update_scale_kernel(const UpdateArgs A)
 #pragma unroll
             for (int q = 0; q < 8; ++q) g[q] = A.nesterov ? g[q] + A.mu * m[q] : m[q];
         }
-        _Float16 h[8];
+        const int64_t at = (z * (int64_t)A.rows_p + r) * A.ld_x + c;
+        _Float16 h[8], rest[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) h[q] = q < left ? (_Float16)(float)(g[q] * scale) : (_Float16)0.0f;
-        __builtin_memcpy((_Float16*)A.x + (z * (int64_t)A.rows_p + r) * A.ld_x + c, h, sizeof(h));
+        for (int q = 0; q < 8; ++q) {
+            const float v = q < left ? (float)(g[q] * scale) : 0.0f;
+            h[q] = (_Float16)v;
+            rest[q] = (_Float16)((v - (float)h[q]) * 2048.0f);
+        }
+        __builtin_memcpy((_Float16*)A.x + at, h, sizeof(h));
+        if (A.rest) __builtin_memcpy((_Float16*)A.rest + at, rest, sizeof(rest));
     }
 }
 

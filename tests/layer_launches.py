@@ -47,6 +47,7 @@ SHAPES = [
     ("update", 0, 8, 1398, 1348), ("update", 0, 8, 1728, 1280), ("update", 0, 8, 2000, 2000),
     ("update", 0, 8, 2019, 475), ("update", 0, 8, 2480, 1971), ("update", 0, 8, 4792, 974),
     ("update", 0, 8, 6583, 2164), ("update", 0, 8, 8201, 2019), ("update", 0, 8, 9442, 1432),
+    ("update", 0, 1, 64, 64), ("update", 0, 8, 2022, 81), ("update", 0, 1, 4655, 451), ("update", 0, 3, 333, 2909),
 ]
 
 PROGRAM = r"""
@@ -60,7 +61,7 @@ const char* hipGetErrorString(hipError_t) { return ""; }
 static int at;
 static void say(const char* fn, const GemmArgs& A, int dtype, int what, const Cut& c, bool second)
 {
-    static const char* const products[] = {"rows rows", "rows cols", "cols cols", "gate up", "gate up back"};
+    static const char* const products[] = {"rows rows", "rows cols", "cols cols", "gate up", "gate up back", "rows rows rest", "rows cols rest"};
     static const char* const kinds[] = {"256", "128", "128 deep", "64"};
     const bool sym = A.sym, dual = what == kGateUp;
     const int64_t side = kTileSide[c.main], tm = (A.M + side - 1) / side, cols = dual ? side / 2 : side;
@@ -133,9 +134,9 @@ int main()
         } else {
             arena_update_desc d;
             memset(&d, 0, sizeof(d));
-            const float k[3] = {1.5f, -0.5f, 0.0f};
+            const float k[9] = {1.5f, -0.5f, 0.0f, 1.5f, -0.5f, 0.0f, 1.5f, -0.5f, 0.0f};
             if (scanf("%d %d %d %d", &d.dtype, &d.batch, &d.rows, &d.cols) != 4) return 1;
-            d.out_dtype = ARENA_BF16; d.steps = 1; d.eps = 1e-7f; d.scale = 1.0f;
+            d.out_dtype = ARENA_BF16; d.steps = 3; d.eps = 1e-7f; d.scale = 1.0f;
             d.coefficients = k;
             d.grad = d.out = p;
             d.ld_grad = d.ld_out = d.cols;
@@ -164,7 +165,8 @@ def build(folder):
 def launches(exe, shapes):
     """One dict a product, in order.  shapes: ("ffn", dtype, act, tokens, model, inner,
     gradients' dtype, accumulate) or ("update", dtype, batch, rows, cols), in the ABI's
-    codes; "shape" in a dict is the index into them."""
+    codes; "shape" in a dict is the index into them.  Updates are of three steps: the
+    first hands on what its 16 bits leave out, the last writes the result."""
     text = "\n".join(" ".join(str(int(v)) if not isinstance(v, str) else v for v in s) for s in shapes)
     done = subprocess.run([exe], input=text, capture_output=True, text=True, check=True)
     return [json.loads(line) for line in done.stdout.splitlines()]

@@ -111,3 +111,39 @@ def test_gate_rows_past_the_tokens_are_one_row(ops, gate_rows):
     got = ops.norm_backward(None, dr, r, y, stats, gate=gate, gate_rows=gate_rows)
     for k in ("dx", "dy", "dgate"):
         assert torch.equal(got[k], want[k]), k
+
+
+def spectrum(rows, cols, power, seed=1):
+    """A matrix of singular values i^-power (on the CPU, in 64 bits)."""
+    gen = torch.Generator().manual_seed(seed)
+    n = min(rows, cols)
+    left = torch.linalg.qr(torch.randn(rows, n, generator=gen, dtype=torch.float64))[0]
+    right = torch.linalg.qr(torch.randn(cols, n, generator=gen, dtype=torch.float64))[0]
+    return (left * torch.arange(1, n + 1, dtype=torch.float64) ** -power) @ right.T
+
+
+@pytest.mark.parametrize("rows,cols", [(512, 768), (768, 512), (100, 90), (1100, 1300)])
+@pytest.mark.parametrize("power", [0.0, 1.0, 1.5, 2.0, 3.0])
+def test_update_of_decaying_spectra(ops, rows, cols, power):
+    """What falls on small singular values grows by 3.4445 a step, and no rounding of
+    X may grow with it for long.  5e-3 of the result's norm, in the mean square: X of
+    the fourth step in 11 bits (2^-11 / sqrt 3 of a norm no larger than the result's,
+    grown by 3.4445^2: 3.4e-3), of the fifth (1.0e-3), three more roundings of that
+    size, and the result's own (1.7e-3)."""
+    u = spectrum(rows, cols, power).float().cuda()
+    got = ops.orthogonal_update(u)
+    want = ref.orthogonal(u, layer.COEFFICIENTS, 5, 1e-7, 1.0)
+    assert (got.double() - want).norm() <= 5e-3 * want.norm()
+
+
+def test_update_of_decaying_spectra_in_batches_and_types(ops):
+    """The same of matrices side by side, with momentum, to float16; and of gradients
+    in 16 bits, whose own rounding the reference shares."""
+    u = torch.stack([spectrum(200, 136, 2.0, seed) * 10.0 ** -seed for seed in range(3)]).float().cuda()
+    for typ in (F32, BF16, F16):
+        grad = u.to(typ)
+        m = torch.zeros_like(u)
+        got = ops.orthogonal_update(grad, momentum=m, dtype=F16)
+        for g, v in zip(got, grad):
+            want = ref.orthogonal(v.double() * 1.95, layer.COEFFICIENTS, 5, 1e-7, 1.0)
+            assert (g.double() - want).norm() <= 5e-3 * want.norm()

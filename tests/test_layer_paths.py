@@ -35,6 +35,9 @@ def test_checked_shapes_take_every_kind_of_tile(program):
         for typ in (1, 2):
             for tile in ("256", "128", "128 deep", "64"):
                 assert any(p[:2] == (product, typ) and tile in p[2:3] for p in taken), (product, typ, tile)
+    for product in ("rows rows rest", "rows cols rest"):
+        for tile in ("256", "128", "128 deep", "64"):
+            assert any(p[:3] == (product, 2, tile) for p in taken), (product, tile)
     for tile in ("256", "128", "128 deep", "64"):
         assert any(p[2] == tile and "mirrored" in p and "split" not in p for p in taken), tile
     assert any("after whole rounds" in p and "smaller tiles" in p and "split" in p and "mirrored" in p for p in taken)
