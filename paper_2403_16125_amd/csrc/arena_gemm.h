@@ -375,8 +375,9 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
     if (A.rest_out) __builtin_memcpy((E*)A.rest + at, w, sizeof(w));
 }
 
-// Values kept for the backward pass: the upper 24 bits of a float, 16 in a row
-// of heads and 8 in a row of tails (all rows of heads, then all of tails).  In
+// Values kept for the backward pass: floats rounded to their upper 24 bits (to
+// nearest, ties to even), 16 in a row of heads and 8 in a row of tails (all rows of
+// heads, then all of tails).  In
 // 16 bits they would cost the gradients two more roundings of the operands'
 // size (1.8 times the error of one rounding of the result instead of 1.4); the
 // tails are a sixth of the bytes that the pass writes here.
@@ -388,7 +389,9 @@ __device__ __forceinline__ void put24(void* p, const GemmArgs& A, int m, int n, 
     uint8_t tail[C];
 #pragma unroll
     for (int r = 0; r < C; ++r) {
-        const uint32_t b = __float_as_uint(v[r]);
+        // a NaN of operands of 16 bits has nothing in the lower 8 that could carry
+        uint32_t b = __float_as_uint(v[r]);
+        b += 127 + (b >> 8 & 1);
         head[r] = (uint16_t)(b >> 16);
         tail[r] = (uint8_t)(b >> 8);
     }

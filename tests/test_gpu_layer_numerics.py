@@ -147,3 +147,25 @@ def test_update_of_decaying_spectra_in_batches_and_types(ops):
         for g, v in zip(got, grad):
             want = ref.orthogonal(v.double() * 1.95, layer.COEFFICIENTS, 5, 1e-7, 1.0)
             assert (g.double() - want).norm() <= 5e-3 * want.norm()
+
+
+@pytest.mark.parametrize("T,D,F", [(5, 8, 264), (150, 8, 264), (150, 2048, 264), (4100, 8, 2000)])
+def test_kept_values_are_rounded_to_nearest(ops, T, D, F):
+    """g and u of one product each: 22 bits of two float16 factors, kept in 16 of 24
+    bits, so off by half a unit of them, 2^-16, and by as much up as down.  Shapes
+    of the kernel for few tokens, of one tile and of split and large products."""
+    x, wg, wu = torch.zeros(T, D, dtype=F16, device="cuda"), *(torch.zeros(F, D, dtype=F16, device="cuda") for _ in range(2))
+    x[:, 0], wg[:, 0], wu[:, 0] = normal((T,), F16, 1, 0.1, 1.0), normal((F,), F16, 2), normal((F,), F16, 3)
+    wd = torch.zeros(D, F, dtype=F16, device="cuda")
+    _, saved = ops.ffn_forward(x, wg, wu, wd, save=True)
+    _, at_g, at_u, _ = saved.parts()
+    n = T * saved.ld
+    for at, w in ((at_g, wg), (at_u, wu)):
+        head = saved.buffer[at:at + 2 * n].view(torch.int16).view(T, saved.ld).int()
+        tail = saved.buffer[at + 2 * n:at + 3 * n].view(T, saved.ld).int()
+        kept = ((head << 16) | (tail << 8)).view(F32)[:, :F].double()
+        want = x[:, :1].double() * w[:, 0].double()
+        off = (kept - want) / want.abs().clamp_min(1e-30)
+        assert off.abs().max() <= 2.0 ** -16
+        # mean of T F independent errors of at most 2^-16: six deviations
+        assert (off * want.sign()).mean().abs() <= 6 * 2.0 ** -16 / (3 * T * F) ** 0.5
