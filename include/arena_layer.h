@@ -68,7 +68,8 @@ extern "C" {
  * stream after it and n the input of the next block.  y NULL: no block before
  * (r = x, not written).  n NULL: no block after.  The weights, biases and the gate
  * are optional (1, 0, 1).  Gate rows: row t / gate_rows scales token t;
- * gate_rows 0 is one row for all tokens.  n is formed from r in 32 bits, before r is rounded. */
+ * gate_rows 0 is one row for all tokens.  n is formed from r in 32 bits, before r is rounded;
+ * the backward pass starts from r as it is stored, so a 16-bit stream costs it that rounding. */
 typedef struct arena_norm_desc {
     int32_t dtype;            /* of y, n, gate, weights, biases: ARENA_F32, BF16 or F16 */
     int32_t stream_dtype;     /* of x and r: dtype or ARENA_F32 */
@@ -120,7 +121,10 @@ arena_status arena_norm_backward(arena_ctx* ctx, const arena_norm_desc* f, const
  * pass, take 3 tokens ld_inner bytes each (rows of 16-bit heads, then rows of
  * 8-bit tails).  All three are 16-byte aligned, ld_inner is a multiple of 8 and
  * at least `inner`; columns past `inner` up to the next multiple of 8 are
- * written as zeros.  g and u NULL (both): not kept, as where no backward pass follows.  Any alignment and stride of x, y and the
+ * written as zeros.  g and u NULL (both): not kept, as where no backward pass follows.
+ * h, and the gradients of g and u that the backward pass forms, are rounded to dtype as
+ * the next products' operands: in float16 an h past 65504 is infinite and gradients below
+ * 6e-5 lose bits, whatever the type of the weights' gradients.  Any alignment and stride of x, y and the
  * weights; 16-byte aligned ones with widths and strides of multiples of 8 are
  * read in place, others are copied to the workspace first. */
 typedef struct arena_ffn_desc {

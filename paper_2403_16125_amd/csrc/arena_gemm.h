@@ -20,9 +20,10 @@
 // through LDS.
 //
 // Large products are bound by the matrix cores and the clock that the power
-// leaves them (60 to 66 % of the compute units' cycles issue products, LDS is
-// busy for 25 %), and by each tile's start and end, since one block of 256 x 256
-// fits a compute unit.  8192 x 4096 x 10944 in bfloat16: 585 to 600 us (1220 to
+// leaves them (the plain ones issue products in 59 to 66 % of the compute units'
+// cycles, those with gated epilogues in 49 to 57 %, the mirrored ones of an update
+// in 51 to 55 %; LDS is busy for 20 to 34 %), and by each tile's start and end, since one
+// block of 256 x 256 fits a compute unit.  8192 x 4096 x 10944 in bfloat16: 585 to 600 us (1220 to
 // 1250 TFLOP/s), with two segments of k 1090 to 1110 us (1320 to 1350), with the
 // gated forward epilogue on twice the columns 1230 to 1270 us (1160 to 1190), as
 // a weight gradient 626 to 660 us.  Small ones are bound by latency: a block of
@@ -521,7 +522,7 @@ struct Int {
 };
 
 // Waits until at most N of the wave's global loads are in flight, and for all
-// of its LDS reads.
+// of its LDS reads.  (The compiler adds waits of its own, see Buffers.)
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -529,8 +530,10 @@ __device__ __forceinline__ void wait_loads()
     __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);
 }
 
-// The LDS buffers of a block: separate arrays, so that a fragment read is known
-// not to meet the loads in flight.
+// The LDS buffers of a block: separate arrays, so that a fragment read can be told
+// from the loads in flight.  Of two buffers the compiler does; of four, where it
+// meets eight arrays, it waits for all loads before the reads of three steps in four:
+// what is loaded two and three steps ahead is then only started earlier.
 struct Buffers {
     char *a0, *a1, *b0, *b1, *a2, *a3, *b2, *b3;
 };
@@ -654,7 +657,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
         }
     };
     // One step, from buffer u.  At its barrier this step's loads have landed
-    // (those of later steps are in flight) and every wave holds its
+    // (those of later steps may be in flight) and every wave holds its
     // fragments of the step before, so that one's buffer is free: the loads
     // kStages - 1 steps ahead start, and the second half of the step before is
     // multiplied while this step's first fragments are read.

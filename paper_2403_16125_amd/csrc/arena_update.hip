@@ -5,8 +5,8 @@
 // The norm has to be known before X0 can be rounded, so U is formed twice: by
 // the sum of squares (which stores M') and by the scaling.  Both are bound by
 // memory, and small beside the products that follow: 10944 x 4096 in float32 with
-// momentum 112 us (538 MB, 4.8 TB/s) and 77 us (448 MB, 5.8 TB/s, part of it from
-// the cache) of 3200.
+// momentum 113 us (538 MB, 4.8 TB/s) and 90 us (538 MB, 6.0 TB/s, part of it from
+// the cache) of 3300.
 //
 // X0 is held in float16 times 2^12.  Its entries are at most 1 in magnitude
 // and about 1 / sqrt(rows cols) in size, and the products' operands keep 11
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void update_sum_kernel(const UpdateArgs A)
     if (threadIdx.x == 0) A.part[z * A.blocks + blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// X0 = 2^12 U / (|U| + eps), zero in the padding.
+// X0 = 2^12 U / (|U| + eps), and what its rounding leaves; zero in the padding.
 template <typename E>
 __global__ __launch_bounds__(256) void update_scale_kernel(const UpdateArgs A)
 {

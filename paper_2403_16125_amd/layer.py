@@ -333,7 +333,8 @@ class LayerOps:
     def norm_backward(self, dn, dr, r, y, stats, *, gate=None, gate_rows=0, scale=1.0, w_post=None, b_post=None,
                       w_pre=None, b_pre=None, kind="rms", eps=1e-6, stream=None):
         """Gradients from dn and dr, those of n and r (either may be None), with
-        the forward's r, y (None: no block before), stats and parameters.
+        the forward's r as it is stored (a float32 stream loses nothing there), y
+        (None: no block before), stats and parameters.
         Returns a dict of dx, dy, dgate, dw_post, db_post, dw_pre and db_pre,
         None where there is no such input."""
         return self._run(stream, (dn, dr, r, y, stats, gate, w_post, b_post, w_pre, b_pre), self._norm_backward, dn, dr, r,
