@@ -15,7 +15,12 @@ SOURCES = [os.path.join(CSRC, "arena_host.cpp"), os.path.join(CSRC, "arena_kerne
            # layer operators (include/arena_layer.h)
            os.path.join(CSRC, "arena_layer_host.cpp"), os.path.join(CSRC, "arena_gemm_bf16.hip"),
            os.path.join(CSRC, "arena_gemm_f16.hip"), os.path.join(CSRC, "arena_norm.hip"),
-           os.path.join(CSRC, "arena_update.hip")]
+           os.path.join(CSRC, "arena_update.hip"),
+           # layers of experts and the vocabulary's loss (include/arena_experts.h, include/arena_loss.h)
+           os.path.join(CSRC, "arena_experts_host.cpp"), os.path.join(CSRC, "arena_groups_bf16.hip"),
+           os.path.join(CSRC, "arena_groups_f16.hip"), os.path.join(CSRC, "arena_route.hip"),
+           os.path.join(CSRC, "arena_loss_host.cpp"), os.path.join(CSRC, "arena_loss_bf16.hip"),
+           os.path.join(CSRC, "arena_loss_f16.hip"), os.path.join(CSRC, "arena_loss.hip")]
 
 VALU_RATE_SRC = os.path.join(CSRC, "valu_rate.hip")
 VALU_RATE_OUT = os.path.join(PKG, "_build", "libvalu_rate.so")   # fp64-vs-fp32 issue-rate microbenchmark

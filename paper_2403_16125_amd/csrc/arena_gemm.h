@@ -40,6 +40,7 @@
 namespace arena {
 namespace mm {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -208,12 +209,15 @@ struct Frags {
     }
 };
 
-template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool ATR_, bool BTR_, int EPI_>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool ATR_, bool BTR_, int EPI_,
+          int GROUP_ = kNoGroups>
 struct Tile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
-    static constexpr int EPI = EPI_;
+    static constexpr int EPI = EPI_, GROUP = GROUP_;
+    // of columns past N, the gated epilogues and the logits' gradient write zeros up to pad
+    static constexpr bool kUpToN = EPI_ == kPlain || EPI_ == kWide;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int kStages = STAGES_;
     // With few blocks on a compute unit a wave that issues its loads in a row
@@ -321,6 +325,90 @@ struct Side<T, kGatedBwd> {
         return __uint_as_float(h << 16 | t << 8);
     }
 };
+
+// wide: as plain, the added matrix of a type of its own and of a group.
+template <typename T>
+struct Side<T, kWide> {
+    u32x4 raw[2];
+    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
+    {
+        if (A.beta == 0.0f) return;
+        const char* p = (const char*)A.e[A.pairs ? z & 1 : 0];
+        const int64_t from = (z >> A.pairs) * A.se + (int64_t)m * A.lde + n;
+        const int left = A.N - n;
+        if (A.e_f32) {
+            const uint32_t* q = (const uint32_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 32);
+            else
+#pragma unroll
+                for (int r = 0; r < 8; ++r) raw[r >> 2][r & 3] = r < left ? q[r] : 0;
+        } else {
+            const uint16_t* q = (const uint16_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 16);
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    raw[0][r] = (2 * r < left ? q[2 * r] : 0) | (2 * r + 1 < left ? (uint32_t)q[2 * r + 1] << 16 : 0);
+        }
+    }
+    __device__ __forceinline__ float get(int r, bool f32) const
+    {
+        typedef typename T::E E;
+        if (f32) return __uint_as_float(raw[r >> 2][r & 3]);
+        const uint16_t h = (uint16_t)(raw[0][r >> 1] >> (16 * (r & 1)));
+        E e;
+        __builtin_memcpy(&e, &h, 2);
+        return (float)e;
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[8],
+                                          const Side<T, kWide>& side)
+{
+    typedef typename T::E E;
+    const int left = A.N - n;
+    const int64_t at = (z >> A.pairs) * A.sc + (int64_t)m * A.ldc + n;
+    void* c = A.c[A.pairs ? z & 1 : 0];
+    const float alpha = A.factor ? A.alpha * A.factor[0] : A.alpha;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] *= alpha;
+    if (A.beta != 0.0f)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] += A.beta * side.get(r, A.e_f32);
+    if (A.out == kOutF32) put((float*)c + at, v, left);
+    else put((E*)c + at, v, left);
+}
+
+template <typename T>
+struct Side<T, kLossStats> {
+    __device__ __forceinline__ void load(const GemmArgs&, int, int, int) {}
+};
+
+// logits' gradient: the row's record.
+template <typename T>
+struct Side<T, kLossGrad> {
+    u32x4 raw;
+    __device__ __forceinline__ void load(const GemmArgs& A, int, int m, int) { raw = *(const u32x4*)(A.rows + m); }
+};
+
+// factor (exp(l - lse) - [column is the target]), zero for tokens left out of the loss,
+// whatever their logits: rounded to 16 bits as the next two products' operand.
+template <typename T>
+__device__ __forceinline__ void loss_grad_out(const GemmArgs& A, int m, int n, const float (&v)[8],
+                                              const Side<T, kLossGrad>& side)
+{
+    typedef typename T::E E;
+    const float lse = __uint_as_float(side.raw[0]), factor = __uint_as_float(side.raw[1]);
+    const int target = (int)side.raw[2], at = target - A.first_col - n;
+    float g[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const float p = __expf(v[r] - lse) - (r == at ? 1.0f : 0.0f);
+        g[r] = n + r < A.N && target >= 0 ? factor * p : 0.0f;
+    }
+    put((E*)A.c[0] + (int64_t)m * A.ldc + n, g, 8);
+}
 
 // Writes eight (or, of few rows, four) columns from n, those below N, of row m;
 // z is the batch index.  Leaves the values written in v.
@@ -463,6 +551,7 @@ __device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, c
 // bands of 8 tile rows.
 struct Place {
     int m0, n0, z;
+    int m_end;           // rows of C past it are not this tile's
     bool mirror;         // symmetric and off the diagonal: the transposed tile is written too
 };
 
@@ -503,8 +592,72 @@ __device__ __forceinline__ bool place_of(const GemmArgs& A, int t, Place* at)
     tn = (tn << A.ratio) + (sub & ((1 << A.ratio) - 1));
     at->m0 = tm * P::BM;
     at->n0 = tn * P::kCols;
+    at->m_end = A.M;
     at->mirror = A.sym && tm != tn;
     return at->m0 < A.M && at->n0 < A.N && !(A.sym && tm < tn);
+}
+
+__device__ __forceinline__ int tile_of(int bid, int n_blocks);
+
+// Rows (steps) of group g, held inside 0 .. rows whatever the offsets are.
+__device__ __forceinline__ int group_end(const int32_t* offsets, int g, int rows)
+{
+    return min(max(offsets[g], 0), rows);
+}
+
+// Groups of rows: tiles of the groups in turn, of each in bands as above.  How many
+// there are only the device knows, so the launch has as many blocks as there can be, and
+// every wave finds its tile by itself: 64 groups at a time, their tile rows summed over
+// the lanes.  That is one read of the offsets on a block's way to its first load, less
+// than a launch that would lay out a table.
+template <typename P>
+__device__ __forceinline__ bool place_in_groups(const GemmArgs& A, int bid, Place* at)
+{
+    const int lane = threadIdx.x & 63;
+    auto rows_of = [&](int g, int* lo, int* hi) {
+        *lo = *hi = 0;
+        if (g < A.groups) {
+            *lo = group_end(A.offsets, g, A.M);
+            *hi = max(*lo, group_end(A.offsets, g + 1, A.M));
+        }
+        return (*hi - *lo + P::BM - 1) / P::BM;
+    };
+    auto sum_below = [&](int v) {      // inclusive over the lanes
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int w = __shfl_up(v, d, 64);
+            v += lane >= d ? w : 0;
+        }
+        return v;
+    };
+    // groups that overlap could have more tiles than the launch
+    int lo, hi, total = 0;
+    const int most = quotient((int)gridDim.x, A.tiles_n);
+    for (int g0 = 0; g0 < A.groups; g0 += 64)
+        total = min(most, total + __builtin_amdgcn_readlane(sum_below(rows_of(g0 + lane, &lo, &hi)), 63));
+    if (bid >= total * A.tiles_n) return false;
+    const int tile = tile_of(bid, total * A.tiles_n);
+    int before = 0;
+    for (int g0 = 0; g0 < A.groups; g0 += 64) {
+        const int mine = rows_of(g0 + lane, &lo, &hi), sum = sum_below(mine), all = __builtin_amdgcn_readlane(sum, 63);
+        if (tile >= (int64_t)(before + all) * A.tiles_n) {
+            before += all;
+            continue;
+        }
+        const uint64_t past = __ballot(tile < (int64_t)(before + sum) * A.tiles_n);
+        const int l = __ffsll((unsigned long long)past) - 1;
+        const int tiles_m = __builtin_amdgcn_readlane(mine, l);
+        const int in_group = tile - (before + __builtin_amdgcn_readlane(sum, l) - tiles_m) * A.tiles_n;
+        const int band = 8 * A.tiles_n, b = quotient(in_group, band), in = in_group - b * band;
+        const int rows = min(8, tiles_m - b * 8), tn = quotient(in, rows);
+        at->z = g0 + l;
+        at->m0 = __builtin_amdgcn_readlane(lo, l) + (b * 8 + in - tn * rows) * P::BM;
+        at->m_end = __builtin_amdgcn_readlane(hi, l);
+        at->n0 = tn * P::kCols;
+        at->mirror = false;
+        return true;
+    }
+    return false;
 }
 
 // Blocks go to the 8 XCDs in turn, so each XCD gets a run of consecutive tiles:
@@ -550,6 +703,74 @@ struct Buffers {
     __shared__ __attribute__((aligned(16))) char sb3_[kMoreB];                                             \
     const Buffers name = {sa0_, sa1_, sb0_, sb1_, sa2_, sa3_, sb2_, sb3_}
 
+// The statistics of a tile's logits, from the sums as they lie in registers: a lane holds
+// row lane & 15 and columns 4 (lane >> 4) + 0..3 of each fragment, so of a row the lane's
+// FN 4 values, then those of four lanes, then those of the block's WN waves meet.  A row's
+// exponentials are summed beside the largest logit of its columns here; the join brings
+// the tiles' to one.  No logit but the target's is written.
+template <typename P>
+__device__ __forceinline__ void loss_stats(const GemmArgs& A, const Place& at, f32x4 (&acc)[P::FM][P::FN],
+                                           const Buffers& lds, int wm, int wn)
+{
+    const int lane = threadIdx.x & 63;
+    const int n_lane = at.n0 + wn * (P::BN / P::WN) + 4 * (lane >> 4);
+    f32x2* const each = (f32x2*)lds.a0;                  // [BM][WN]
+    static_assert(P::BM * P::WN * 8 <= P::BM * 128, "statistics fit a buffer");
+    // loads into LDS may be in flight, of other waves too
+    asm volatile("" ::: "memory");
+    wait_loads<0>();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int r = wm * (P::BM / P::WM) + i * 16 + (lane & 15), m = at.m0 + r;
+        int64_t target = -1;
+        if (m < at.m_end)
+            target = (A.target_wide ? ((const int64_t*)A.target)[m] : ((const int32_t*)A.target)[m]) - A.first_col - n_lane;
+        float most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (n_lane + j * 16 + q < A.N) most = fmaxf(most, acc[i][j][q]);
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const float by = most == -INFINITY ? 0.0f : most;       // of nothing but -inf the sum is 0
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (n_lane + j * 16 + q < A.N) sum += __expf(acc[i][j][q] - by);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (target >= 0 && target < P::FN * 16 && (target & 12) == 0) {
+            float l = 0.0f;
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (target == j * 16 + q) l = acc[i][j][q];
+            A.picked[m] = l;
+        }
+        if (lane < 16) each[r * P::WN + wn] = f32x2{most, sum};
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < P::BM; r += P::kThreads) {
+        const int m = at.m0 + r;
+        if (m >= at.m_end) continue;
+        float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < P::WN; ++w) most = fmaxf(most, each[r * P::WN + w][0]);
+        const float by = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int w = 0; w < P::WN; ++w) {
+            const f32x2 e = each[r * P::WN + w];
+            sum += e[0] == -INFINITY ? e[1] : e[1] * __expf(e[0] - by);
+        }
+        ((f32x2*)A.stats)[(int64_t)(at.n0 / P::kCols) * A.M + m] = f32x2{most, sum};
+    }
+}
+
 // Tile t of a launch's n_tiles; part: which of the splits of k.
 template <typename P>
 __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, const int n_tiles, const int part,
@@ -563,12 +784,21 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
     Place at;
-    if (!place_of<P>(A, t, &at)) return;
-    const int zb = at.z, m0 = at.m0, n0 = at.n0;
+    if (P::GROUP == kRowGroups ? !place_in_groups<P>(A, t, &at) : !place_of<P>(A, t, &at)) return;
+    // zb: what the epilogue takes as the batch index
+    const int zb = P::GROUP == kRowGroups ? 0 : at.z, m0 = at.m0, n0 = at.n0, m_end = at.m_end;
+    int k_from = 0, K = A.K;
+    if (P::GROUP == kStepGroups) {
+        const int g = at.z >> A.pairs;
+        if (A.K > 0) {                // of no steps there need be no offsets
+            k_from = group_end(A.offsets, g, A.K);
+            K = max(0, group_end(A.offsets, g + 1, A.K) - k_from);
+        }
+    }
 
     Loader<P, P::BM, P::ATR, false> la;
     Loader<P, P::BN, P::BTR, P::DUAL> lb;
-    la.init(tid, m0, A.M, A.lda);
+    la.init(tid, m0, m_end, A.lda);
     lb.init(tid, n0, A.N, A.ldb);
     Frags<P, P::BM, P::ATR> fa;
     Frags<P, P::BN, P::BTR> fb;
@@ -581,22 +811,31 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
 #pragma unroll
         for (int j = 0; j < P::FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    const int sps = (A.K + kBK - 1) / kBK;     // steps of a segment
+    const int sps = (K + kBK - 1) / kBK;     // steps of a segment
     int s = 0, end = sps * A.nseg;
     if (A.splits > 1) {
-        s = part * A.per;
-        end = min(end, s + A.per);
+        const int per = P::GROUP == kStepGroups ? (end + A.splits - 1) / A.splits : A.per;
+        s = part * per;
+        end = min(end, s + per);
     }
-    const int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
-    const int sel = A.pairs ? zb : 0;
+    int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
+    int sel = A.pairs ? zb : 0;
+    if (P::GROUP == kRowGroups) {
+        za = 0;
+        zB = at.z * A.sb;
+    } else if (P::GROUP == kStepGroups) {
+        za = k_from * A.lda;
+        zB = k_from * A.ldb;
+        sel = A.pairs ? at.z & 1 : 0;
+    }
 
     auto where = [&](int step, const char** pa, const char** pb, const char** pb1, int* left) {
         int q = step, seg = sel;
         if (A.nseg == 2 && step >= sps) { q -= sps; seg = 1; }
         *pa = la.base(A.a[seg], za) + q * la.step;
         *pb = lb.base(A.b[seg], zB) + q * lb.step;
-        *pb1 = P::DUAL ? lb.base(A.b[1], 0) + q * lb.step : *pb;
-        *left = A.K - q * kBK;
+        *pb1 = P::DUAL ? lb.base(A.b[1], P::GROUP == kRowGroups ? zB : 0) + q * lb.step : *pb;
+        *left = K - q * kBK;
     };
     // The loads of a step, of both operands (which = 3) or one of them.  Woven
     // between products they may not branch, so every lane compares its k with
@@ -627,7 +866,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
             const int x = (at + q) * 64 + lane, m = mw + x / kChunks, n = nw + x % kChunks * 8;
-            if (m < A.M && n < (P::EPI == kPlain ? A.N : A.pad)) to[q].load(A, zb, m, n);
+            if (m < m_end && n < (P::kUpToN ? A.N : A.pad)) to[q].load(A, zb, m, n);
         }
     };
 
@@ -717,7 +956,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
             *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
         }
-        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) return;
+        if (m >= m_end || n >= (P::kUpToN ? A.N : A.pad)) return;
         if (A.splits > 1) {
             float* to = A.part + ((int64_t)part * n_tiles + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
             put(to, v, 8);
@@ -728,7 +967,9 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             gated_fwd_out<T>(A, m, n, v, u);
         } else if constexpr (P::EPI == kGatedBwd) {
             gated_bwd_out<T>(A, m, n, v, from);
-        } else {
+        } else if constexpr (P::EPI == kLossGrad) {
+            loss_grad_out<T>(A, m, n, v, from);
+        } else if constexpr (P::EPI != kLossStats) {
             plain_out<T>(A, zb, m, n, v, from);
             if (mirror) {
                 *piece(r, 2 * c) = *(f32x4*)v;
@@ -736,6 +977,10 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             }
         }
     };
+    if constexpr (P::EPI == kLossStats) {
+        loss_stats<P>(A, at, acc, lds, wm, wn);
+        return;
+    }
     // Loads into LDS may still be in flight here, and a wave's land in slices that
     // others write: each waits for its own before the barrier, which does not.
     asm volatile("" ::: "memory");
@@ -781,7 +1026,8 @@ template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
 {
     ARENA_TILE_BUFFERS(P, lds);
-    tile_product<P>(A, tile_of(blockIdx.x, gridDim.x), gridDim.x, blockIdx.y, lds);
+    // groups of rows: the block maps itself, over the tiles that there are
+    tile_product<P>(A, P::GROUP == kRowGroups ? blockIdx.x : tile_of(blockIdx.x, gridDim.x), gridDim.x, blockIdx.y, lds);
 }
 
 // Two independent products in one launch: blocks below n1 * A.splits belong to
@@ -825,7 +1071,7 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A, int n_tiles
         const float* p = part + (r0 + r) * P::kCols + c0 + c;
         float v[8] = {}, u[8] = {};
         Side<T, P::EPI> side;
-        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
+        if (m >= A.M || n >= (P::kUpToN ? A.N : A.pad)) continue;
         side.load(A, at.z, m, n);
 #pragma unroll 4
         for (int s = 0; s < A.splits; ++s) {
@@ -840,6 +1086,7 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A, int n_tiles
         }
         if constexpr (P::EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
         else if constexpr (P::EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v, side);
+        else if constexpr (P::EPI == kLossGrad) loss_grad_out<T>(A, m, n, v, side);
         else plain_out<T>(A, at.z, m, n, v, side);
         if (P::EPI == kPlain && at.mirror)
 #pragma unroll
@@ -961,9 +1208,13 @@ hipError_t launch_tile(const GemmArgs& A, int64_t n_tiles, hipStream_t s)
     gemm_kernel<P><<<dim3((unsigned)n_tiles, A.splits), P::kThreads, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
-    join_kernel<P><<<(unsigned)(n_tiles * kEach), 256, 0, s>>>(A, (int)n_tiles);
-    return hipGetLastError();
+    if constexpr (P::EPI == kLossStats || P::GROUP == kRowGroups) {
+        return hipErrorInvalidValue;          // never split
+    } else {
+        constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
+        join_kernel<P><<<(unsigned)(n_tiles * kEach), 256, 0, s>>>(A, (int)n_tiles);
+        return hipGetLastError();
+    }
 }
 
 template <typename T, bool ATR, bool BTR, int EPI>
@@ -1017,6 +1268,50 @@ hipError_t launch_pair_t(GemmArgs A, GemmArgs B, const Cut& cut, hipStream_t s)
     if (e != hipSuccess || A.splits == 1) return e;
     join_kernel<P><<<n1 * 4, 256, 0, s>>>(A, n1);
     return hipGetLastError();
+}
+
+// Products of groups, all of one kind of tile.  Of rows: as many blocks as there can be
+// tiles, each group's last one not full.
+template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
+hipError_t launch_groups_of(GemmArgs A, int kind, hipStream_t s)
+{
+    const int side = kTileSide[kind], cols = EPI == kGatedFwd ? side / 2 : side;
+    A.tiles_m = (A.M + side - 1) / side;
+    A.tiles_n = (A.N + cols - 1) / cols;
+    A.first = A.ratio = 0;
+    int64_t tiles = (int64_t)A.tiles_m * A.tiles_n * A.batch;
+    if (GROUP == kRowGroups) tiles = group_tiles(A.M, A.groups, side) * A.tiles_n;
+    switch (kind) {
+    case k256: return launch_tile<Tile<T, 256, 256, 2, 4, 2, ATR, BTR, EPI, GROUP>>(A, tiles, s);
+    case k128: return launch_tile<Tile<T, 128, 128, 2, 2, 2, ATR, BTR, EPI, GROUP>>(A, tiles, s);
+    case k64: return launch_tile<Tile<T, 64, 64, 2, 2, 4, ATR, BTR, EPI, GROUP>>(A, tiles, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
+{
+    switch (what) {
+    case kRowsRows: return launch_groups_of<T, false, false, kPlain, kRowGroups>(A, kind, s);
+    case kRowsCols: return launch_groups_of<T, false, true, kPlain, kRowGroups>(A, kind, s);
+    case kColsCols: return launch_groups_of<T, true, true, kWide, kStepGroups>(A, kind, s);
+    case kGateUp: return launch_groups_of<T, false, false, kGatedFwd, kRowGroups>(A, kind, s);
+    case kGateUpBack: return launch_groups_of<T, false, true, kGatedBwd, kRowGroups>(A, kind, s);
+    default: return hipErrorInvalidValue;
+    }
+}
+
+template <typename T>
+hipError_t launch_loss_t(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
+{
+    switch (what) {
+    case kLossLogits: return launch_layout<T, false, false, kLossStats>(A, cut, s);
+    case kLossGradient: return launch_layout<T, false, false, kLossGrad>(A, cut, s);
+    case kRowsCols: return launch_layout<T, false, true, kWide>(A, cut, s);
+    case kColsCols: return launch_layout<T, true, true, kWide>(A, cut, s);
+    default: return hipErrorInvalidValue;
+    }
 }
 
 template <typename T>

@@ -1,0 +1,13 @@
+// The experts' tiled products in float16.
+#include "arena_gemm.h"
+
+namespace arena {
+namespace mm {
+
+hipError_t launch_groups_f16(const GemmArgs& A, Product what, int kind, hipStream_t s)
+{
+    return launch_groups_t<F16>(A, what, kind, s);
+}
+
+}  // namespace mm
+}  // namespace arena

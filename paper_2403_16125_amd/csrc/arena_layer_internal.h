@@ -19,9 +19,19 @@ namespace mm {
 constexpr int kBK = 64;                 // k per step
 constexpr int kMaxLd = 1 << 22;         // row stride limit, elements: 256 rows stay within 32-bit byte offsets
 
-enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2, kPlainRest = 3 };
+enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2, kPlainRest = 3, kWide = 4, kLossStats = 5, kLossGrad = 6 };
 enum Out { kOut16 = 0, kOutF32 = 1, kOutBf16 = 2 };   // the operands' own type, float, bf16
 enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
+// Products whose rows or steps come in groups (experts) of lengths that only the
+// device knows: rows offsets[g] .. offsets[g + 1] - 1 of A and C meet matrix g of B, or
+// those steps of k of both operands make matrix g of C.
+enum Group { kNoGroups = 0, kRowGroups = 1, kStepGroups = 2 };
+
+// A token as the products of a loss's gradient read it.  target < 0: left out of the loss.
+struct LossRow {
+    float lse, factor;        // log sum exp of its logits; its gradient's factor
+    int32_t target, unused;
+};
 
 struct GemmArgs {
     // segments of k (nseg = 2: the second operand pair follows the first), or
@@ -62,11 +72,27 @@ struct GemmArgs {
     // a place of tile size for each block
     int32_t splits, per;
     float* part;
+    // groups: of rows, matrix g of b lies sb values on; of steps, matrix g of c (and e) sc
+    // (se).  With pairs = 1 every group's two products are neighbouring batch indices
+    const int32_t* offsets;   // [groups + 1], held inside 0 .. rows
+    int32_t groups;
+    // wide: C = alpha factor[0] product + beta e, e in 32 bits or in C's type
+    const float* factor;      // nullable
+    int32_t e_f32;
+    // loss: columns are entries first_col + n of the vocabulary.  Statistics: of each tile
+    // column and row the largest logit and the sum of exponentials beside it, at pair
+    // stats[column * M + row], and the logit of target[row]; gradient: c[0]
+    const LossRow* rows;
+    const void* target;
+    float* stats;
+    float* picked;            // [M]
+    int32_t first_col, target_wide;
 };
 
 // Products by the layouts of their operands (rows: k contiguous; cols: m or n
 // contiguous) and epilogue; those with a rest in float16 only.
-enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack, kRowsRowsRest, kRowsColsRest };
+enum Product { kRowsRows = 0, kRowsCols, kColsCols, kGateUp, kGateUpBack, kRowsRowsRest, kRowsColsRest,
+               kLossLogits, kLossGradient };
 
 // Tiles: 256 x 256 (8 waves, two buffers, one block on a compute unit), 128 x 128
 // (4 waves) with two buffers (two blocks) or four (one block), 64 x 64 (4 waves,
@@ -95,6 +121,21 @@ hipError_t launch_gemm(const GemmArgs& A, int dtype, Product what, const Cut& cu
 // layout cols x cols.
 hipError_t launch_pair(const GemmArgs& A, int dtype, Product what, const GemmArgs& B, const Cut& cut, hipStream_t s);
 
+// Most tiles of `side` rows that `groups` groups of M rows in all make.
+constexpr int64_t group_tiles(int64_t M, int64_t groups, int64_t side)
+{
+    return M / side + (groups < M ? groups : M);
+}
+
+// The products of experts: C of groups of rows (gate and up, down, and the gradients of
+// both operands' inner sides), C of groups of steps (the weights' gradients, wide).  One
+// kind of tile for the whole; splits of k with groups of steps only.
+hipError_t launch_groups(const GemmArgs& A, int dtype, Product what, int kind, hipStream_t s);
+
+// The products of a loss: the logits' statistics, their gradient (what: kLossLogits,
+// kLossGradient: one kind of tile), and the gradients of both operands (wide).
+hipError_t launch_loss(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s);
+
 constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel without LDS tiles takes
 
 // C = A B^T with both operands' k contiguous, M <= kSkinnyRows; dual: the gated
@@ -102,16 +143,96 @@ constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel wi
 hipError_t launch_skinny(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
 
 // Copies of matrices of 16-bit values, rows x cols, with zeros in columns cols ..
-// ld_to - 1; one launch.
+// ld_to - 1; one launch.  batch: so many matrices, `stride` values apart, copied one
+// behind the other.
 struct Pack {
     const void* from;
     void* to;
     int64_t ld_from, ld_to, rows, cols;
+    int64_t batch = 1, stride = 0;
 };
 constexpr int kMaxPacks = 5;
 hipError_t launch_packs(const Pack* packs, int n, hipStream_t s);
 
 }  // namespace mm
+
+// Loss: the passes beside the products.
+struct LossArgs {
+    int64_t tokens;
+    int32_t vocabulary, model;
+    const void* target;           // int64 or int32
+    int32_t target_wide;
+    int64_t ignore;
+    // forward: the tiles' statistics, `columns` of them a token
+    const float *stats, *picked;
+    int32_t columns;
+    float *loss, *lse;
+    // backward
+    const float* dloss;
+    int64_t s_dloss;              // elements between tokens' gradients, 0 for one of all
+    const float* lse_in;
+    mm::LossRow* rows;
+    float* scale;                 // [2] or null: a power of two for the factors, and its inverse
+    const void* x;                // copied with zeros in rows that the loss leaves out
+    int64_t ld_x;
+    void* x_to;
+    int64_t ld_to;
+};
+
+hipError_t launch_loss_join(const LossArgs& A, hipStream_t s);
+hipError_t launch_loss_rows(const LossArgs& A, hipStream_t s);
+
+// Router and tokens to experts.
+constexpr int kRouteMaxExperts = 1024;
+constexpr int kRouteMaxChoices = 16;
+
+struct RouteArgs {
+    int64_t tokens;
+    int32_t experts, k, normalise;
+    float scale;
+    const void* logits;
+    int64_t ld_logits;
+    void* index;                  // int32 [tokens][k]
+    float* weight;                // [tokens][k]
+    const float* dweight;
+    int64_t ld_dweight;
+    void* dlogits;
+    int64_t ld_dlogits;
+};
+
+hipError_t launch_route_forward(const RouteArgs& A, int dtype, hipStream_t s);
+hipError_t launch_route_backward(const RouteArgs& A, int dtype, hipStream_t s);
+
+struct SortArgs {
+    int64_t choices;
+    int32_t experts, wide;        // wide: int64 indices
+    const void* index;
+    int32_t *offsets, *row;
+    int32_t* counts;              // [blocks][experts], of more than one block
+    int32_t blocks, each;         // choices of a block
+};
+
+constexpr int kSortThreads = 1024;
+void sort_plan(int64_t choices, int experts, int* blocks, int* each);
+hipError_t launch_sort(const SortArgs& A, hipStream_t s);
+
+// One row of x (dispatch), y, dy or dx a token; one of xs, ys, dys or dxs a choice.
+struct MoveArgs {
+    int64_t tokens, rows;         // rows: of xs and ys, all that `row` may name
+    int32_t model, k;
+    const int32_t* row;           // [tokens][k]
+    const float* weight;          // nullable
+    int64_t ld_weight;
+    const void *token, *choice;   // read: rows of tokens, rows of choices
+    int64_t ld_token, ld_choice;
+    void *to_token, *to_choice;
+    int64_t ld_to_token, ld_to_choice;
+    float* dweight;
+};
+
+hipError_t launch_dispatch(const MoveArgs& A, int dtype, hipStream_t s);
+hipError_t launch_combine(const MoveArgs& A, int dtype, hipStream_t s);
+hipError_t launch_combine_backward(const MoveArgs& A, int dtype, hipStream_t s);
 
 // Norms around a block.
 struct NormArgs {

@@ -1,0 +1,13 @@
+// The loss's tiled products in float16.
+#include "arena_gemm.h"
+
+namespace arena {
+namespace mm {
+
+hipError_t launch_loss_f16(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
+{
+    return launch_loss_t<F16>(A, what, cut, s);
+}
+
+}  // namespace mm
+}  // namespace arena

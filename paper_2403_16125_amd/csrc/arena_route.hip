@@ -1,0 +1,570 @@
+// The router of a layer of experts, and tokens to experts and back.
+//
+//   route      of each token's logits the k largest, their softmax (over them or over
+//              all), and the gradient of that
+//   sort       where each choice's row lies when the choices are sorted by expert
+//   dispatch   xs[row[t, j]] = x[t]
+//   combine    y[t] = sum_j w[t, j] ys[row[t, j]], and its gradients
+//
+// Nothing here multiplies matrices: the moves are bound by memory, the router of many
+// tokens by the passes over its lanes, small calls by the launch.
+#include <hip/hip_runtime.h>
+
+#include "arena_layer_internal.h"
+
+namespace arena {
+namespace {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// ---------------------------------------------------------------- router
+
+// Sums and maxima over groups of W neighbouring lanes, in every lane: within 16 by
+// cross-lane operands, past that through the permute network.
+template <int CTRL>
+__device__ __forceinline__ uint32_t cross(uint32_t v)
+{
+    return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+
+template <int W>
+__device__ __forceinline__ uint32_t group_max(uint32_t v)
+{
+    v = max(v, cross<0xb1>(v));                   // lanes ^ 1
+    v = max(v, cross<0x4e>(v));                   // lanes ^ 2
+    v = max(v, cross<0x141>(v));                  // mirrored in 8
+    if (W > 8) v = max(v, cross<0x140>(v));       // mirrored in 16
+    if (W > 16) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    if (W > 32) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    return v;
+}
+
+template <int W>
+__device__ __forceinline__ float group_sum(float v)
+{
+    v += __uint_as_float(cross<0xb1>(__float_as_uint(v)));
+    v += __uint_as_float(cross<0x4e>(__float_as_uint(v)));
+    v += __uint_as_float(cross<0x141>(__float_as_uint(v)));
+    if (W > 8) v += __uint_as_float(cross<0x140>(__float_as_uint(v)));
+    if (W > 16) v += __shfl_xor(v, 16, 64);
+    if (W > 32) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
+// Numbers as unsigned ones of the same order: NaN above everything, both zeros alike,
+// -inf (an expert that is never chosen) 0.
+__device__ __forceinline__ uint32_t key_of(float f)
+{
+    if (f != f) return 0xffffffffu;
+    if (f == -INFINITY) return 0;
+    const uint32_t u = __float_as_uint(f + 0.0f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ float value_of(uint32_t key)
+{
+    return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void fetch(const E* p, int left, float (&v)[N], float past)
+{
+    if (left >= N) {
+        E w[N];
+        __builtin_memcpy(w, p, sizeof(w));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (float)w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = i < left ? (float)p[i] : past;
+    }
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void store(E* p, int left, const float (&v)[N])
+{
+    if (left >= N) {
+        E w[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = (E)v[i];
+        __builtin_memcpy(p, w, sizeof(w));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = (E)v[i];
+    }
+}
+
+// A group of W lanes takes a token, each lane NV neighbouring experts in registers.  The
+// largest key of the group is found k times: the first lane that holds it has the lowest
+// index, and takes it out of its own.
+template <typename E, int W, int NV>
+__global__ __launch_bounds__(256) void route_kernel(const RouteArgs A)
+{
+    const int lane = threadIdx.x & 63, in = lane & (W - 1), base = lane & ~(W - 1);
+    const int64_t t = (int64_t)blockIdx.x * (256 / W) + threadIdx.x / W;
+    const bool there = t < A.tokens;
+    float l[NV];
+    const int e0 = in * NV;
+    fetch((const E*)A.logits + (there ? t : 0) * A.ld_logits + e0, A.experts - e0, l, -INFINITY);
+    uint32_t key[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) key[v] = key_of(l[v]);
+    float first = 0.0f, mine = -INFINITY;
+    int index = -1;
+    for (int j = 0; j < A.k; ++j) {
+        uint32_t most = key[0];
+#pragma unroll
+        for (int v = 1; v < NV; ++v) most = max(most, key[v]);
+        const uint32_t top = group_max<W>(most);
+        const uint64_t holders = __ballot(most == top && top != 0) >> base & (~0ull >> (64 - W));
+        const int owner = holders ? __ffsll((unsigned long long)holders) - 1 : 0;
+        int at = -1;
+        if (holders && in == owner) {
+#pragma unroll
+            for (int v = NV - 1; v >= 0; --v) at = key[v] == top ? v : at;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) key[v] = v == at ? 0 : key[v];
+            at += e0;
+        }
+        at = __shfl(at, base + owner, 64);
+        const float value = top ? value_of(top) : -INFINITY;
+        if (j == 0 && top) first = value;
+        if (in == j) {
+            mine = value;
+            index = at;
+        }
+    }
+    // weights of -inf are 0 without an exponential of -inf - inf
+    const float chosen = index >= 0 ? expf(mine - first) : 0.0f;
+    float part = chosen;
+    if (!A.normalise) {
+        part = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) part += l[v] == -INFINITY ? 0.0f : expf(l[v] - first);
+    }
+    const float total = group_sum<W>(part);
+    if (!there || in >= A.k) return;
+    ((int32_t*)A.index)[t * A.k + in] = index;
+    A.weight[t * A.k + in] = index >= 0 ? A.scale * (chosen / total) : 0.0f;
+}
+
+// With q the softmax without the scale:  over the chosen, of a chosen logit
+// q (s dw - sum_i q_i s dw_i); over all, of every logit -p sum_i p_i s dw_i, and of a
+// chosen one p s dw more.  Choices that name an expert twice add up.
+template <typename E, int W, int NV>
+__global__ __launch_bounds__(256) void route_back_kernel(const RouteArgs A)
+{
+    const int lane = threadIdx.x & 63, in = lane & (W - 1), base = lane & ~(W - 1);
+    const int64_t t = (int64_t)blockIdx.x * (256 / W) + threadIdx.x / W;
+    const bool there = t < A.tokens;
+    const E* row = (const E*)A.logits + (there ? t : 0) * A.ld_logits;
+    const int e0 = in * NV;
+    int index = -1;
+    float dw = 0.0f, taken = -INFINITY;
+    if (there && in < A.k) {
+        index = ((const int32_t*)A.index)[t * A.k + in];
+        if (index < 0 || index >= A.experts) index = -1;
+    }
+    if (index >= 0) {
+        dw = A.scale * A.dweight[t * A.ld_dweight + in];
+        taken = (float)row[index];
+    }
+    float l[NV], d[NV];
+    uint32_t most = key_of(taken);
+    if (!A.normalise) {
+        fetch(row + e0, A.experts - e0, l, -INFINITY);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) most = max(most, key_of(l[v]));
+    }
+    most = group_max<W>(most);
+    const float first = most ? value_of(most) : 0.0f;
+    const float e = index >= 0 && taken != -INFINITY ? expf(taken - first) : 0.0f;
+    float part = e;
+    if (!A.normalise) {
+        part = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            l[v] = l[v] == -INFINITY ? 0.0f : expf(l[v] - first);
+            part += l[v];
+        }
+    }
+    const float total = group_sum<W>(part), inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    const float q = e * inverse, mean = group_sum<W>(index >= 0 ? q * dw : 0.0f);
+    const float mine = index < 0 ? 0.0f : A.normalise ? q * (dw - mean) : q * dw;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) d[v] = A.normalise ? 0.0f : -(l[v] * inverse) * mean;
+    for (int j = 0; j < A.k; ++j) {
+        const int at = __shfl(index, base + j, 64) - e0;
+        const float more = __shfl(mine, base + j, 64);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) d[v] += v == at ? more : 0.0f;
+    }
+    if (there) store((E*)A.dlogits + t * A.ld_dlogits + e0, A.experts - e0, d);
+}
+
+template <typename E, int W, int NV>
+hipError_t launch_route_of(const RouteArgs& A, bool back, hipStream_t s)
+{
+    const int64_t blocks = (A.tokens + 256 / W - 1) / (256 / W);
+    if (back) route_back_kernel<E, W, NV><<<(unsigned)blocks, 256, 0, s>>>(A);
+    else route_kernel<E, W, NV><<<(unsigned)blocks, 256, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+// Lanes of a token: a power of two that holds its experts and its choices.
+template <typename E>
+hipError_t launch_route_t(const RouteArgs& A, bool back, hipStream_t s)
+{
+    const int n = A.experts > A.k ? A.experts : A.k;
+    if (n <= 8) return launch_route_of<E, 8, 1>(A, back, s);
+    if (n <= 16) return launch_route_of<E, 16, 1>(A, back, s);
+    if (n <= 32) return launch_route_of<E, 16, 2>(A, back, s);
+    if (n <= 64) return launch_route_of<E, 16, 4>(A, back, s);
+    if (n <= 128) return launch_route_of<E, 16, 8>(A, back, s);
+    if (n <= 256) return launch_route_of<E, 32, 8>(A, back, s);
+    if (n <= 512) return launch_route_of<E, 64, 8>(A, back, s);
+    return launch_route_of<E, 64, 16>(A, back, s);
+}
+
+hipError_t launch_route(const RouteArgs& A, int dtype, bool back, hipStream_t s)
+{
+    if (A.tokens == 0) return hipSuccess;
+    switch (dtype) {
+    case ARENA_F32: return launch_route_t<float>(A, back, s);
+    case ARENA_BF16: return launch_route_t<bf16>(A, back, s);
+    case ARENA_F16: return launch_route_t<f16>(A, back, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+// ---------------------------------------------------------------- sort by expert
+
+// The expert of choice i, or -1.
+__device__ __forceinline__ int expert_of(const SortArgs& A, int64_t i, int64_t end)
+{
+    if (i >= end) return -1;
+    const int64_t e = A.wide ? ((const int64_t*)A.index)[i] : ((const int32_t*)A.index)[i];
+    return e >= 0 && e < A.experts ? (int)e : -1;
+}
+
+// How many choices of a block's share name each expert.
+__device__ __forceinline__ void count_choices(const SortArgs& A, int64_t begin, int64_t end, int* hist)
+{
+    for (int e = threadIdx.x; e < A.experts; e += kSortThreads) hist[e] = 0;
+    __syncthreads();
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
+        const int e = expert_of(A, i, end);
+        if (e >= 0) atomicAdd(&hist[e], 1);
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs A)
+{
+    __shared__ int hist[kRouteMaxExperts];
+    const int64_t begin = (int64_t)blockIdx.x * A.each, end = min(A.choices, begin + A.each);
+    count_choices(A, begin, end, hist);
+    for (int e = threadIdx.x; e < A.experts; e += kSortThreads) A.counts[(int64_t)blockIdx.x * A.experts + e] = hist[e];
+}
+
+// Rows of a block's choices, 1024 at a time: an expert's rows begin where those of the
+// experts before end, within it those of the blocks before, of the chunks before, of the
+// waves before and of the lanes before that chose it.  Counts are whole numbers, so
+// nothing depends on the order in which they are added.
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs A)
+{
+    constexpr int kWaves = kSortThreads / 64;
+    __shared__ int next[kRouteMaxExperts];            // the expert's next row
+    __shared__ int sums[kSortThreads], below[kSortThreads];
+    __shared__ int waves[kWaves];
+    __shared__ uint16_t each[kWaves][kRouteMaxExperts];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = A.experts;
+    const int64_t begin = (int64_t)blockIdx.x * A.each, end = min(A.choices, begin + A.each);
+
+    // all choices of expert `tid`, and those of the blocks before this one
+    int all = 0, before = 0;
+    if (A.blocks == 1) {
+        count_choices(A, begin, end, next);
+        if (tid < E) all = next[tid];
+    } else {
+        // several threads share an expert's column
+        int width = 1;
+        while (width < E) width *= 2;
+        const int parts = kSortThreads / width, e = tid & (width - 1), part = tid / width;
+        if (e < E)
+#pragma unroll 4
+            for (int b = part; b < A.blocks; b += parts) {
+                const int n = A.counts[(int64_t)b * E + e];
+                all += n;
+                before += b < (int)blockIdx.x ? n : 0;
+            }
+        sums[tid] = all;
+        below[tid] = before;
+        __syncthreads();
+        all = before = 0;
+        if (tid < E)
+            for (int p = 0; p < parts; ++p) {
+                all += sums[p * width + tid];
+                before += below[p * width + tid];
+            }
+    }
+    // exclusive sums over the experts
+    int sum = tid < E ? all : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int w = __shfl_up(sum, d, 64);
+        sum += lane >= d ? w : 0;
+    }
+    if (lane == 63) waves[wave] = sum;
+    __syncthreads();
+    int start = sum - all;
+    for (int w = 0; w < wave; ++w) start += waves[w];
+    if (tid < E) {
+        next[tid] = start + before;
+        if (blockIdx.x == 0) {
+            A.offsets[tid] = start;
+            if (tid == E - 1) A.offsets[E] = start + all;
+        }
+    }
+    int bits = 0;
+    while (1 << bits < E) ++bits;
+    for (int64_t from = begin; from < end; from += kSortThreads) {
+        __syncthreads();
+        for (int e = tid; e < kWaves * E; e += kSortThreads) each[e / E][e % E] = 0;
+        const int e = expert_of(A, from + tid, end);
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t ones = __ballot(e >> b & 1);
+            same &= e >> b & 1 ? ones : ~ones;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        __syncthreads();
+        if (e >= 0 && rank == 0) each[wave][e] = (uint16_t)__popcll(same);
+        __syncthreads();
+        if (tid < E) {
+            int n = 0;
+            for (int w = 0; w < kWaves; ++w) {
+                const int mine = each[w][tid];
+                each[w][tid] = (uint16_t)n;          // at most 1024
+                n += mine;
+            }
+            sums[tid] = next[tid];
+            next[tid] += n;
+        }
+        __syncthreads();
+        if (from + tid < end) A.row[from + tid] = e >= 0 ? sums[e] + each[wave][e] + rank : -1;
+    }
+}
+
+// ---------------------------------------------------------------- moves
+
+constexpr int kChunks = 4;            // 16-byte pieces that a lane has in flight
+
+template <typename E>
+struct Chunk {
+    static constexpr int n = 16 / sizeof(E);
+};
+
+// A wave's stretch of a token's row: kChunks times 64 pieces from column `from`.
+template <typename E>
+__device__ __forceinline__ void dispatch_row(const MoveArgs& A, int64_t t, int from, int lane)
+{
+    constexpr int N = Chunk<E>::n;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const E* x = (const E*)A.token + t * A.ld_token;
+    u32x4 v[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = from + (i * 64 + lane) * N;
+        if (c + N <= A.model) __builtin_memcpy(&v[i], x + c, 16);
+    }
+    for (int j = 0; j < A.k; ++j) {
+        const int64_t r = A.row[t * A.k + j];
+        if (r < 0 || r >= A.rows) continue;
+        E* to = (E*)A.to_choice + r * A.ld_to_choice;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = from + (i * 64 + lane) * N;
+            if (c + N <= A.model) __builtin_memcpy(to + c, &v[i], 16);
+            else
+                for (int q = c; q < A.model; ++q) to[q] = x[q];
+        }
+    }
+}
+
+// y = sum_j w_j ys[row_j], in 32 bits and in the order of j, rounded once.
+template <typename E>
+__device__ __forceinline__ void combine_row(const MoveArgs& A, int64_t t, int from, int lane)
+{
+    constexpr int N = Chunk<E>::n;
+    float sum[kChunks][N];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[i][q] = 0.0f;
+#pragma unroll 2
+    for (int j = 0; j < A.k; ++j) {
+        const int64_t r = A.row[t * A.k + j];
+        if (r < 0 || r >= A.rows) continue;
+        const float w = A.weight ? A.weight[t * A.ld_weight + j] : 1.0f;
+        const E* p = (const E*)A.choice + r * A.ld_choice;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = from + (i * 64 + lane) * N;
+            if (c >= A.model) continue;
+            float v[N];
+            fetch(p + c, A.model - c, v, 0.0f);
+#pragma unroll
+            for (int q = 0; q < N; ++q) sum[i][q] += A.weight ? w * v[q] : v[q];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = from + (i * 64 + lane) * N;
+        if (c < A.model) store((E*)A.to_token + t * A.ld_to_token + c, A.model - c, sum[i]);
+    }
+}
+
+// Waves take stretches of tokens in turn.
+template <typename E, bool BACK>
+__global__ __launch_bounds__(256) void move_kernel(const MoveArgs A, int stretches)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t n = A.tokens * stretches, step = (int64_t)gridDim.x * 4;
+    int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (; i < n; i += step) {
+        const int64_t t = stretches == 1 ? i : i / stretches;
+        const int from = (int)(i - t * stretches) * (kChunks * 64 * Chunk<E>::n);
+        if (BACK) combine_row<E>(A, t, from, lane);
+        else dispatch_row<E>(A, t, from, lane);
+    }
+}
+
+// dys[row_j] = w_j dy and dw_j = <dy, ys[row_j]>: WAVES waves share a token, dy stays in
+// registers while the choices' rows pass.
+template <typename E, int WAVES>
+__global__ __launch_bounds__(256) void combine_back_kernel(const MoveArgs A)
+{
+    constexpr int N = Chunk<E>::n, kEach = 256 / 64 / WAVES, kWide = WAVES * 64 * N * kChunks;
+    __shared__ float dots[WAVES > 1 ? WAVES : 1][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % WAVES;
+    for (int64_t t = (int64_t)blockIdx.x * kEach + wave / WAVES; t < A.tokens; t += (int64_t)gridDim.x * kEach) {
+        const E* dy = (const E*)A.token + t * A.ld_token;
+        float mine = 0.0f;                  // of choice `lane`
+        for (int from = 0; from < A.model; from += kWide) {
+            float d[kChunks][N];
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+                const int c = from + ((i * WAVES + share) * 64 + lane) * N;
+                if (c < A.model) fetch(dy + c, A.model - c, d[i], 0.0f);
+            }
+            for (int j = 0; j < A.k; ++j) {
+                const int64_t r = A.row[t * A.k + j];
+                if (r < 0 || r >= A.rows) continue;
+                const float w = A.weight[t * A.ld_weight + j];
+                const E* p = (const E*)A.choice + r * A.ld_choice;
+                E* to = (E*)A.to_choice + r * A.ld_to_choice;
+                float dot = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = from + ((i * WAVES + share) * 64 + lane) * N;
+                    if (c >= A.model) continue;
+                    float v[N];
+                    fetch(p + c, A.model - c, v, 0.0f);
+#pragma unroll
+                    for (int q = 0; q < N; ++q) {
+                        dot += q < A.model - c ? d[i][q] * v[q] : 0.0f;
+                        v[q] = w * d[i][q];
+                    }
+                    store(to + c, A.model - c, v);
+                }
+                dot = group_sum<64>(dot);
+                if (lane == j) mine += dot;
+            }
+        }
+        if (WAVES > 1) {
+            dots[share][lane] = mine;
+            __syncthreads();
+            mine = 0.0f;
+#pragma unroll
+            for (int s = 0; s < WAVES; ++s) mine += dots[s][lane];
+            __syncthreads();
+        }
+        if (share == 0 && lane < A.k) A.dweight[t * A.k + lane] = mine;
+    }
+}
+
+template <typename E, bool BACK>
+hipError_t launch_move(const MoveArgs& A, hipStream_t s)
+{
+    const int wide = kChunks * 64 * Chunk<E>::n, stretches = (A.model + wide - 1) / wide;
+    const int64_t blocks = (A.tokens * stretches + 3) / 4;
+    if (blocks == 0) return hipSuccess;
+    move_kernel<E, BACK><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(A, stretches);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_combine_back(const MoveArgs& A, hipStream_t s)
+{
+    if (A.tokens == 0) return hipSuccess;
+    // a wave a token where that fills the card and a row fits its registers
+    if (A.tokens >= 4096 && A.model <= 64 * Chunk<E>::n * kChunks) {
+        const int64_t blocks = (A.tokens + 3) / 4;
+        combine_back_kernel<E, 1><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(A);
+    } else {
+        combine_back_kernel<E, 4><<<(unsigned)(A.tokens < 65536 ? A.tokens : 65536), 256, 0, s>>>(A);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_route_forward(const RouteArgs& A, int dtype, hipStream_t s) { return launch_route(A, dtype, false, s); }
+hipError_t launch_route_backward(const RouteArgs& A, int dtype, hipStream_t s) { return launch_route(A, dtype, true, s); }
+
+// One block up to 4096 choices; past that at most 128 blocks of whole chunks, whose
+// counts every block reads.
+void sort_plan(int64_t choices, int experts, int* blocks, int* each)
+{
+    (void)experts;
+    *blocks = 1;
+    *each = (int)choices;
+    if (choices <= 4096) return;
+    const int64_t per = (choices + 127) / 128;
+    *each = (int)((per + kSortThreads - 1) / kSortThreads * kSortThreads);
+    *blocks = (int)((choices + *each - 1) / *each);
+}
+
+hipError_t launch_sort(const SortArgs& A, hipStream_t s)
+{
+    if (A.blocks > 1) {
+        sort_count_kernel<<<A.blocks, kSortThreads, 0, s>>>(A);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    sort_place_kernel<<<A.blocks, kSortThreads, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+hipError_t launch_dispatch(const MoveArgs& A, int dtype, hipStream_t s)
+{
+    // bits are copied: 16-bit types alike
+    return dtype == ARENA_F32 ? launch_move<float, false>(A, s) : launch_move<bf16, false>(A, s);
+}
+
+hipError_t launch_combine(const MoveArgs& A, int dtype, hipStream_t s)
+{
+    return dtype == ARENA_F32 ? launch_move<float, true>(A, s)
+           : dtype == ARENA_BF16 ? launch_move<bf16, true>(A, s) : launch_move<f16, true>(A, s);
+}
+
+hipError_t launch_combine_backward(const MoveArgs& A, int dtype, hipStream_t s)
+{
+    return dtype == ARENA_F32 ? launch_combine_back<float>(A, s)
+           : dtype == ARENA_BF16 ? launch_combine_back<bf16>(A, s) : launch_combine_back<f16>(A, s);
+}
+
+}  // namespace arena

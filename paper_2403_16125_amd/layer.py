@@ -13,8 +13,9 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 
-from . import arena
+from . import arena, layer_experts
 from .arena import ArenaError, _check
+from .layer_experts import ExpertOps, ExpertPlan
 
 F32, BF16, F16 = 0, 1, 2
 NORM_KINDS = {"rms": 0, "layer": 1}
@@ -166,8 +167,10 @@ class FfnSaved:
         return 0, g, u, u + 3 * n
 
 
-class LayerOps:
-    """The layer operators on one device, for torch tensors.
+class LayerOps(ExpertOps):
+    """The layer operators on one device, for torch tensors: norms around a block, the
+    gated feed-forward block and the orthogonalised update here, the router, tokens to
+    experts and back, the experts' blocks and the cross entropy in layer_experts.py.
 
     Tensors live on `device`; matrices have unit stride along their last axis
     and any row stride.  Outputs are new tensors unless given.  Work goes to the
@@ -179,6 +182,7 @@ class LayerOps:
         self.torch = torch
         self.dev = torch.device("cuda", device)
         load()
+        layer_experts.load()
         self.ctx = arena.arena_create(device)
         self._alive = True
         self._index, self._new, self._current = int(device), torch.empty, torch.cuda.current_stream
@@ -379,12 +383,24 @@ class LayerOps:
 
     # -- gated feed-forward block
 
-    def _ffn_desc(self, x, w_gate, w_up, w_down, activation):
-        if activation not in ACTIVATIONS:
+    @staticmethod
+    def _activation(name) -> int:
+        if name not in ACTIVATIONS:
             raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+        return ACTIVATIONS[name]
+
+    def _inner(self, tokens, inner, save):
+        """A new buffer for h, with save for g and u too: FfnSaved, its address and the
+        offsets of g and u."""
+        saved = FfnSaved(None, tokens, -(-inner // 8) * 8)
+        _, g, u, size = saved.parts()
+        saved.buffer = self._empty((size if save else g,), self.torch.uint8)
+        return saved, saved.buffer.data_ptr(), g, u
+
+    def _ffn_desc(self, x, w_gate, w_up, w_down, activation):
         tokens, model = self._rows(x)
         inner = w_gate.shape[0]
-        d = FfnDesc(dtype=self._type(x), activation=ACTIVATIONS[activation], tokens=tokens, model=model, inner=inner)
+        d = FfnDesc(dtype=self._type(x), activation=self._activation(activation), tokens=tokens, model=model, inner=inner)
         d.x, d.ld_x = self._matrix("x", x, (tokens, model), x.dtype)
         d.w_gate, d.ld_gate = self._matrix("w_gate", w_gate, (inner, model), x.dtype)
         d.w_up, d.ld_up = self._matrix("w_up", w_up, (inner, model), x.dtype)
@@ -402,12 +418,8 @@ class LayerOps:
         d = self._ffn_desc(x, w_gate, w_up, w_down, activation)
         y = self._empty(x.shape, x.dtype) if out is None else out
         d.y, d.ld_y = self._matrix("out", y, (d.tokens, d.model), x.dtype)
-        d.ld_inner = -(-d.inner // 8) * 8
-        saved = FfnSaved(None, d.tokens, d.ld_inner)
-        _, g, u, size = saved.parts()
-        saved.buffer = self._empty((size if save else g,), self.torch.uint8)
-        base = saved.buffer.data_ptr()
-        d.h = base
+        saved, base, g, u = self._inner(d.tokens, d.inner, save)
+        d.h, d.ld_inner = base, saved.ld
         if save:
             d.g, d.u = base + g, base + u
         keep = self._workspace(d, arena_ffn_forward_workspace(self.ctx, d))
