@@ -257,18 +257,42 @@ bool direct(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts
     return Operand::direct(p, ld, cols) && (experts == 1 || stride % 8 == 0);
 }
 
+// What a kind of tile costs in microseconds (measured on one MI355X): a step of 64 of k
+// with every slot of the compute units taken and with at most one block on each, a tile
+// beside its steps, and how many blocks a compute unit holds.
+struct GroupCost {
+    double full, alone, start;
+    int slots;
+};
+constexpr GroupCost kGroupCost[arena::mm::kGroupKinds] = {
+    {1.75, 1.30, 4.0, 1}, {1.00, 0.75, 3.0, 2}, {0.80, 0.60, 2.0, 2}};
+
+// uneven: how much longer than the average one the longest of few tiles takes.
+double group_time(double tiles, double steps, int kind, int64_t splits, double bytes, double uneven)
+{
+    const GroupCost& k = kGroupCost[kind];
+    const double per = std::ceil(steps / splits), values = (double)arena::mm::kGroupRows[kind] * arena::mm::kGroupCols[kind];
+    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate;
+    const double blocks = tiles * splits, round = kUnits * k.slots;
+    // how many tiles there are is an estimate: half a round more than they fill
+    const double t = blocks <= kUnits  ? per * uneven * k.alone + k.start + end
+                     : blocks <= round ? per * uneven * k.full + k.start + end * k.slots
+                                       : (blocks / round + 0.5) * (per * k.full + k.start + end * k.slots);
+    return kLaunch + t + (splits > 1 ? kJoin + blocks * values * 4e-6 / kJoinRate : 0.0);
+}
+
 // The kind of tile for a product of groups of rows: how they fall is not known here, so
 // each group that can have rows is taken to waste half a tile.
 int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes)
 {
     using namespace arena::mm;
-    int best = k256;
+    int best = kGroup256;
     double least = INFINITY;
-    for (int kind : {k256, k128, k64}) {
-        const int64_t side = kTileSide[kind], some = std::min(groups, rows);
-        const int64_t tm = std::max(some, rows / side + some / 2), tn = ceil_div(N, dual ? side / 2 : side);
-        if (group_tiles(rows, groups, side) * tn > 0x7fffffff) continue;
-        const double t = launch_time(tm * tn, steps, kind, 1, bytes);
+    for (int kind = 0; kind < kGroupKinds; ++kind) {
+        const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
+        const double tm = std::max((double)some, (double)rows / kGroupRows[kind] + 0.5 * some);
+        if (group_tiles(rows, groups, kGroupRows[kind]) * tn > 0x7fffffff) continue;
+        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0);
         if (t < least) {
             least = t;
             best = kind;
@@ -287,37 +311,43 @@ struct StepCut {
 StepCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes)
 {
     using namespace arena::mm;
-    StepCut best = {k256, 1, 0};
+    StepCut best = {kGroup256, 1, 0};
     double least = INFINITY;
     const int64_t steps = std::max<int64_t>(1, ceil_div(rows, groups * kBK));
-    for (int kind : {k256, k128, k64}) {
-        const int64_t side = kTileSide[kind], tiles = ceil_div(M, side) * ceil_div(N, side) * groups * pairs;
-        if (tiles > 0x7fffffff) continue;
+    for (int kind = 0; kind < kGroupKinds; ++kind) {
+        const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * groups * pairs;
         for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
-            const double t = launch_time(tiles, steps, kind, s, bytes);
+            if (tiles * s > 0x7fffffff) continue;
+            const double t = group_time((double)tiles, (double)steps, kind, s, bytes, 1.5);
             if (t < least) {
                 least = t;
-                best = {kind, s, s > 1 ? 4 * s * tiles * side * side : 0};
+                best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0};
             }
         }
     }
     return best;
 }
 
+// Whether a forward pass takes the kernel for few rows, which streams the weights of one
+// group after the other past 16 rows.  With more the tiles read them as fast, and those
+// of a group only once (64 experts of 2048 x 1408: 16 rows 48 us against 58, 32 rows 86
+// against 77; 8 of 4096 x 10944: 292 against 390, 64 rows 471 against 421).
+bool few_rows(const arena_experts_desc* d) { return d->rows <= 16; }
+
 struct ExpertsPlan {
     Pieces w;
-    bool gate_ok;
+    bool skinny, gate_ok;
     Operand x, gate, up, down;
-    ExpertsPlan(const arena_experts_desc* d, void* base)
-        : w(base),
+    ExpertsPlan(const arena_experts_desc* d, bool skinny_, void* base)
+        : w(base), skinny(skinny_),
           gate_ok(direct(d->w_gate, d->ld_gate, d->model, d->stride_gate, d->experts) &&
                   direct(d->w_up, d->ld_up, d->model, d->stride_up, d->experts) && d->ld_gate == d->ld_up &&
                   (d->experts == 1 || d->stride_gate == d->stride_up)),
-          x(w, d->x, d->ld_x, d->rows, d->model, Operand::direct(d->x, d->ld_x, d->model)),
-          gate(w, d->w_gate, d->ld_gate, d->inner, d->model, gate_ok, d->experts, d->stride_gate),
-          up(w, d->w_up, d->ld_up, d->inner, d->model, gate_ok, d->experts, d->stride_up),
+          x(w, d->x, d->ld_x, d->rows, d->model, skinny || Operand::direct(d->x, d->ld_x, d->model)),
+          gate(w, d->w_gate, d->ld_gate, d->inner, d->model, skinny || gate_ok, d->experts, d->stride_gate),
+          up(w, d->w_up, d->ld_up, d->inner, d->model, skinny || gate_ok, d->experts, d->stride_up),
           down(w, d->w_down, d->ld_down, d->model, d->inner,
-               direct(d->w_down, d->ld_down, d->inner, d->stride_down, d->experts), d->experts, d->stride_down)
+               skinny || direct(d->w_down, d->ld_down, d->inner, d->stride_down, d->experts), d->experts, d->stride_down)
     {
     }
 };
@@ -329,7 +359,7 @@ struct ExpertsBackPlan : ExpertsPlan {
     bool pair;                // both weight gradients of the first products in one launch
     StepCut cut_up, cut_down;
     ExpertsBackPlan(const arena_experts_desc* d, const arena_experts_grads* g, void* base)
-        : ExpertsPlan(d, base),
+        : ExpertsPlan(d, false, base),
           dy(w, g->dy, g->ld_dy, d->rows, d->model, Operand::direct(g->dy, g->ld_dy, d->model))
     {
         ld = pad8(d->inner);
@@ -477,7 +507,7 @@ arena_status arena_experts_forward_workspace(arena_ctx* c, const arena_experts_d
     if (!bytes) return ctx_fail(c, ARENA_ERR_INVALID_ARG, "experts forward: bytes is NULL");
     const arena_status s = check_experts(c, "experts forward", d, false);
     if (s) return s;
-    *bytes = d->rows ? ExpertsPlan(d, nullptr).w.used : 0;
+    *bytes = d->rows ? ExpertsPlan(d, few_rows(d), nullptr).w.used : 0;
     return ARENA_OK;
 }
 
@@ -487,7 +517,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     ctx_clear(c);
     arena_status st = check_experts(c, "experts forward", d, false);
     if (st || d->rows == 0) return st;
-    const ExpertsPlan P(d, d->workspace);
+    const ExpertsPlan P(d, few_rows(d), d->workspace);
     if ((st = check_workspace(c, "experts forward", d->workspace, d->workspace_bytes, P.w.used))) return st;
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
@@ -501,21 +531,24 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     A.splits = 1;
     A.a[0] = P.x.p; A.lda = P.x.ld;
     A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld; A.sb = P.gate.stride;
+    A.ldb1 = P.up.ld; A.sb1 = P.up.stride;
     A.c[0] = d->h; A.ldc = d->ld_inner;
     A.g = d->g; A.u = d->u; A.ldg = d->ld_inner;
     A.act = d->activation;
     A.pad = (int)pad8(d->inner);
-    if ((e = arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
-                                      choose_rows(R, E, d->inner, ceil_div(d->model, bk), true, d->g ? 4.0 : 1.0), s)))
-        return hip_error(c, e, "experts gate and up launch");
+    e = P.skinny ? arena::mm::launch_skinny_groups(A, d->dtype, true, s)
+                 : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
+                                            choose_rows(R, E, d->inner, ceil_div(d->model, bk), true, d->g ? 4.0 : 1.0), s);
+    if (e) return hip_error(c, e, "experts gate and up launch");
     GemmArgs B = new_args(R, d->model, d->inner);
     B.offsets = d->offsets; B.groups = d->experts;
     B.splits = 1;
     B.a[0] = d->h; B.lda = d->ld_inner;
     B.b[0] = P.down.p; B.ldb = P.down.ld; B.sb = P.down.stride;
     B.c[0] = d->y; B.ldc = d->ld_y;
-    e = arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
-                                 choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0), s);
+    e = P.skinny ? arena::mm::launch_skinny_groups(B, d->dtype, false, s)
+                 : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
+                                            choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0), s);
     return e == hipSuccess ? ARENA_OK : hip_error(c, e, "experts down launch");
 }
 

@@ -209,13 +209,12 @@ struct Frags {
     }
 };
 
-template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool ATR_, bool BTR_, int EPI_,
-          int GROUP_ = kNoGroups>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool ATR_, bool BTR_, int EPI_>
 struct Tile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
-    static constexpr int EPI = EPI_, GROUP = GROUP_;
+    static constexpr int EPI = EPI_;
     // of columns past N, the gated epilogues and the logits' gradient write zeros up to pad
     static constexpr bool kUpToN = EPI_ == kPlain || EPI_ == kWide;
     static constexpr int kThreads = 64 * WM * WN;
@@ -321,8 +320,8 @@ struct Side<T, kGatedBwd> {
     }
     static __device__ __forceinline__ float value(u32x4 head, u32x2 tail, int r)
     {
-        const uint32_t h = (head[r >> 1] >> (16 * (r & 1))) & 0xffff, t = (tail[r >> 2] >> (8 * (r & 3))) & 0xff;
-        return __uint_as_float(h << 16 | t << 8);
+        const uint32_t high = r & 1 ? 0x07060000 : 0x05040000;      // bytes: 0, the tail, the head's two
+        return __uint_as_float(__builtin_amdgcn_perm(head[r >> 1], tail[r >> 2], high | (r & 3) << 8 | 0x0c));
     }
 };
 
@@ -474,16 +473,19 @@ template <int C>
 __device__ __forceinline__ void put24(void* p, const GemmArgs& A, int m, int n, const float (&v)[C])
 {
     const int64_t at = (int64_t)m * A.ldg + n;
-    uint16_t head[C];
-    uint8_t tail[C];
+    uint32_t b[C], head[C / 2], tail[C / 4];
 #pragma unroll
     for (int r = 0; r < C; ++r) {
         // a NaN of operands of 16 bits has nothing in the lower 8 that could carry
-        uint32_t b = __float_as_uint(v[r]);
-        b += 127 + (b >> 8 & 1);
-        head[r] = (uint16_t)(b >> 16);
-        tail[r] = (uint8_t)(b >> 8);
+        b[r] = __float_as_uint(v[r]);
+        b[r] += 127 + (b[r] >> 8 & 1);
     }
+#pragma unroll
+    for (int r = 0; r < C; r += 2) head[r / 2] = __builtin_amdgcn_perm(b[r + 1], b[r], 0x07060302);
+#pragma unroll
+    for (int r = 0; r < C; r += 4)
+        tail[r / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[r + 3], b[r + 2], 0x0c0c0501),
+                                            __builtin_amdgcn_perm(b[r + 1], b[r], 0x0c0c0501), 0x05040100);
     __builtin_memcpy((uint16_t*)p + at, head, sizeof(head));
     __builtin_memcpy((uint8_t*)p + 2 * (int64_t)A.M * A.ldg + at, tail, sizeof(tail));
 }
@@ -496,13 +498,16 @@ __device__ __forceinline__ void gated_fwd(const GemmArgs& A, int m, int n, float
 {
     typedef typename T::E E;
     float h[C];
+    if (n + C > A.N) {
+        // zeros past the last column: h is 0 there too
 #pragma unroll
-    for (int r = 0; r < C; ++r) {
-        const bool in = n + r < A.N;
-        g[r] = in ? g[r] : 0.0f;
-        u[r] = in ? u[r] : 0.0f;
-        h[r] = in ? act_value<ACT>(g[r]) * u[r] : 0.0f;
+        for (int r = 0; r < C; ++r) {
+            g[r] = n + r < A.N ? g[r] : 0.0f;
+            u[r] = n + r < A.N ? u[r] : 0.0f;
+        }
     }
+#pragma unroll
+    for (int r = 0; r < C; ++r) h[r] = act_value<ACT>(g[r]) * u[r];
     put((E*)A.c[0] + (int64_t)m * A.ldc + n, h, C);
     if (A.g) {
         put24(A.g, A, m, n, g);
@@ -527,12 +532,17 @@ __device__ __forceinline__ void gated_bwd(const GemmArgs& A, int m, int n, const
     float dg[8], du[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const bool in = n + r < A.N;
         float a, d;
         act_both<ACT>(side.value(side.gh, side.gt, r), &a, &d);
-        du[r] = in ? v[r] * a : 0.0f;
-        dg[r] = in ? v[r] * side.value(side.uh, side.ut, r) * d : 0.0f;
+        du[r] = v[r] * a;
+        dg[r] = v[r] * side.value(side.uh, side.ut, r) * d;
     }
+    if (n + 8 > A.N)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            du[r] = n + r < A.N ? du[r] : 0.0f;
+            dg[r] = n + r < A.N ? dg[r] : 0.0f;
+        }
     put((E*)A.c[0] + (int64_t)m * A.ldc + n, dg, 8);
     put((E*)A.c[1] + (int64_t)m * A.ldc + n, du, 8);
 }
@@ -551,7 +561,6 @@ __device__ __forceinline__ void gated_bwd_out(const GemmArgs& A, int m, int n, c
 // bands of 8 tile rows.
 struct Place {
     int m0, n0, z;
-    int m_end;           // rows of C past it are not this tile's
     bool mirror;         // symmetric and off the diagonal: the transposed tile is written too
 };
 
@@ -592,72 +601,8 @@ __device__ __forceinline__ bool place_of(const GemmArgs& A, int t, Place* at)
     tn = (tn << A.ratio) + (sub & ((1 << A.ratio) - 1));
     at->m0 = tm * P::BM;
     at->n0 = tn * P::kCols;
-    at->m_end = A.M;
     at->mirror = A.sym && tm != tn;
     return at->m0 < A.M && at->n0 < A.N && !(A.sym && tm < tn);
-}
-
-__device__ __forceinline__ int tile_of(int bid, int n_blocks);
-
-// Rows (steps) of group g, held inside 0 .. rows whatever the offsets are.
-__device__ __forceinline__ int group_end(const int32_t* offsets, int g, int rows)
-{
-    return min(max(offsets[g], 0), rows);
-}
-
-// Groups of rows: tiles of the groups in turn, of each in bands as above.  How many
-// there are only the device knows, so the launch has as many blocks as there can be, and
-// every wave finds its tile by itself: 64 groups at a time, their tile rows summed over
-// the lanes.  That is one read of the offsets on a block's way to its first load, less
-// than a launch that would lay out a table.
-template <typename P>
-__device__ __forceinline__ bool place_in_groups(const GemmArgs& A, int bid, Place* at)
-{
-    const int lane = threadIdx.x & 63;
-    auto rows_of = [&](int g, int* lo, int* hi) {
-        *lo = *hi = 0;
-        if (g < A.groups) {
-            *lo = group_end(A.offsets, g, A.M);
-            *hi = max(*lo, group_end(A.offsets, g + 1, A.M));
-        }
-        return (*hi - *lo + P::BM - 1) / P::BM;
-    };
-    auto sum_below = [&](int v) {      // inclusive over the lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int w = __shfl_up(v, d, 64);
-            v += lane >= d ? w : 0;
-        }
-        return v;
-    };
-    // groups that overlap could have more tiles than the launch
-    int lo, hi, total = 0;
-    const int most = quotient((int)gridDim.x, A.tiles_n);
-    for (int g0 = 0; g0 < A.groups; g0 += 64)
-        total = min(most, total + __builtin_amdgcn_readlane(sum_below(rows_of(g0 + lane, &lo, &hi)), 63));
-    if (bid >= total * A.tiles_n) return false;
-    const int tile = tile_of(bid, total * A.tiles_n);
-    int before = 0;
-    for (int g0 = 0; g0 < A.groups; g0 += 64) {
-        const int mine = rows_of(g0 + lane, &lo, &hi), sum = sum_below(mine), all = __builtin_amdgcn_readlane(sum, 63);
-        if (tile >= (int64_t)(before + all) * A.tiles_n) {
-            before += all;
-            continue;
-        }
-        const uint64_t past = __ballot(tile < (int64_t)(before + sum) * A.tiles_n);
-        const int l = __ffsll((unsigned long long)past) - 1;
-        const int tiles_m = __builtin_amdgcn_readlane(mine, l);
-        const int in_group = tile - (before + __builtin_amdgcn_readlane(sum, l) - tiles_m) * A.tiles_n;
-        const int band = 8 * A.tiles_n, b = quotient(in_group, band), in = in_group - b * band;
-        const int rows = min(8, tiles_m - b * 8), tn = quotient(in, rows);
-        at->z = g0 + l;
-        at->m0 = __builtin_amdgcn_readlane(lo, l) + (b * 8 + in - tn * rows) * P::BM;
-        at->m_end = __builtin_amdgcn_readlane(hi, l);
-        at->n0 = tn * P::kCols;
-        at->mirror = false;
-        return true;
-    }
-    return false;
 }
 
 // Blocks go to the 8 XCDs in turn, so each XCD gets a run of consecutive tiles:
@@ -724,7 +669,7 @@ __device__ __forceinline__ void loss_stats(const GemmArgs& A, const Place& at, f
     for (int i = 0; i < P::FM; ++i) {
         const int r = wm * (P::BM / P::WM) + i * 16 + (lane & 15), m = at.m0 + r;
         int64_t target = -1;
-        if (m < at.m_end)
+        if (m < A.M)
             target = (A.target_wide ? ((const int64_t*)A.target)[m] : ((const int32_t*)A.target)[m]) - A.first_col - n_lane;
         float most = -INFINITY;
 #pragma unroll
@@ -757,7 +702,7 @@ __device__ __forceinline__ void loss_stats(const GemmArgs& A, const Place& at, f
     __syncthreads();
     for (int r = threadIdx.x; r < P::BM; r += P::kThreads) {
         const int m = at.m0 + r;
-        if (m >= at.m_end) continue;
+        if (m >= A.M) continue;
         float most = -INFINITY, sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < P::WN; ++w) most = fmaxf(most, each[r * P::WN + w][0]);
@@ -784,21 +729,12 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
     Place at;
-    if (P::GROUP == kRowGroups ? !place_in_groups<P>(A, t, &at) : !place_of<P>(A, t, &at)) return;
-    // zb: what the epilogue takes as the batch index
-    const int zb = P::GROUP == kRowGroups ? 0 : at.z, m0 = at.m0, n0 = at.n0, m_end = at.m_end;
-    int k_from = 0, K = A.K;
-    if (P::GROUP == kStepGroups) {
-        const int g = at.z >> A.pairs;
-        if (A.K > 0) {                // of no steps there need be no offsets
-            k_from = group_end(A.offsets, g, A.K);
-            K = max(0, group_end(A.offsets, g + 1, A.K) - k_from);
-        }
-    }
+    if (!place_of<P>(A, t, &at)) return;
+    const int zb = at.z, m0 = at.m0, n0 = at.n0;
 
     Loader<P, P::BM, P::ATR, false> la;
     Loader<P, P::BN, P::BTR, P::DUAL> lb;
-    la.init(tid, m0, m_end, A.lda);
+    la.init(tid, m0, A.M, A.lda);
     lb.init(tid, n0, A.N, A.ldb);
     Frags<P, P::BM, P::ATR> fa;
     Frags<P, P::BN, P::BTR> fb;
@@ -811,31 +747,22 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
 #pragma unroll
         for (int j = 0; j < P::FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    const int sps = (K + kBK - 1) / kBK;     // steps of a segment
+    const int sps = (A.K + kBK - 1) / kBK;     // steps of a segment
     int s = 0, end = sps * A.nseg;
     if (A.splits > 1) {
-        const int per = P::GROUP == kStepGroups ? (end + A.splits - 1) / A.splits : A.per;
-        s = part * per;
-        end = min(end, s + per);
+        s = part * A.per;
+        end = min(end, s + A.per);
     }
-    int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
-    int sel = A.pairs ? zb : 0;
-    if (P::GROUP == kRowGroups) {
-        za = 0;
-        zB = at.z * A.sb;
-    } else if (P::GROUP == kStepGroups) {
-        za = k_from * A.lda;
-        zB = k_from * A.ldb;
-        sel = A.pairs ? at.z & 1 : 0;
-    }
+    const int64_t za = A.pairs ? 0 : zb * A.sa, zB = A.pairs ? 0 : zb * A.sb;
+    const int sel = A.pairs ? zb : 0;
 
     auto where = [&](int step, const char** pa, const char** pb, const char** pb1, int* left) {
         int q = step, seg = sel;
         if (A.nseg == 2 && step >= sps) { q -= sps; seg = 1; }
         *pa = la.base(A.a[seg], za) + q * la.step;
         *pb = lb.base(A.b[seg], zB) + q * lb.step;
-        *pb1 = P::DUAL ? lb.base(A.b[1], P::GROUP == kRowGroups ? zB : 0) + q * lb.step : *pb;
-        *left = K - q * kBK;
+        *pb1 = P::DUAL ? lb.base(A.b[1], 0) + q * lb.step : *pb;
+        *left = A.K - q * kBK;
     };
     // The loads of a step, of both operands (which = 3) or one of them.  Woven
     // between products they may not branch, so every lane compares its k with
@@ -866,7 +793,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
             const int x = (at + q) * 64 + lane, m = mw + x / kChunks, n = nw + x % kChunks * 8;
-            if (m < m_end && n < (P::kUpToN ? A.N : A.pad)) to[q].load(A, zb, m, n);
+            if (m < A.M && n < (P::kUpToN ? A.N : A.pad)) to[q].load(A, zb, m, n);
         }
     };
 
@@ -956,7 +883,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
             *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
         }
-        if (m >= m_end || n >= (P::kUpToN ? A.N : A.pad)) return;
+        if (m >= A.M || n >= (P::kUpToN ? A.N : A.pad)) return;
         if (A.splits > 1) {
             float* to = A.part + ((int64_t)part * n_tiles + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
             put(to, v, 8);
@@ -1026,8 +953,7 @@ template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void gemm_kernel(const GemmArgs A)
 {
     ARENA_TILE_BUFFERS(P, lds);
-    // groups of rows: the block maps itself, over the tiles that there are
-    tile_product<P>(A, P::GROUP == kRowGroups ? blockIdx.x : tile_of(blockIdx.x, gridDim.x), gridDim.x, blockIdx.y, lds);
+    tile_product<P>(A, tile_of(blockIdx.x, gridDim.x), gridDim.x, blockIdx.y, lds);
 }
 
 // Two independent products in one launch: blocks below n1 * A.splits belong to
@@ -1208,7 +1134,7 @@ hipError_t launch_tile(const GemmArgs& A, int64_t n_tiles, hipStream_t s)
     gemm_kernel<P><<<dim3((unsigned)n_tiles, A.splits), P::kThreads, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    if constexpr (P::EPI == kLossStats || P::GROUP == kRowGroups) {
+    if constexpr (P::EPI == kLossStats) {
         return hipErrorInvalidValue;          // never split
     } else {
         constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
@@ -1268,38 +1194,6 @@ hipError_t launch_pair_t(GemmArgs A, GemmArgs B, const Cut& cut, hipStream_t s)
     if (e != hipSuccess || A.splits == 1) return e;
     join_kernel<P><<<n1 * 4, 256, 0, s>>>(A, n1);
     return hipGetLastError();
-}
-
-// Products of groups, all of one kind of tile.  Of rows: as many blocks as there can be
-// tiles, each group's last one not full.
-template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
-hipError_t launch_groups_of(GemmArgs A, int kind, hipStream_t s)
-{
-    const int side = kTileSide[kind], cols = EPI == kGatedFwd ? side / 2 : side;
-    A.tiles_m = (A.M + side - 1) / side;
-    A.tiles_n = (A.N + cols - 1) / cols;
-    A.first = A.ratio = 0;
-    int64_t tiles = (int64_t)A.tiles_m * A.tiles_n * A.batch;
-    if (GROUP == kRowGroups) tiles = group_tiles(A.M, A.groups, side) * A.tiles_n;
-    switch (kind) {
-    case k256: return launch_tile<Tile<T, 256, 256, 2, 4, 2, ATR, BTR, EPI, GROUP>>(A, tiles, s);
-    case k128: return launch_tile<Tile<T, 128, 128, 2, 2, 2, ATR, BTR, EPI, GROUP>>(A, tiles, s);
-    case k64: return launch_tile<Tile<T, 64, 64, 2, 2, 4, ATR, BTR, EPI, GROUP>>(A, tiles, s);
-    }
-    return hipErrorInvalidValue;
-}
-
-template <typename T>
-hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
-{
-    switch (what) {
-    case kRowsRows: return launch_groups_of<T, false, false, kPlain, kRowGroups>(A, kind, s);
-    case kRowsCols: return launch_groups_of<T, false, true, kPlain, kRowGroups>(A, kind, s);
-    case kColsCols: return launch_groups_of<T, true, true, kWide, kStepGroups>(A, kind, s);
-    case kGateUp: return launch_groups_of<T, false, false, kGatedFwd, kRowGroups>(A, kind, s);
-    case kGateUpBack: return launch_groups_of<T, false, true, kGatedBwd, kRowGroups>(A, kind, s);
-    default: return hipErrorInvalidValue;
-    }
 }
 
 template <typename T>

@@ -1,0 +1,681 @@
+// Matrix products of groups (experts): rows offsets[g] .. offsets[g + 1] - 1 of A and C
+// meet matrix g of B, or those steps of k of both operands make matrix g of C.  Loaders,
+// fragments and epilogues' formulas are those of arena_gemm.h.
+//
+// The groups are short and many, so what a tile costs beside its steps decides.  Blocks
+// are resident: each takes tile after tile, and starts the next one's first loads before it
+// writes the last.  For that the epilogue leaves the LDS alone: a lane holds four
+// neighbouring columns of a row in each fragment, and a swap of rows of lanes between two
+// fragments makes them eight of one.
+//
+// Waves whose rows all lie past the group's end only load for the others: they share a
+// SIMD with waves that do not, so such a step takes little more than half the time.
+#pragma once
+
+#include <algorithm>
+
+#include "arena_gemm.h"
+
+namespace arena {
+namespace mm {
+
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool ATR_, bool BTR_, int EPI_, int GROUP_>
+struct GroupTile {
+    typedef T_ T;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
+    static constexpr int EPI = EPI_, GROUP = GROUP_;
+    static constexpr bool kUpToN = EPI_ == kPlain || EPI_ == kWide;
+    static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    static constexpr int kCols = DUAL ? BN / 2 : BN;
+    static constexpr bool kLean = BM == 256 && (EPI == kGatedBwd || EPI == kWide);
+    static constexpr int kSegs = GROUP == kRowGroups && EPI == kPlain && BTR ? 2 : 1;    // both halves of dx
+    // blocks on a compute unit, by their LDS (the groups' table is 8 to 12 KB)
+    static constexpr int kBlocks = 2 * (BM + BN) * 128 <= 65536 ? 2 : 1;
+    static constexpr int kWavesEach = kThreads / 256 * kBlocks;
+    static constexpr int kRun = 32 * kBlocks;            // tiles that an XCD has in work at once
+};
+
+// The q-th tile of XCD x, -1 past its last: runs of RUN tiles go to the XCDs in turn, and
+// what is left in eighths.  An eighth of all tiles to each would give the XCD with the longest
+// groups of steps half as much again to do (8 experts of 16384 rows, 4096 x 10944: 1988 us
+// so, in runs 1455), and takes 5 to 7 % longer with groups of rows too, where the XCDs then
+// read different experts at a time.
+template <int RUN>
+__device__ __forceinline__ int tile_of_xcd(int x, int q, int tiles)
+{
+    const int whole = tiles / (8 * RUN);
+    if (q < whole * RUN) return (q / RUN * 8 + x) * RUN + q % RUN;
+    const int r = q - whole * RUN, rest = tiles - whole * 8 * RUN, per = rest >> 3, more = rest & 7;
+    return r < per + (x < more ? 1 : 0) ? whole * 8 * RUN + x * per + min(x, more) + r : -1;
+}
+
+constexpr int kMostGroups = 1024;
+
+// Groups of rows: their first rows and ends, and how many tile rows end with the group.
+struct GroupTable {
+    int first[kMostGroups], end[kMostGroups];
+    int tiles[kMostGroups];
+};
+
+// Offset g, held inside 0 .. rows whatever the offsets are.
+__device__ __forceinline__ int group_end(const int32_t* offsets, int g, int rows)
+{
+    return min(max(offsets[g], 0), rows);
+}
+
+// Groups of steps: first steps and ends.
+struct StepTable {
+    int first[kMostGroups], end[kMostGroups];
+};
+
+template <bool ROWS>
+struct TableOf {
+    typedef StepTable Type;
+};
+
+template <>
+struct TableOf<true> {
+    typedef GroupTable Type;
+};
+
+// Rows of group g and the tile rows that they make.
+template <int BM>
+__device__ __forceinline__ int tile_rows(const GemmArgs& A, int g, int* lo, int* hi)
+{
+    *lo = *hi = 0;
+    if (g < A.groups) {
+        *lo = group_end(A.offsets, g, A.M);
+        *hi = max(*lo, group_end(A.offsets, g + 1, A.M));
+    }
+    return (*hi - *lo + BM - 1) / BM;
+}
+
+// Fills the table (one wave) and returns how many tile rows there are, at most `most`:
+// groups that overlap could have more than a launch counts.
+template <int BM>
+__device__ __forceinline__ int fill_table(const GemmArgs& A, GroupTable* table, int lane, int most)
+{
+    int total = 0;
+    for (int g0 = 0; g0 < A.groups; g0 += 64) {
+        int lo, hi;
+        const int mine = tile_rows<BM>(A, g0 + lane, &lo, &hi);
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int w = __shfl_up(sum, d, 64);
+            sum += lane >= d ? w : 0;
+        }
+        if (g0 + lane < A.groups) {
+            table->first[g0 + lane] = lo;
+            table->end[g0 + lane] = hi;
+            table->tiles[g0 + lane] = min(most, total + sum);
+        }
+        total = min(most, total + __builtin_amdgcn_readlane(sum, 63));
+    }
+    return total;
+}
+
+// A tile: its place, its steps and its operands' first addresses.
+struct Work {
+    int m0, n0, m_end, z;       // z: group, or with pairs twice that and which of the two
+    int part;                   // of a split k
+    int steps, sps, K;          // steps of all segments, of one, and k of a segment
+    int s0;                     // first step of the part
+};
+
+// The loader of arena_gemm.h, with its lanes' part apart.
+template <typename P, int R, bool TR, bool DUAL>
+struct GroupLoader : Loader<P, R, TR, DUAL> {
+    typedef Loader<P, R, TR, DUAL> Base;
+    __device__ __forceinline__ void lanes(int) {}
+    __device__ __forceinline__ void start(int tid, int first, int n, int64_t ld) { Base::init(tid, first, n, ld); }
+    __device__ __forceinline__ int64_t pitch() const { return Base::step; }
+};
+
+// The same in two registers a lane: where a lane's chunks lie is worked out again for every
+// load.  That costs a tenth of the plain products' time, but with the gated backward epilogue
+// a 256 x 256 tile (128 sums, 96 of fragments) would fetch them from memory in every step,
+// behind the loads in flight.
+template <typename P, int R, bool TR, bool DUAL>
+struct LeanLoader {
+    static constexpr int kThreads = P::kThreads;
+    static constexpr int kChunks = R * 8 / kThreads;
+    static constexpr int kEach = TR ? kThreads * 8 / R : kThreads / 8;       // rows of the tile (of k: TR) that one load covers
+    static constexpr int kGran = R / 16;
+    int lane_row, lane_at;       // row within a load; byte offset of the chunk in it (TR: its column before the swizzle of `it`)
+    int row0, ld, last;
+
+    __device__ __forceinline__ void lanes(int tid)
+    {
+        if (TR) {
+            lane_row = tid / (R / 8);
+            const int pos = tid % (R / 8), f = ((lane_row & 3) | (lane_row >> 3 & 3) << 2) & (kGran - 1);
+            lane_at = ((pos >> 1 ^ f) << 4) + ((pos & 1) << 3);
+        } else {
+            const int r = tid >> 3;
+            static_assert(!DUAL || kEach % (P::BN / P::WN / 2) == 0, "a load's rows are of the gate or of the up matrix, or of both alike");
+            lane_row = DUAL ? Dual<P::BN / P::WN>::row(r) : r;
+            lane_at = ((tid & 7) ^ (r & 7)) << 4;
+        }
+    }
+    __device__ __forceinline__ void start(int, int first, int n, int64_t ld_)
+    {
+        ld = (int)ld_;
+        row0 = first;
+        last = n - first;
+    }
+    __device__ __forceinline__ int64_t pitch() const { return TR ? (int64_t)ld * (2 * kBK) : 2 * kBK; }
+    __device__ __forceinline__ const char* base(const void* p, int64_t from) const
+    {
+        const char* q = (const char*)p + 2 * from;
+        return TR ? q + 2 * (int64_t)row0 : q + 2 * (int64_t)row0 * ld;
+    }
+    template <bool TAIL>
+    __device__ __forceinline__ void fetch(const char* p0, const char* p1, char* lds, int tid, int left) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        int row = lane_row, at = lane_at;
+        asm volatile("" : "+v"(row), "+v"(at));       // not kept over the steps
+#pragma unroll
+        for (int it = 0; it < kChunks; ++it) {
+            const char* p = p0;
+            if (DUAL) p = Dual<P::BN / P::WN>::up(it * kEach + wave * 8) ? p1 : p0;
+            uint32_t off;
+            int k;
+            if (TR) {
+                k = row + it * kEach;
+                // f of row + it kEach differs from that of row in the bits that kEach moves
+                static_assert(kEach % 4 == 0 && (kEach % 32 == 0 || kEach == 16 || kEach == 8), "f over the loads");
+                const int col = at ^ (kEach % 32 == 0 ? 0 : ((it * kEach >> 3 & 3) << 2 & (kGran - 1)) << 4);
+                off = (uint32_t)k * (uint32_t)(ld * 2) + (uint32_t)(col < last ? col : 0) * 2;
+            } else {
+                k = at >> 1;
+                const int r = DUAL ? Dual<P::BN / P::WN>::row(it * kEach) : it * kEach;
+                off = (uint32_t)min(row + r, last - 1) * (uint32_t)(ld * 2) + (uint32_t)at;
+            }
+            const char* src = p + off;
+            if (TAIL && k >= left) src = (const char*)&g_zero_chunk;
+            load_to_lds(src, lds + (it * kThreads + wave * 64) * 16);
+        }
+    }
+};
+
+template <typename P, int R, bool TR, bool DUAL, bool LEAN>
+struct LoaderOf {
+    typedef GroupLoader<P, R, TR, DUAL> Type;
+};
+
+template <typename P, int R, bool TR, bool DUAL>
+struct LoaderOf<P, R, TR, DUAL, true> {
+    typedef LeanLoader<P, R, TR, DUAL> Type;
+};
+
+// Four columns of two fragments j and j + 1 in lanes of rows of 16 (columns 4 r + 0..3 of
+// row r) become eight of one: rows 0 and 2 hold columns 0..7 and 8..15 of fragment j, rows
+// 1 and 3 those of fragment j + 1.
+__device__ __forceinline__ void eight_columns(const f32x4& a, const f32x4& b, float (&v)[8])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(a[q]),
+                                                                                   __float_as_uint(b[q]), false, false));
+        v[q] = __uint_as_float(w[0]);
+        v[4 + q] = __uint_as_float(w[1]);
+    }
+}
+
+// tiles: of groups of steps, all of them (parts of k behind each other); of groups of rows,
+// the most there can be.
+template <typename P>
+__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GemmArgs A, const int tiles)
+{
+    typedef typename P::T T;
+    constexpr bool kRows = P::GROUP == kRowGroups;
+    __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
+    __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
+    __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
+    __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
+    __shared__ typename TableOf<kRows>::Type table;
+    auto bufa = [&](int i) { return i == 0 ? sa0 : sa1; };
+    auto bufb = [&](int i) { return i == 0 ? sb0 : sb1; };
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / P::WN, wn = wave % P::WN;
+    int n_tiles = tiles;
+    if constexpr (kRows) {
+        __shared__ int rows;
+        if (wave == 0) {
+            const int total = fill_table<P::BM>(A, &table, lane, quotient(tiles, A.tiles_n));
+            if (lane == 0) rows = total;
+        }
+        __syncthreads();
+        n_tiles = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
+    } else {
+        for (int g = tid; g < A.groups; g += P::kThreads) {
+            // of no steps there need be no offsets
+            const int lo = A.K > 0 ? group_end(A.offsets, g, A.K) : 0;
+            table.first[g] = lo;
+            table.end[g] = A.K > 0 ? max(lo, group_end(A.offsets, g + 1, A.K)) : 0;
+        }
+        __syncthreads();
+    }
+
+    const int xcd = blockIdx.x & 7;
+    int q = blockIdx.x >> 3;
+    // The tile that comes next; false if there is none.
+    auto next_work = [&](Work* w) {
+        int tile = tile_of_xcd<P::kRun>(xcd, q, n_tiles);
+        q += gridDim.x >> 3;
+        if (tile < 0) return false;
+        int band_rows, in;
+        w->part = 0;
+        w->K = A.K;
+        if constexpr (kRows) {
+            int below = 0;
+            for (int g0 = 0;; g0 += 64) {
+                const int ends = g0 + lane < A.groups ? table.tiles[g0 + lane] : 0x7fffffff;
+                const int first = g0 + lane < A.groups ? table.first[g0 + lane] : 0;
+                const uint64_t past = __ballot(tile < (int64_t)ends * A.tiles_n);
+                if (past) {
+                    const int l = __ffsll((unsigned long long)past) - 1;
+                    if (l > 0) below = __builtin_amdgcn_readlane(ends, l - 1);
+                    w->z = g0 + l;
+                    w->m0 = __builtin_amdgcn_readlane(first, l);
+                    band_rows = __builtin_amdgcn_readlane(ends, l) - below;
+                    break;
+                }
+                below = __builtin_amdgcn_readlane(ends, 63);
+            }
+            in = tile - below * A.tiles_n;
+        } else {
+            const int each = A.tiles_m * A.tiles_n, all = each * A.batch;
+            if (A.splits > 1) {
+                w->part = quotient(tile, all);
+                tile -= w->part * all;
+            }
+            w->z = quotient(tile, each);
+            w->m0 = 0;
+            band_rows = A.tiles_m;
+            in = tile - w->z * each;
+        }
+        // bands of 8 tile rows
+        const int band = 8 * A.tiles_n, b = quotient(in, band), at = in - b * band;
+        const int high = min(8, band_rows - b * 8), tn = quotient(at, high);
+        const int tm = b * 8 + at - tn * high;
+        w->n0 = tn * P::kCols;
+        w->m_end = A.M;
+        if constexpr (kRows) w->m_end = __builtin_amdgcn_readfirstlane(table.end[w->z]);
+        w->m0 += tm * P::BM;
+        return true;
+    };
+
+    typename LoaderOf<P, P::BM, P::ATR, false, P::kLean>::Type la;
+    typename LoaderOf<P, P::BN, P::BTR, P::DUAL, P::kLean>::Type lb;
+    la.lanes(tid);
+    lb.lanes(tid);
+    Frags<P, P::BM, P::ATR> fa;
+    Frags<P, P::BN, P::BTR> fb;
+    fa.init(lane, wm * (P::BM / P::WM));
+    fb.init(lane, wn * (P::BN / P::WN));
+    const char *a0, *a1, *b0, *b1;        // of the segments, or b1 of the up matrix
+    auto begin = [&](Work* w) {
+        int k_from = 0;
+        if (!kRows) {
+            const int g = w->z >> A.pairs;
+            k_from = __builtin_amdgcn_readfirstlane(table.first[g]);
+            w->K = __builtin_amdgcn_readfirstlane(table.end[g]) - k_from;
+        }
+        w->sps = (w->K + kBK - 1) / kBK;
+        w->steps = w->sps * P::kSegs;
+        w->s0 = 0;
+        if (!kRows && A.splits > 1) {
+            const int per = quotient(w->steps + A.splits - 1, A.splits);
+            w->s0 = min(w->part * per, w->steps);
+            w->steps = min(per, w->steps - w->s0);
+        }
+        la.start(tid, w->m0, w->m_end, A.lda);
+        lb.start(tid, w->n0, A.N, A.ldb);
+        const int sel = !kRows && A.pairs ? w->z & 1 : 0;
+        a0 = la.base(A.a[sel], kRows ? 0 : k_from * A.lda);
+        b0 = lb.base(A.b[sel], kRows ? w->z * A.sb : k_from * A.ldb);
+        a1 = P::kSegs == 2 ? la.base(A.a[1], 0) : a0;
+        b1 = P::kSegs == 2 || P::DUAL ? lb.base(A.b[1], w->z * A.sb) : b0;
+    };
+    auto fetch = [&](const Work& w, int step, char* sa, char* sb) {
+        int at = w.s0 + step;
+        const char *pa = a0, *pb = b0;
+        if (P::kSegs == 2 && at >= w.sps) {
+            at -= w.sps;
+            pa = a1;
+            pb = b1;
+        }
+        const int left = w.K - at * kBK;
+        pa += at * la.pitch();
+        pb += at * lb.pitch();
+        const char* pu = P::DUAL ? b1 + at * lb.pitch() : pb;
+        if (left < kBK) {
+            la.template fetch<true>(pa, pa, sa, tid, left);
+            lb.template fetch<true>(pb, pu, sb, tid, left);
+        } else {
+            la.template fetch<false>(pa, pa, sa, tid, left);
+            lb.template fetch<false>(pb, pu, sb, tid, left);
+        }
+    };
+
+    f32x4 acc[P::FM][P::FN];
+    typename T::V8 fa0[P::FM], fb0[P::FN], fa1[P::FM], fb1[P::FN];    // fragments of the step's halves
+    auto read = [&](const char* sa, const char* sb, int kk, typename T::V8* a, typename T::V8* b) {
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) b[j] = fb.get(sb, j, kk);
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i) a[i] = fa.get(sa, i, kk);
+    };
+    auto multiply = [&](const typename T::V8* a, const typename T::V8* b) {
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) acc[i][j] = T::mfma(b[j], a[i], acc[i][j]);
+    };
+    auto weave = [&]() {
+        constexpr int reads = P::FM * (P::ATR ? 2 : 1) + P::FN * (P::BTR ? 2 : 1), products = P::FM * P::FN;
+        constexpr int each = products / reads > 0 ? products / reads : 1;
+#pragma unroll
+        for (int i = 0; i < reads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);          // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, each, 0);       // products
+        }
+    };
+    // Waits for a step's loads.  In a tile's first step the stores of the tile before, which
+    // were issued later, may be left: operations complete in order.  kStores is the least
+    // that a whole tile's epilogue issues; after another one everything is awaited.
+    constexpr int kStores = P::FM * P::FN / (P::DUAL ? 4 : 2);
+    static_assert(P::FM % 2 == 0 && kStores < 64, "rows in pairs, stores counted in six bits");
+    bool stored = false, idle = false;
+    auto arrive = [&](int step) {
+        asm volatile("" ::: "memory");
+        if (stored && step == 0) wait_loads<kStores>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // One step, from buffer u: see tile_product in arena_gemm.h.
+    auto turn = [&](const Work& w, int step, int u, bool first) {
+        arrive(step);
+        if (step + 1 < w.steps) fetch(w, step + 1, bufa(u ^ 1), bufb(u ^ 1));
+        if (kRows && idle) return;
+        __builtin_amdgcn_sched_barrier(0);
+        read(bufa(u), bufb(u), 0, fa0, fb0);
+        if (!first) multiply(fa1, fb1);
+        weave();
+        __builtin_amdgcn_sched_barrier(0);
+        read(bufa(u), bufb(u), 1, fa1, fb1);
+        multiply(fa0, fb0);
+        weave();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    Work w;
+    if (!next_work(&w)) return;
+    begin(&w);
+    if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        const int steps = w.steps;
+        idle = kRows && w.m0 + wm * (P::BM / P::WM) >= w.m_end;
+        if (steps > 0) {
+            turn(w, 0, 0, true);
+            for (int s = 1; s < steps; s += 2) {
+                turn(w, s, 1, false);
+                if (s + 1 < steps) turn(w, s + 1, 0, false);
+            }
+        }
+        // every wave holds its last fragments: the buffers are free for the next tile
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);         // LDS reads
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (steps > 0 && !idle) multiply(fa1, fb1);
+        const Work done = w;
+        const bool more = next_work(&w);
+        if (more) {
+            begin(&w);
+            if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+
+        // A lane holds row lane & 15 and columns 4 (lane >> 4) + 0..3 of each fragment.
+        constexpr int kAcross = P::DUAL ? P::FN / 4 : P::FN / 2;
+        int l = lane;
+        asm volatile("" : "+v"(l));       // places are worked out here, not kept over the steps
+        const int mw = done.m0 + wm * (P::BM / P::WM) + (l & 15);
+        const int nw = done.n0 + wn * (P::DUAL ? P::BN / P::WN / 2 : P::BN / P::WN) + 16 * (l >> 4 & 1) + 8 * (l >> 5);
+        const int n_end = P::kUpToN ? A.N : A.pad;
+        auto row_out = [&](int m, const f32x4 (&row)[P::FN]) {
+            Side<T, P::EPI> side[kAcross];
+            if (P::EPI == kGatedBwd || (P::EPI == kWide && A.beta != 0.0f && A.splits <= 1))
+#pragma unroll
+                for (int j = 0; j < kAcross; ++j)
+                    if (m < done.m_end && nw + j * 32 < n_end) side[j].load(A, done.z, m, nw + j * 32);
+#pragma unroll
+            for (int j = 0; j < kAcross; ++j) {
+                const int n = nw + j * 32;
+                float v[8], u[8];
+                eight_columns(row[2 * j], row[2 * j + 1], v);
+                if constexpr (P::DUAL) eight_columns(row[2 * (j + kAcross)], row[2 * (j + kAcross) + 1], u);
+                if (m >= done.m_end || n >= n_end) continue;
+                if (!kRows && A.splits > 1) {
+                    const int64_t t = ((int64_t)done.part * A.batch + done.z) * (A.tiles_m * A.tiles_n) +
+                                      done.m0 / P::BM * A.tiles_n + done.n0 / P::kCols;
+                    put(A.part + t * (P::BM * P::BN) + (m - done.m0) * P::kCols + n - done.n0, v, 8);
+                } else if constexpr (P::EPI == kGatedFwd) {
+                    gated_fwd_out<T>(A, m, n, v, u);
+                } else if constexpr (P::EPI == kGatedBwd) {
+                    gated_bwd_out<T>(A, m, n, v, side[j]);
+                } else if constexpr (P::EPI == kWide) {
+                    plain_out<T>(A, done.z, m, n, v, side[j]);
+                } else {
+                    put((typename T::E*)A.c[0] + (int64_t)m * A.ldc + n, v, A.N - n);
+                }
+            }
+        };
+        if constexpr (P::EPI == kGatedFwd || P::EPI == kGatedBwd) {
+            // Unrolled over all rows the activations would not fit the instruction cache:
+            // two rows at a time, the others move up.
+#pragma unroll 1
+            for (int i = 0; i < P::FM; i += 2) {
+                row_out(mw + i * 16, acc[0]);
+                row_out(mw + i * 16 + 16, acc[1]);
+#pragma unroll
+                for (int k = 0; k + 2 < P::FM; ++k)
+#pragma unroll
+                    for (int j = 0; j < P::FN; ++j) acc[k][j] = acc[k + 2][j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::FM; ++i) row_out(mw + i * 16, acc[i]);
+        }
+        if (!more) return;
+        stored = done.m0 + P::BM <= done.m_end && done.n0 + P::kCols <= A.N;
+    }
+}
+
+// Joins the parts of a split product of groups of steps: a thread takes eight columns of
+// a row of C, all parts in their order.
+template <typename P>
+__global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
+{
+    typedef typename P::T T;
+    const int chunks = (A.N + 7) / 8;
+    const int64_t n = (int64_t)A.batch * A.M * chunks;
+    const int64_t each = (int64_t)A.batch * A.tiles_m * A.tiles_n * (P::BM * P::BN);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / chunks;
+        const int c = (int)(i - row * chunks) * 8, z = (int)(row / A.M), m = (int)(row - (int64_t)z * A.M);
+        const float* p = A.part + (((int64_t)z * A.tiles_m + m / P::BM) * A.tiles_n + c / P::kCols) * (P::BM * P::BN) +
+                         (m % P::BM) * P::kCols + c % P::kCols;
+        float v[8] = {};
+        for (int s = 0; s < A.splits; ++s) {
+            float w[8];
+            get(p + s * each, w, 8);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] += w[r];
+        }
+        Side<T, P::EPI> side;
+        side.load(A, z, m, c);
+        plain_out<T>(A, z, m, c, v, side);
+    }
+}
+
+template <typename P>
+hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
+{
+    A.tiles_m = (A.M + P::BM - 1) / P::BM;
+    A.tiles_n = (A.N + P::kCols - 1) / P::kCols;
+    int64_t tiles = P::GROUP == kRowGroups ? group_tiles(A.M, A.groups, P::BM) * A.tiles_n
+                                           : (int64_t)A.tiles_m * A.tiles_n * A.batch * A.splits;
+    if (tiles == 0) return hipSuccess;
+    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t most = 256 * P::kBlocks, grid = (std::min(tiles, most) + 7) / 8 * 8;
+    groups_kernel<P><<<(unsigned)grid, P::kThreads, 0, s>>>(A, (int)tiles);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || A.splits <= 1) return e;
+    if constexpr (P::GROUP == kStepGroups) {
+        const int64_t blocks = ((int64_t)A.batch * A.M * ((A.N + 7) / 8) + 255) / 256;
+        groups_join_kernel<P><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, s>>>(A);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// Few rows: as skinny_kernel of arena_gemm.h, for 16 columns of C and a group that has rows,
+// 16 of its rows at a time.  Bound by the read of the groups' weights: two experts of 4096 x
+// 10944 in bfloat16 read 359 MB of gate and up weights in 68 us (5.3 TB/s) and 179 MB of down
+// weights in 37 us (4.8 TB/s).
+template <typename T, bool DUAL, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArgs A)
+{
+    typedef typename T::E E;
+    typedef typename T::V8 V8;
+    constexpr int NB = DUAL ? 2 : 1;
+    __shared__ f32x4 part[WAVES][NB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the blockIdx.y-th group with rows
+    int group = -1, lo = 0, hi = 0, left = blockIdx.y;
+    for (int g0 = 0; g0 < A.groups; g0 += 64) {
+        int first, end;
+        (void)tile_rows<1>(A, g0 + lane, &first, &end);
+        uint64_t some = __ballot(end > first);
+        const int n = __popcll(some);
+        if (left >= n) {
+            left -= n;
+            continue;
+        }
+        for (; left > 0; --left) some &= some - 1;
+        const int l = __ffsll((unsigned long long)some) - 1;
+        group = g0 + l;
+        lo = __builtin_amdgcn_readlane(first, l);
+        hi = __builtin_amdgcn_readlane(end, l);
+        break;
+    }
+    if (group < 0) return;
+    const int n0 = blockIdx.x * 16, kc = (lane >> 4) * 8;
+    const int row = min(n0 + (lane & 15), A.N - 1);
+    const E* w[NB];
+    w[0] = (const E*)A.b[0] + group * A.sb + (int64_t)row * A.ldb + kc;
+    if (DUAL) w[NB - 1] = (const E*)A.b[1] + group * A.sb1 + (int64_t)row * A.ldb1 + kc;
+    constexpr int U = 4;          // steps of 32 in flight
+    const int steps = (A.K + 31) / 32, per = (steps + WAVES - 1) / WAVES;
+    const int begin = wave * per * 32, end = min(A.K, begin + per * 32);
+    for (int m0 = lo; m0 < hi; m0 += 16) {
+        const E* x = (const E*)A.a[0] + (int64_t)min(m0 + (lane & 15), hi - 1) * A.lda + kc;
+        f32x4 acc[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = f32x4{0, 0, 0, 0};
+        int k = begin;
+        for (; k + 32 * U <= end; k += 32 * U) {
+            V8 wv[NB][U], xv[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) __builtin_memcpy(&wv[b][i], w[b] + k + 32 * i, 16);
+                __builtin_memcpy(&xv[i], x + k + 32 * i, 16);
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) acc[b] = T::mfma(wv[b][i], xv[i], acc[b]);
+        }
+        for (; k < end; k += 32) {
+            const int rest = A.K - k - kc;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) acc[b] = T::mfma(load_k<T>(w[b] + k, rest), load_k<T>(x + k, rest), acc[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) part[wave][b][lane] = acc[b];
+        __syncthreads();
+        if (wave == 0) {
+            const int m = m0 + (lane & 15), n = n0 + 4 * (lane >> 4);
+            f32x4 v = part[0][0][lane], u = part[0][NB - 1][lane];
+#pragma unroll
+            for (int q = 1; q < WAVES; ++q) {
+                v += part[q][0][lane];
+                if (DUAL) u += part[q][NB - 1][lane];
+            }
+            float fv[4], fu[4];
+            *(f32x4*)fv = v;
+            *(f32x4*)fu = u;
+            if constexpr (DUAL) {
+                if (m < hi && n < A.pad) gated_fwd_out<T>(A, m, n, fv, fu);
+            } else {
+                if (m < hi && n < A.N) put((E*)A.c[0] + (int64_t)m * A.ldc + n, fv, A.N - n);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T, bool DUAL, int WAVES>
+hipError_t launch_skinny_groups_n(const GemmArgs& A, hipStream_t s)
+{
+    const dim3 grid((A.N + 15) / 16, A.groups < A.M ? A.groups : A.M);
+    skinny_groups_kernel<T, DUAL, WAVES><<<grid, 64 * WAVES, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_skinny_groups_t(const GemmArgs& A, bool dual, hipStream_t s)
+{
+    return dual ? launch_skinny_groups_n<T, true, 8>(A, s) : launch_skinny_groups_n<T, false, 8>(A, s);
+}
+
+template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
+hipError_t launch_groups_of(const GemmArgs& A, int kind, hipStream_t s)
+{
+    switch (kind) {
+    case kGroup256: return launch_group_tile<GroupTile<T, 256, 256, 2, 4, ATR, BTR, EPI, GROUP>>(A, s);
+    case kGroup128: return launch_group_tile<GroupTile<T, 128, 128, 2, 2, ATR, BTR, EPI, GROUP>>(A, s);
+    case kGroup64x128: return launch_group_tile<GroupTile<T, 64, 128, 2, 2, ATR, BTR, EPI, GROUP>>(A, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
+{
+    switch (what) {
+    case kRowsRows: return launch_groups_of<T, false, false, kPlain, kRowGroups>(A, kind, s);
+    case kRowsCols: return launch_groups_of<T, false, true, kPlain, kRowGroups>(A, kind, s);
+    case kColsCols: return launch_groups_of<T, true, true, kWide, kStepGroups>(A, kind, s);
+    case kGateUp: return launch_groups_of<T, false, false, kGatedFwd, kRowGroups>(A, kind, s);
+    case kGateUpBack: return launch_groups_of<T, false, true, kGatedBwd, kRowGroups>(A, kind, s);
+    default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace mm
+}  // namespace arena

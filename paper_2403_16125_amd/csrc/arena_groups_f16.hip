@@ -1,5 +1,5 @@
 // The experts' tiled products in float16.
-#include "arena_gemm.h"
+#include "arena_groups.h"
 
 namespace arena {
 namespace mm {
@@ -7,6 +7,11 @@ namespace mm {
 hipError_t launch_groups_f16(const GemmArgs& A, Product what, int kind, hipStream_t s)
 {
     return launch_groups_t<F16>(A, what, kind, s);
+}
+
+hipError_t launch_skinny_groups_f16(const GemmArgs& A, bool dual, hipStream_t s)
+{
+    return launch_skinny_groups_t<F16>(A, dual, s);
 }
 
 }  // namespace mm

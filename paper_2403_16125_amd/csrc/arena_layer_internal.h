@@ -25,7 +25,7 @@ enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
 // Products whose rows or steps come in groups (experts) of lengths that only the
 // device knows: rows offsets[g] .. offsets[g + 1] - 1 of A and C meet matrix g of B, or
 // those steps of k of both operands make matrix g of C.
-enum Group { kNoGroups = 0, kRowGroups = 1, kStepGroups = 2 };
+enum Group { kRowGroups = 1, kStepGroups = 2 };
 
 // A token as the products of a loss's gradient read it.  target < 0: left out of the loss.
 struct LossRow {
@@ -41,7 +41,7 @@ struct GemmArgs {
     const void* b[2];
     void* c[2];
     int64_t lda, ldb, ldc;    // elements
-    int64_t ldb1;             // few tokens: of b[1]
+    int64_t ldb1, sb1;        // few tokens: of b[1]
     int64_t sa, sb, sc;       // batch strides, elements
     int32_t M, N, K;
     int32_t nseg, pairs, batch;
@@ -127,10 +127,18 @@ constexpr int64_t group_tiles(int64_t M, int64_t groups, int64_t side)
     return M / side + (groups < M ? groups : M);
 }
 
+// Tiles of the products of groups, two buffers each: 256 x 256 (8 waves, one block on a
+// compute unit), 128 x 128 and 64 x 128 (4 waves, two blocks).
+enum GroupKind { kGroup256 = 0, kGroup128, kGroup64x128, kGroupKinds };
+constexpr int kGroupRows[kGroupKinds] = {256, 128, 64}, kGroupCols[kGroupKinds] = {256, 128, 128};
+
 // The products of experts: C of groups of rows (gate and up, down, and the gradients of
-// both operands' inner sides), C of groups of steps (the weights' gradients, wide).  One
-// kind of tile for the whole; splits of k with groups of steps only.
+// both operands' inner sides), C of groups of steps (the weights' gradients, wide: beta e
+// and the type of C).  kind: of GroupKind; splits of k with groups of steps only.
 hipError_t launch_groups(const GemmArgs& A, int dtype, Product what, int kind, hipStream_t s);
+
+// Few rows a group: C = A B^T without LDS tiles; dual: the gated forward product.
+hipError_t launch_skinny_groups(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
 
 // The products of a loss: the logits' statistics, their gradient (what: kLossLogits,
 // kLossGradient: one kind of tile), and the gradients of both operands (wide).

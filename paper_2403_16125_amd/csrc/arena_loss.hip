@@ -60,7 +60,8 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(const LossArgs A)
     const float lse = (most == -INFINITY ? 0.0f : most) + logf(sum);
     const int64_t target = target_of(A, t);
     float loss = 0.0f;
-    if (target != A.ignore) loss = target >= 0 && target < A.vocabulary ? lse - A.picked[t] : NAN;
+    // not lse - picked: of a target that has nearly all of the sum that would keep lse's rounding only
+    if (target != A.ignore) loss = target >= 0 && target < A.vocabulary ? logf(sum) + (most - A.picked[t]) : NAN;
     if (A.loss) A.loss[t] = loss;
     A.lse[t] = lse;
 }

@@ -233,12 +233,12 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
     if ((st = check_loss(c, who, f)) || (st = check_loss_grads(c, who, f, g))) return st;
     const LossBackPlan P(f, g, f->workspace);
     if ((st = check_workspace(c, who, f->workspace, f->workspace_bytes, P.w.used))) return st;
-    DeviceScope scope(arena::ctx_device(c));
-    if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
-    hipStream_t s = (hipStream_t)stream;
     const int64_t T = f->tokens, V = f->vocabulary, D = f->model;
     const bool dx = g->dx && T > 0, scaled = f->dtype == ARENA_F16 && T > 0;
     if (!dx && !g->dw) return ARENA_OK;
+    DeviceScope scope(arena::ctx_device(c));
+    if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
+    hipStream_t s = (hipStream_t)stream;
     using namespace arena::mm;
     hipError_t e = T > 0 ? pack({&P.weight}, s) : hipSuccess;
     if (e) return hip_error(c, e, "cross entropy backward copies");

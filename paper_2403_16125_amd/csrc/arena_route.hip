@@ -360,71 +360,137 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
 
 // ---------------------------------------------------------------- moves
 
-constexpr int kChunks = 4;            // 16-byte pieces that a lane has in flight
+constexpr int kPieces = 2;            // 16-byte pieces of a row that a lane holds
+constexpr int kBatch = 4;             // choices whose rows are read before the first is used
 
 template <typename E>
-struct Chunk {
+struct Piece {
     static constexpr int n = 16 / sizeof(E);
 };
 
-// A wave's stretch of a token's row: kChunks times 64 pieces from column `from`.
+// The first value of piece i of a row of `width` values, where it is one: the last
+// piece ends with the row and takes up values of the piece before (`twice` of them), so
+// that no piece is moved value by value.  Rows may start on any value.
 template <typename E>
-__device__ __forceinline__ void dispatch_row(const MoveArgs& A, int64_t t, int from, int lane)
+__device__ __forceinline__ bool piece_of(int i, int width, int* c, int* twice)
 {
-    constexpr int N = Chunk<E>::n;
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const E* x = (const E*)A.token + t * A.ld_token;
-    u32x4 v[kChunks];
+    constexpr int n = Piece<E>::n;
+    *c = min(i * n, width - n);
+    *twice = i * n - *c;
+    return *twice < n && *c >= 0;
+}
+
+typedef uint32_t Bits __attribute__((ext_vector_type(4), aligned(2)));
+
+template <typename E>
+__device__ __forceinline__ void fetch_piece(const E* p, E (&w)[Piece<E>::n])
+{
+    const Bits v = __builtin_nontemporal_load((const Bits*)p);
+    __builtin_memcpy(w, &v, 16);
+}
+
+// The rows of a token's choices from j on, -1 for those that are dropped or past the last.
+__device__ __forceinline__ void rows_from(const MoveArgs& A, int64_t t, int j, int (&r)[kBatch])
+{
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int c = from + (i * 64 + lane) * N;
-        if (c + N <= A.model) __builtin_memcpy(&v[i], x + c, 16);
+    for (int q = 0; q < kBatch; ++q) {
+        r[q] = j + q < A.k ? A.row[t * A.k + j + q] : -1;
+        if (r[q] >= A.rows) r[q] = -1;
+    }
+}
+
+// A wave's stretch of a token's row, copied to its choices' rows; first: its first piece.
+template <typename E>
+__device__ __forceinline__ void dispatch_row(const MoveArgs& A, int64_t t, int first, int lane)
+{
+    const E* x = (const E*)A.token + t * A.ld_token;
+    int c[kPieces], twice;
+    bool is[kPieces];
+    Bits v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        is[i] = piece_of<E>(first + i * 64 + lane, A.model, &c[i], &twice);
+        if (is[i]) v[i] = *(const Bits*)(x + c[i]);
     }
     for (int j = 0; j < A.k; ++j) {
         const int64_t r = A.row[t * A.k + j];
         if (r < 0 || r >= A.rows) continue;
         E* to = (E*)A.to_choice + r * A.ld_to_choice;
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            const int c = from + (i * 64 + lane) * N;
-            if (c + N <= A.model) __builtin_memcpy(to + c, &v[i], 16);
-            else
-                for (int q = c; q < A.model; ++q) to[q] = x[q];
-        }
+        for (int i = 0; i < kPieces; ++i)
+            if (is[i]) *(Bits*)(to + c[i]) = v[i];
     }
 }
 
 // y = sum_j w_j ys[row_j], in 32 bits and in the order of j, rounded once.
 template <typename E>
-__device__ __forceinline__ void combine_row(const MoveArgs& A, int64_t t, int from, int lane)
+__device__ __forceinline__ void combine_row(const MoveArgs& A, int64_t t, int first, int lane)
 {
-    constexpr int N = Chunk<E>::n;
-    float sum[kChunks][N];
+    constexpr int n = Piece<E>::n;
+    int c[kPieces], twice;
+    bool is[kPieces];
+    float sum[kPieces][n];
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
+    for (int i = 0; i < kPieces; ++i) {
+        is[i] = piece_of<E>(first + i * 64 + lane, A.model, &c[i], &twice);
 #pragma unroll
-        for (int q = 0; q < N; ++q) sum[i][q] = 0.0f;
-#pragma unroll 2
+        for (int q = 0; q < n; ++q) sum[i][q] = 0.0f;
+    }
+    for (int j = 0; j < A.k; j += kBatch) {
+        int r[kBatch];
+        rows_from(A, t, j, r);
+        E raw[kBatch][kPieces][n];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            if (r[b] >= 0) {
+                const E* p = (const E*)A.choice + r[b] * A.ld_choice;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+                    if (is[i]) fetch_piece(p + c[i], raw[b][i]);
+            }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            if (r[b] >= 0) {
+                const float w = A.weight ? A.weight[t * A.ld_weight + j + b] : 1.0f;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                    for (int q = 0; q < n; ++q) sum[i][q] += w * (float)raw[b][i][q];
+            }
+    }
+    E* y = (E*)A.to_token + t * A.ld_to_token;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+        if (is[i]) store(y + c[i], n, sum[i]);
+}
+
+// Rows of fewer values than a piece: a thread a value.
+template <typename E, int WHAT>
+__global__ __launch_bounds__(256) void narrow_kernel(const MoveArgs A)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = i / A.model;
+    if (t >= A.tokens) return;
+    const int c = (int)(i - t * A.model);
+    float sum = 0.0f;
     for (int j = 0; j < A.k; ++j) {
         const int64_t r = A.row[t * A.k + j];
-        if (r < 0 || r >= A.rows) continue;
-        const float w = A.weight ? A.weight[t * A.ld_weight + j] : 1.0f;
-        const E* p = (const E*)A.choice + r * A.ld_choice;
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            const int c = from + (i * 64 + lane) * N;
-            if (c >= A.model) continue;
-            float v[N];
-            fetch(p + c, A.model - c, v, 0.0f);
-#pragma unroll
-            for (int q = 0; q < N; ++q) sum[i][q] += A.weight ? w * v[q] : v[q];
+        const bool there = r >= 0 && r < A.rows;
+        const E* ys = (const E*)A.choice + r * A.ld_choice;
+        E* to = (E*)A.to_choice + r * A.ld_to_choice;
+        const E* x = (const E*)A.token + t * A.ld_token;
+        if (WHAT == 0) {
+            if (there) to[c] = x[c];
+        } else if (WHAT == 1) {
+            if (there) sum += (A.weight ? A.weight[t * A.ld_weight + j] : 1.0f) * (float)ys[c];
+        } else {
+            if (there) to[c] = (E)(A.weight[t * A.ld_weight + j] * (float)x[c]);
+            if (c != 0) continue;
+            float dot = 0.0f;
+            for (int q = 0; there && q < A.model; ++q) dot += (float)x[q] * (float)ys[q];
+            A.dweight[t * A.k + j] = dot;
         }
     }
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int c = from + (i * 64 + lane) * N;
-        if (c < A.model) store((E*)A.to_token + t * A.ld_to_token + c, A.model - c, sum[i]);
-    }
+    if (WHAT == 1) ((E*)A.to_token + t * A.ld_to_token)[c] = (E)sum;
 }
 
 // Waves take stretches of tokens in turn.
@@ -436,73 +502,98 @@ __global__ __launch_bounds__(256) void move_kernel(const MoveArgs A, int stretch
     int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (; i < n; i += step) {
         const int64_t t = stretches == 1 ? i : i / stretches;
-        const int from = (int)(i - t * stretches) * (kChunks * 64 * Chunk<E>::n);
-        if (BACK) combine_row<E>(A, t, from, lane);
-        else dispatch_row<E>(A, t, from, lane);
+        const int first = (int)(i - t * stretches) * (kPieces * 64);
+        if (BACK) combine_row<E>(A, t, first, lane);
+        else dispatch_row<E>(A, t, first, lane);
     }
 }
 
-// dys[row_j] = w_j dy and dw_j = <dy, ys[row_j]>: WAVES waves share a token, dy stays in
-// registers while the choices' rows pass.
+// dys[row_j] = w_j dy and dw_j = <dy, ys[row_j]>: WAVES waves share a token's row.
 template <typename E, int WAVES>
 __global__ __launch_bounds__(256) void combine_back_kernel(const MoveArgs A)
 {
-    constexpr int N = Chunk<E>::n, kEach = 256 / 64 / WAVES, kWide = WAVES * 64 * N * kChunks;
-    __shared__ float dots[WAVES > 1 ? WAVES : 1][64];
+    constexpr int n = Piece<E>::n, kEach = 4 / WAVES, kWide = WAVES * 64 * kPieces;
+    __shared__ float dots[4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % WAVES;
-    for (int64_t t = (int64_t)blockIdx.x * kEach + wave / WAVES; t < A.tokens; t += (int64_t)gridDim.x * kEach) {
-        const E* dy = (const E*)A.token + t * A.ld_token;
+    // a block's waves pass the barriers together, with or without a token
+    for (int64_t t0 = (int64_t)blockIdx.x * kEach; t0 < A.tokens; t0 += (int64_t)gridDim.x * kEach) {
+        const int64_t t = t0 + wave / WAVES;
         float mine = 0.0f;                  // of choice `lane`
-        for (int from = 0; from < A.model; from += kWide) {
-            float d[kChunks][N];
+        if (t < A.tokens) {
+            const E* dy = (const E*)A.token + t * A.ld_token;
+            for (int from = 0; from * n < A.model; from += kWide) {
+                int c[kPieces], twice[kPieces];
+                bool is[kPieces];
+                float d[kPieces][n];
 #pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-                const int c = from + ((i * WAVES + share) * 64 + lane) * N;
-                if (c < A.model) fetch(dy + c, A.model - c, d[i], 0.0f);
-            }
-            for (int j = 0; j < A.k; ++j) {
-                const int64_t r = A.row[t * A.k + j];
-                if (r < 0 || r >= A.rows) continue;
-                const float w = A.weight[t * A.ld_weight + j];
-                const E* p = (const E*)A.choice + r * A.ld_choice;
-                E* to = (E*)A.to_choice + r * A.ld_to_choice;
-                float dot = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int c = from + ((i * WAVES + share) * 64 + lane) * N;
-                    if (c >= A.model) continue;
-                    float v[N];
-                    fetch(p + c, A.model - c, v, 0.0f);
-#pragma unroll
-                    for (int q = 0; q < N; ++q) {
-                        dot += q < A.model - c ? d[i][q] * v[q] : 0.0f;
-                        v[q] = w * d[i][q];
-                    }
-                    store(to + c, A.model - c, v);
+                for (int i = 0; i < kPieces; ++i) {
+                    is[i] = piece_of<E>(from + (i * WAVES + share) * 64 + lane, A.model, &c[i], &twice[i]);
+                    if (is[i]) fetch(dy + c[i], n, d[i], 0.0f);
                 }
-                dot = group_sum<64>(dot);
-                if (lane == j) mine += dot;
+                for (int j = 0; j < A.k; j += kBatch) {
+                    int r[kBatch];
+                    rows_from(A, t, j, r);
+                    E raw[kBatch][kPieces][n];
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        if (r[b] >= 0) {
+                            const E* p = (const E*)A.choice + r[b] * A.ld_choice;
+#pragma unroll
+                            for (int i = 0; i < kPieces; ++i)
+                                if (is[i]) fetch_piece(p + c[i], raw[b][i]);
+                        }
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        if (r[b] >= 0) {
+                            const float w = A.weight[t * A.ld_weight + j + b];
+                            E* to = (E*)A.to_choice + r[b] * A.ld_to_choice;
+                            float dot = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < kPieces; ++i) {
+                                if (!is[i]) continue;
+                                float v[n];
+#pragma unroll
+                                for (int q = 0; q < n; ++q) {
+                                    dot += q >= twice[i] ? d[i][q] * (float)raw[b][i][q] : 0.0f;
+                                    v[q] = w * d[i][q];
+                                }
+                                store(to + c[i], n, v);
+                            }
+                            dot = group_sum<64>(dot);
+                            if (lane == j + b) mine += dot;
+                        }
+                }
             }
         }
         if (WAVES > 1) {
-            dots[share][lane] = mine;
+            dots[wave][lane] = mine;
             __syncthreads();
             mine = 0.0f;
 #pragma unroll
-            for (int s = 0; s < WAVES; ++s) mine += dots[s][lane];
+            for (int s = 0; s < WAVES; ++s) mine += dots[wave / WAVES * WAVES + s][lane];
             __syncthreads();
         }
-        if (share == 0 && lane < A.k) A.dweight[t * A.k + lane] = mine;
+        if (t < A.tokens && share == 0 && lane < A.k) A.dweight[t * A.k + lane] = mine;
     }
+}
+
+template <typename E, int WHAT>
+hipError_t launch_narrow(const MoveArgs& A, hipStream_t s)
+{
+    const int64_t blocks = (A.tokens * A.model + 255) / 256;
+    if (blocks > 0) narrow_kernel<E, WHAT><<<(unsigned)blocks, 256, 0, s>>>(A);
+    return hipGetLastError();
 }
 
 template <typename E, bool BACK>
 hipError_t launch_move(const MoveArgs& A, hipStream_t s)
 {
-    const int wide = kChunks * 64 * Chunk<E>::n, stretches = (A.model + wide - 1) / wide;
+    constexpr int wide = kPieces * 64 * Piece<E>::n;
+    if (A.model < Piece<E>::n) return launch_narrow<E, BACK ? 1 : 0>(A, s);
+    const int stretches = (A.model + wide - 1) / wide;
     const int64_t blocks = (A.tokens * stretches + 3) / 4;
     if (blocks == 0) return hipSuccess;
-    move_kernel<E, BACK><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(A, stretches);
+    move_kernel<E, BACK><<<(unsigned)(blocks < 1 << 20 ? blocks : 1 << 20), 256, 0, s>>>(A, stretches);
     return hipGetLastError();
 }
 
@@ -510,13 +601,13 @@ template <typename E>
 hipError_t launch_combine_back(const MoveArgs& A, hipStream_t s)
 {
     if (A.tokens == 0) return hipSuccess;
-    // a wave a token where that fills the card and a row fits its registers
-    if (A.tokens >= 4096 && A.model <= 64 * Chunk<E>::n * kChunks) {
-        const int64_t blocks = (A.tokens + 3) / 4;
-        combine_back_kernel<E, 1><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(A);
-    } else {
-        combine_back_kernel<E, 4><<<(unsigned)(A.tokens < 65536 ? A.tokens : 65536), 256, 0, s>>>(A);
-    }
+    constexpr int wide = kPieces * 64 * Piece<E>::n;
+    if (A.model < Piece<E>::n) return launch_narrow<E, 2>(A, s);
+    const int waves = A.model <= wide ? 1 : A.model <= 2 * wide ? 2 : 4;
+    const int64_t blocks = (A.tokens * waves + 3) / 4, grid = blocks < 1 << 20 ? blocks : 1 << 20;
+    if (waves == 1) combine_back_kernel<E, 1><<<(unsigned)grid, 256, 0, s>>>(A);
+    else if (waves == 2) combine_back_kernel<E, 2><<<(unsigned)grid, 256, 0, s>>>(A);
+    else combine_back_kernel<E, 4><<<(unsigned)grid, 256, 0, s>>>(A);
     return hipGetLastError();
 }
 

@@ -177,6 +177,8 @@ class LayerOps(ExpertOps):
     current stream, or to `stream`, on which the outputs and workspaces are then
     allocated."""
 
+    _handle = None        # of the current stream, where it can be had without an object for it (1 us)
+
     def __init__(self, device: int = 0):
         import torch
         self.torch = torch
@@ -186,6 +188,8 @@ class LayerOps(ExpertOps):
         self.ctx = arena.arena_create(device)
         self._alive = True
         self._index, self._new, self._current = int(device), torch.empty, torch.cuda.current_stream
+        self._handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._torch_current = self._current
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
     def close(self) -> None:
@@ -263,6 +267,8 @@ class LayerOps(ExpertOps):
                 if t is not None and t.requires_grad:
                     raise ValueError(f"a tensor of shape {tuple(t.shape)} requires a gradient, which these calls do not "
                                      "record: detach it, or call under torch.no_grad()")
+        if stream is None and self._handle is not None and self._current is self._torch_current:
+            return body(self._handle(self._index), *args)
         current = self._current(self._index)
         if stream is None or stream == current:
             return body(current.cuda_stream, *args)
