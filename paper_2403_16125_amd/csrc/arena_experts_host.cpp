@@ -257,30 +257,6 @@ bool direct(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts
     return Operand::direct(p, ld, cols) && (experts == 1 || stride % 8 == 0);
 }
 
-// What a kind of tile costs in microseconds (measured on one MI355X): a step of 64 of k
-// with every slot of the compute units taken and with at most one block on each, a tile
-// beside its steps, and how many blocks a compute unit holds.
-struct GroupCost {
-    double full, alone, start;
-    int slots;
-};
-constexpr GroupCost kGroupCost[arena::mm::kGroupKinds] = {
-    {1.75, 1.30, 4.0, 1}, {1.00, 0.75, 3.0, 2}, {0.80, 0.60, 2.0, 2}};
-
-// uneven: how much longer than the average one the longest of few tiles takes.
-double group_time(double tiles, double steps, int kind, int64_t splits, double bytes, double uneven)
-{
-    const GroupCost& k = kGroupCost[kind];
-    const double per = std::ceil(steps / splits), values = (double)arena::mm::kGroupRows[kind] * arena::mm::kGroupCols[kind];
-    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate;
-    const double blocks = tiles * splits, round = kUnits * k.slots;
-    // how many tiles there are is an estimate: half a round more than they fill
-    const double t = blocks <= kUnits  ? per * uneven * k.alone + k.start + end
-                     : blocks <= round ? per * uneven * k.full + k.start + end * k.slots
-                                       : (blocks / round + 0.5) * (per * k.full + k.start + end * k.slots);
-    return kLaunch + t + (splits > 1 ? kJoin + blocks * values * 4e-6 / kJoinRate : 0.0);
-}
-
 // The kind of tile for a product of groups of rows: how they fall is not known here, so
 // each group that can have rows is taken to waste half a tile.
 int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes)
@@ -292,7 +268,7 @@ int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dua
         const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
         const double tm = std::max((double)some, (double)rows / kGroupRows[kind] + 0.5 * some);
         if (group_tiles(rows, groups, kGroupRows[kind]) * tn > 0x7fffffff) continue;
-        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0);
+        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0, false);
         if (t < least) {
             least = t;
             best = kind;
@@ -302,30 +278,11 @@ int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dua
 }
 
 // The kind of tile and the parts of k for a product of groups of steps, taken to be of
-// one length.
-struct StepCut {
-    int kind, splits;
-    int64_t part;             // bytes
-};
-
-StepCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes)
+// one length but for the longest.
+GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes)
 {
-    using namespace arena::mm;
-    StepCut best = {kGroup256, 1, 0};
-    double least = INFINITY;
-    const int64_t steps = std::max<int64_t>(1, ceil_div(rows, groups * kBK));
-    for (int kind = 0; kind < kGroupKinds; ++kind) {
-        const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * groups * pairs;
-        for (int s = 1; s <= 16 && (s == 1 || s * 4 <= steps); ++s) {
-            if (tiles * s > 0x7fffffff) continue;
-            const double t = group_time((double)tiles, (double)steps, kind, s, bytes, 1.5);
-            if (t < least) {
-                least = t;
-                best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0};
-            }
-        }
-    }
-    return best;
+    return choose_groups(M, N, std::max<int64_t>(1, ceil_div(rows, groups * arena::mm::kBK)), groups * pairs, bytes, true,
+                         1.5, false);
 }
 
 // Whether a forward pass takes the kernel for few rows, which streams the weights of one
@@ -357,7 +314,7 @@ struct ExpertsBackPlan : ExpertsPlan {
     int64_t ld;               // rows of dg and du
     void *dg, *du, *part;
     bool pair;                // both weight gradients of the first products in one launch
-    StepCut cut_up, cut_down;
+    GroupCut cut_up, cut_down;
     ExpertsBackPlan(const arena_experts_desc* d, const arena_experts_grads* g, void* base)
         : ExpertsPlan(d, false, base),
           dy(w, g->dy, g->ld_dy, d->rows, d->model, Operand::direct(g->dy, g->ld_dy, d->model))
@@ -536,7 +493,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     A.g = d->g; A.u = d->u; A.ldg = d->ld_inner;
     A.act = d->activation;
     A.pad = (int)pad8(d->inner);
-    e = P.skinny ? arena::mm::launch_skinny_groups(A, d->dtype, true, s)
+    e = P.skinny ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kGateUp, s)
                  : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
                                             choose_rows(R, E, d->inner, ceil_div(d->model, bk), true, d->g ? 4.0 : 1.0), s);
     if (e) return hip_error(c, e, "experts gate and up launch");
@@ -546,7 +503,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     B.a[0] = d->h; B.lda = d->ld_inner;
     B.b[0] = P.down.p; B.ldb = P.down.ld; B.sb = P.down.stride;
     B.c[0] = d->y; B.ldc = d->ld_y;
-    e = P.skinny ? arena::mm::launch_skinny_groups(B, d->dtype, false, s)
+    e = P.skinny ? arena::mm::launch_skinny_groups(B, d->dtype, arena::mm::kRowsRows, s)
                  : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
                                             choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0), s);
     return e == hipSuccess ? ARENA_OK : hip_error(c, e, "experts down launch");
@@ -596,7 +553,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     }
     // of every group C[m, n] = sum over its rows of a(t, m) b(t, n), beside what accumulate keeps
     auto weight = [&](const void* a0, const void* a1, int64_t lda, const void* b, int64_t ldb, int64_t M, int64_t N,
-                      void* c0, void* c1, int64_t ldc, int64_t sc, const StepCut& cut) {
+                      void* c0, void* c1, int64_t ldc, int64_t sc, const GroupCut& cut) {
         GemmArgs A = new_args(M, N, R);
         A.offsets = f->offsets; A.groups = f->experts;
         A.pairs = c1 != nullptr;

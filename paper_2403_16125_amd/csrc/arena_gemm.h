@@ -215,8 +215,6 @@ struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
     static constexpr int EPI = EPI_;
-    // of columns past N, the gated epilogues and the logits' gradient write zeros up to pad
-    static constexpr bool kUpToN = EPI_ == kPlain || EPI_ == kWide;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int kStages = STAGES_;
     // With few blocks on a compute unit a wave that issues its loads in a row
@@ -324,90 +322,6 @@ struct Side<T, kGatedBwd> {
         return __uint_as_float(__builtin_amdgcn_perm(head[r >> 1], tail[r >> 2], high | (r & 3) << 8 | 0x0c));
     }
 };
-
-// wide: as plain, the added matrix of a type of its own and of a group.
-template <typename T>
-struct Side<T, kWide> {
-    u32x4 raw[2];
-    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
-    {
-        if (A.beta == 0.0f) return;
-        const char* p = (const char*)A.e[A.pairs ? z & 1 : 0];
-        const int64_t from = (z >> A.pairs) * A.se + (int64_t)m * A.lde + n;
-        const int left = A.N - n;
-        if (A.e_f32) {
-            const uint32_t* q = (const uint32_t*)p + from;
-            if (left >= 8) __builtin_memcpy(raw, q, 32);
-            else
-#pragma unroll
-                for (int r = 0; r < 8; ++r) raw[r >> 2][r & 3] = r < left ? q[r] : 0;
-        } else {
-            const uint16_t* q = (const uint16_t*)p + from;
-            if (left >= 8) __builtin_memcpy(raw, q, 16);
-            else
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    raw[0][r] = (2 * r < left ? q[2 * r] : 0) | (2 * r + 1 < left ? (uint32_t)q[2 * r + 1] << 16 : 0);
-        }
-    }
-    __device__ __forceinline__ float get(int r, bool f32) const
-    {
-        typedef typename T::E E;
-        if (f32) return __uint_as_float(raw[r >> 2][r & 3]);
-        const uint16_t h = (uint16_t)(raw[0][r >> 1] >> (16 * (r & 1)));
-        E e;
-        __builtin_memcpy(&e, &h, 2);
-        return (float)e;
-    }
-};
-
-template <typename T>
-__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[8],
-                                          const Side<T, kWide>& side)
-{
-    typedef typename T::E E;
-    const int left = A.N - n;
-    const int64_t at = (z >> A.pairs) * A.sc + (int64_t)m * A.ldc + n;
-    void* c = A.c[A.pairs ? z & 1 : 0];
-    const float alpha = A.factor ? A.alpha * A.factor[0] : A.alpha;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) v[r] *= alpha;
-    if (A.beta != 0.0f)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] += A.beta * side.get(r, A.e_f32);
-    if (A.out == kOutF32) put((float*)c + at, v, left);
-    else put((E*)c + at, v, left);
-}
-
-template <typename T>
-struct Side<T, kLossStats> {
-    __device__ __forceinline__ void load(const GemmArgs&, int, int, int) {}
-};
-
-// logits' gradient: the row's record.
-template <typename T>
-struct Side<T, kLossGrad> {
-    u32x4 raw;
-    __device__ __forceinline__ void load(const GemmArgs& A, int, int m, int) { raw = *(const u32x4*)(A.rows + m); }
-};
-
-// factor (exp(l - lse) - [column is the target]), zero for tokens left out of the loss,
-// whatever their logits: rounded to 16 bits as the next two products' operand.
-template <typename T>
-__device__ __forceinline__ void loss_grad_out(const GemmArgs& A, int m, int n, const float (&v)[8],
-                                              const Side<T, kLossGrad>& side)
-{
-    typedef typename T::E E;
-    const float lse = __uint_as_float(side.raw[0]), factor = __uint_as_float(side.raw[1]);
-    const int target = (int)side.raw[2], at = target - A.first_col - n;
-    float g[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const float p = __expf(v[r] - lse) - (r == at ? 1.0f : 0.0f);
-        g[r] = n + r < A.N && target >= 0 ? factor * p : 0.0f;
-    }
-    put((E*)A.c[0] + (int64_t)m * A.ldc + n, g, 8);
-}
 
 // Writes eight (or, of few rows, four) columns from n, those below N, of row m;
 // z is the batch index.  Leaves the values written in v.
@@ -648,74 +562,6 @@ struct Buffers {
     __shared__ __attribute__((aligned(16))) char sb3_[kMoreB];                                             \
     const Buffers name = {sa0_, sa1_, sb0_, sb1_, sa2_, sa3_, sb2_, sb3_}
 
-// The statistics of a tile's logits, from the sums as they lie in registers: a lane holds
-// row lane & 15 and columns 4 (lane >> 4) + 0..3 of each fragment, so of a row the lane's
-// FN 4 values, then those of four lanes, then those of the block's WN waves meet.  A row's
-// exponentials are summed beside the largest logit of its columns here; the join brings
-// the tiles' to one.  No logit but the target's is written.
-template <typename P>
-__device__ __forceinline__ void loss_stats(const GemmArgs& A, const Place& at, f32x4 (&acc)[P::FM][P::FN],
-                                           const Buffers& lds, int wm, int wn)
-{
-    const int lane = threadIdx.x & 63;
-    const int n_lane = at.n0 + wn * (P::BN / P::WN) + 4 * (lane >> 4);
-    f32x2* const each = (f32x2*)lds.a0;                  // [BM][WN]
-    static_assert(P::BM * P::WN * 8 <= P::BM * 128, "statistics fit a buffer");
-    // loads into LDS may be in flight, of other waves too
-    asm volatile("" ::: "memory");
-    wait_loads<0>();
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i) {
-        const int r = wm * (P::BM / P::WM) + i * 16 + (lane & 15), m = at.m0 + r;
-        int64_t target = -1;
-        if (m < A.M)
-            target = (A.target_wide ? ((const int64_t*)A.target)[m] : ((const int32_t*)A.target)[m]) - A.first_col - n_lane;
-        float most = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < P::FN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (n_lane + j * 16 + q < A.N) most = fmaxf(most, acc[i][j][q]);
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
-        const float by = most == -INFINITY ? 0.0f : most;       // of nothing but -inf the sum is 0
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < P::FN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (n_lane + j * 16 + q < A.N) sum += __expf(acc[i][j][q] - by);
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        if (target >= 0 && target < P::FN * 16 && (target & 12) == 0) {
-            float l = 0.0f;
-#pragma unroll
-            for (int j = 0; j < P::FN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (target == j * 16 + q) l = acc[i][j][q];
-            A.picked[m] = l;
-        }
-        if (lane < 16) each[r * P::WN + wn] = f32x2{most, sum};
-    }
-    __syncthreads();
-    for (int r = threadIdx.x; r < P::BM; r += P::kThreads) {
-        const int m = at.m0 + r;
-        if (m >= A.M) continue;
-        float most = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < P::WN; ++w) most = fmaxf(most, each[r * P::WN + w][0]);
-        const float by = most == -INFINITY ? 0.0f : most;
-#pragma unroll
-        for (int w = 0; w < P::WN; ++w) {
-            const f32x2 e = each[r * P::WN + w];
-            sum += e[0] == -INFINITY ? e[1] : e[1] * __expf(e[0] - by);
-        }
-        ((f32x2*)A.stats)[(int64_t)(at.n0 / P::kCols) * A.M + m] = f32x2{most, sum};
-    }
-}
-
 // Tile t of a launch's n_tiles; part: which of the splits of k.
 template <typename P>
 __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, const int n_tiles, const int part,
@@ -793,7 +639,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
             const int x = (at + q) * 64 + lane, m = mw + x / kChunks, n = nw + x % kChunks * 8;
-            if (m < A.M && n < (P::kUpToN ? A.N : A.pad)) to[q].load(A, zb, m, n);
+            if (m < A.M && n < (P::EPI == kPlain ? A.N : A.pad)) to[q].load(A, zb, m, n);
         }
     };
 
@@ -883,7 +729,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             *(f32x4*)u = *piece(r, CW / 8 + 2 * c);
             *(f32x4*)(u + 4) = *piece(r, CW / 8 + 2 * c + 1);
         }
-        if (m >= A.M || n >= (P::kUpToN ? A.N : A.pad)) return;
+        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) return;
         if (A.splits > 1) {
             float* to = A.part + ((int64_t)part * n_tiles + t) * (P::BM * P::BN) + (m - m0) * P::kCols + n - n0;
             put(to, v, 8);
@@ -894,9 +740,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             gated_fwd_out<T>(A, m, n, v, u);
         } else if constexpr (P::EPI == kGatedBwd) {
             gated_bwd_out<T>(A, m, n, v, from);
-        } else if constexpr (P::EPI == kLossGrad) {
-            loss_grad_out<T>(A, m, n, v, from);
-        } else if constexpr (P::EPI != kLossStats) {
+        } else {
             plain_out<T>(A, zb, m, n, v, from);
             if (mirror) {
                 *piece(r, 2 * c) = *(f32x4*)v;
@@ -904,10 +748,6 @@ __device__ __forceinline__ void tile_product(const GemmArgs& A, const int t, con
             }
         }
     };
-    if constexpr (P::EPI == kLossStats) {
-        loss_stats<P>(A, at, acc, lds, wm, wn);
-        return;
-    }
     // Loads into LDS may still be in flight here, and a wave's land in slices that
     // others write: each waits for its own before the barrier, which does not.
     asm volatile("" ::: "memory");
@@ -997,7 +837,7 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A, int n_tiles
         const float* p = part + (r0 + r) * P::kCols + c0 + c;
         float v[8] = {}, u[8] = {};
         Side<T, P::EPI> side;
-        if (m >= A.M || n >= (P::kUpToN ? A.N : A.pad)) continue;
+        if (m >= A.M || n >= (P::EPI == kPlain ? A.N : A.pad)) continue;
         side.load(A, at.z, m, n);
 #pragma unroll 4
         for (int s = 0; s < A.splits; ++s) {
@@ -1012,7 +852,6 @@ __global__ __launch_bounds__(256) void join_kernel(const GemmArgs A, int n_tiles
         }
         if constexpr (P::EPI == kGatedFwd) gated_fwd_out<T>(A, m, n, v, u);
         else if constexpr (P::EPI == kGatedBwd) gated_bwd_out<T>(A, m, n, v, side);
-        else if constexpr (P::EPI == kLossGrad) loss_grad_out<T>(A, m, n, v, side);
         else plain_out<T>(A, at.z, m, n, v, side);
         if (P::EPI == kPlain && at.mirror)
 #pragma unroll
@@ -1134,13 +973,9 @@ hipError_t launch_tile(const GemmArgs& A, int64_t n_tiles, hipStream_t s)
     gemm_kernel<P><<<dim3((unsigned)n_tiles, A.splits), P::kThreads, 0, s>>>(A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    if constexpr (P::EPI == kLossStats) {
-        return hipErrorInvalidValue;          // never split
-    } else {
-        constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
-        join_kernel<P><<<(unsigned)(n_tiles * kEach), 256, 0, s>>>(A, (int)n_tiles);
-        return hipGetLastError();
-    }
+    constexpr int kEach = (P::BM / 64) * (P::kCols < 64 ? 1 : P::kCols / 64);
+    join_kernel<P><<<(unsigned)(n_tiles * kEach), 256, 0, s>>>(A, (int)n_tiles);
+    return hipGetLastError();
 }
 
 template <typename T, bool ATR, bool BTR, int EPI>
@@ -1194,18 +1029,6 @@ hipError_t launch_pair_t(GemmArgs A, GemmArgs B, const Cut& cut, hipStream_t s)
     if (e != hipSuccess || A.splits == 1) return e;
     join_kernel<P><<<n1 * 4, 256, 0, s>>>(A, n1);
     return hipGetLastError();
-}
-
-template <typename T>
-hipError_t launch_loss_t(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
-{
-    switch (what) {
-    case kLossLogits: return launch_layout<T, false, false, kLossStats>(A, cut, s);
-    case kLossGradient: return launch_layout<T, false, false, kLossGrad>(A, cut, s);
-    case kRowsCols: return launch_layout<T, false, true, kWide>(A, cut, s);
-    case kColsCols: return launch_layout<T, true, true, kWide>(A, cut, s);
-    default: return hipErrorInvalidValue;
-    }
 }
 
 template <typename T>

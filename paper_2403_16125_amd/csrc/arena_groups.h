@@ -1,6 +1,7 @@
 // Matrix products of groups (experts): rows offsets[g] .. offsets[g + 1] - 1 of A and C
-// meet matrix g of B, or those steps of k of both operands make matrix g of C.  Loaders,
-// fragments and epilogues' formulas are those of arena_gemm.h.
+// meet matrix g of B, or those steps of k of both operands make matrix g of C.  The products
+// of a loss are of one group.  Loaders, fragments and the gated epilogues' formulas are those
+// of arena_gemm.h.
 //
 // The groups are short and many, so what a tile costs beside its steps decides.  Blocks
 // are resident: each takes tile after tile, and starts the next one's first loads before it
@@ -35,6 +36,9 @@ struct GroupTile {
     static constexpr int kBlocks = 2 * (BM + BN) * 128 <= 65536 ? 2 : 1;
     static constexpr int kWavesEach = kThreads / 256 * kBlocks;
     static constexpr int kRun = 32 * kBlocks;            // tiles that an XCD has in work at once
+    // bytes of a row that the epilogue reads, brought to the LDS with the tile's first step:
+    // read in the epilogue they would wait for the next tile's loads
+    static constexpr int kRowBytes = EPI == kLossGrad ? 16 : EPI == kLossStats ? 4 : 0;
 };
 
 // The q-th tile of XCD x, -1 past its last: runs of RUN tiles go to the XCDs in turn, and
@@ -70,14 +74,21 @@ struct StepTable {
     int first[kMostGroups], end[kMostGroups];
 };
 
-template <bool ROWS>
+struct NoTable {};
+
+template <int GROUP>
 struct TableOf {
-    typedef StepTable Type;
+    typedef NoTable Type;
 };
 
 template <>
-struct TableOf<true> {
+struct TableOf<kRowGroups> {
     typedef GroupTable Type;
+};
+
+template <>
+struct TableOf<kStepGroups> {
+    typedef StepTable Type;
 };
 
 // Rows of group g and the tile rows that they make.
@@ -116,6 +127,127 @@ __device__ __forceinline__ int fill_table(const GemmArgs& A, GroupTable* table, 
     }
     return total;
 }
+
+// wide: as plain, the added matrix of a type of its own and of a group.
+template <typename T>
+struct Side<T, kWide> {
+    u32x4 raw[2];
+    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
+    {
+        if (A.beta == 0.0f) return;
+        const char* p = (const char*)A.e[A.pairs ? z & 1 : 0];
+        const int64_t from = (z >> A.pairs) * A.se + (int64_t)m * A.lde + n;
+        const int left = A.N - n;
+        if (A.e_f32) {
+            const uint32_t* q = (const uint32_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 32);
+            else
+#pragma unroll
+                for (int r = 0; r < 8; ++r) raw[r >> 2][r & 3] = r < left ? q[r] : 0;
+        } else {
+            const uint16_t* q = (const uint16_t*)p + from;
+            if (left >= 8) __builtin_memcpy(raw, q, 16);
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    raw[0][r] = (2 * r < left ? q[2 * r] : 0) | (2 * r + 1 < left ? (uint32_t)q[2 * r + 1] << 16 : 0);
+        }
+    }
+    __device__ __forceinline__ float get(int r, bool f32) const
+    {
+        typedef typename T::E E;
+        if (f32) return __uint_as_float(raw[r >> 2][r & 3]);
+        const uint16_t h = (uint16_t)(raw[0][r >> 1] >> (16 * (r & 1)));
+        E e;
+        __builtin_memcpy(&e, &h, 2);
+        return (float)e;
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[8],
+                                          const Side<T, kWide>& side)
+{
+    typedef typename T::E E;
+    const int left = A.N - n;
+    const int64_t at = (z >> A.pairs) * A.sc + (int64_t)m * A.ldc + n;
+    void* c = A.c[A.pairs ? z & 1 : 0];
+    const float alpha = A.factor ? A.alpha * A.factor[0] : A.alpha;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] *= alpha;
+    if (A.beta != 0.0f)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] += A.beta * side.get(r, A.e_f32);
+    if (A.out == kOutF32) put((float*)c + at, v, left);
+    else put((E*)c + at, v, left);
+}
+
+// factor (exp(l - lse) - [column is the target]), zero for tokens left out of the loss,
+// whatever their logits: rounded to 16 bits as the next two products' operand.
+template <typename T>
+__device__ __forceinline__ void loss_grad_out(const GemmArgs& A, int m, int n, const float (&v)[8], const LossRow& row)
+{
+    typedef typename T::E E;
+    const float lse = row.lse, factor = row.factor;
+    const int target = row.target, at = target - A.first_col - n;
+    float g[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const float p = __expf(v[r] - lse) - (r == at ? 1.0f : 0.0f);
+        g[r] = n + r < A.N && target >= 0 ? factor * p : 0.0f;
+    }
+    put((E*)A.c[0] + (int64_t)m * A.ldc + n, g, 8);
+}
+
+// The statistics of a row's logits as they lie in the sums: a lane has columns 4 (lane >> 4) +
+// 0..3 of each fragment, from column n on; four lanes share the row.  Of those below N the
+// largest, the sum of exponentials beside it, and the target's (in A.picked[m]), if it is
+// among them.
+template <typename P>
+__device__ __forceinline__ f32x2 row_stats(const GemmArgs& A, const f32x4 (&row)[P::FN], int m, int n, int target)
+{
+    float most = -INFINITY, sum = 0.0f;
+    const bool whole = __all(n + (P::FN - 1) * 16 + 4 <= A.N);
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) most = fmaxf(most, row[j][q]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (n + j * 16 + q < A.N) most = fmaxf(most, row[j][q]);
+    }
+    most = fmaxf(most, __shfl_xor(most, 16, 64));
+    most = fmaxf(most, __shfl_xor(most, 32, 64));
+    const float by = most == -INFINITY ? 0.0f : most;       // of nothing but -inf the sum is 0
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float e = __expf(row[j][q] - by);
+            sum += whole || n + j * 16 + q < A.N ? e : 0.0f;
+        }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    const int at = target - n;
+    if (m < A.M && at >= 0 && at < P::FN * 16 && (at & 12) == 0) {
+        float l = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (at == j * 16 + q) l = row[j][q];
+        A.picked[m] = l;
+    }
+    return f32x2{most, sum};
+}
+
+struct OneFragment {
+    static constexpr int FN = 1;
+};
 
 // A tile: its place, its steps and its operands' first addresses.
 struct Work {
@@ -232,12 +364,15 @@ template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GemmArgs A, const int tiles)
 {
     typedef typename P::T T;
-    constexpr bool kRows = P::GROUP == kRowGroups;
+    constexpr bool kRows = P::GROUP == kRowGroups, kSteps = P::GROUP == kStepGroups;
     __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
     __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
-    __shared__ typename TableOf<kRows>::Type table;
+    __shared__ typename TableOf<P::GROUP>::Type table;
+    __shared__ __attribute__((aligned(16))) char rows0[P::kRowBytes ? P::BM * P::kRowBytes : 16];
+    __shared__ __attribute__((aligned(16))) char rows1[P::kRowBytes ? P::BM * P::kRowBytes : 16];
+    __shared__ f32x2 stats[P::EPI == kLossStats ? P::BM * P::WN : 1];
     auto bufa = [&](int i) { return i == 0 ? sa0 : sa1; };
     auto bufb = [&](int i) { return i == 0 ? sb0 : sb1; };
 
@@ -252,7 +387,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         }
         __syncthreads();
         n_tiles = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
-    } else {
+    }
+    if constexpr (kSteps) {
         for (int g = tid; g < A.groups; g += P::kThreads) {
             // of no steps there need be no offsets
             const int lo = A.K > 0 ? group_end(A.offsets, g, A.K) : 0;
@@ -322,7 +458,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     const char *a0, *a1, *b0, *b1;        // of the segments, or b1 of the up matrix
     auto begin = [&](Work* w) {
         int k_from = 0;
-        if (!kRows) {
+        if constexpr (kSteps) {
             const int g = w->z >> A.pairs;
             k_from = __builtin_amdgcn_readfirstlane(table.first[g]);
             w->K = __builtin_amdgcn_readfirstlane(table.end[g]) - k_from;
@@ -342,6 +478,17 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         b0 = lb.base(A.b[sel], kRows ? w->z * A.sb : k_from * A.ldb);
         a1 = P::kSegs == 2 ? la.base(A.a[1], 0) : a0;
         b1 = P::kSegs == 2 || P::DUAL ? lb.base(A.b[1], w->z * A.sb) : b0;
+    };
+    auto fetch_rows = [&](const Work& w, char* to) {
+        if (P::kRowBytes == 0 || wave >= P::BM / 64) return;
+        const int m = min(w.m0 + wave * 64 + lane, A.M - 1);
+        if (P::kRowBytes == 16) {
+            load_to_lds((const char*)(A.rows + m), to + wave * 1024);
+        } else {
+            // the lower half of a wide target: one past 32 bits is no entry and picks nothing
+            const char* p = (const char*)A.target + ((int64_t)m << (A.target_wide ? 3 : 2));
+            __builtin_amdgcn_global_load_lds((GlobalVoid*)p, (LdsVoid*)(to + wave * 256), 4, 0, 0);
+        }
     };
     auto fetch = [&](const Work& w, int step, char* sa, char* sb) {
         int at = w.s0 + step;
@@ -419,7 +566,9 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     Work w;
     if (!next_work(&w)) return;
     begin(&w);
+    fetch_rows(w, rows0);
     if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+    bool odd = false;             // which rows are the tile's
     for (;;) {
 #pragma unroll
         for (int i = 0; i < P::FM; ++i)
@@ -444,6 +593,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         const bool more = next_work(&w);
         if (more) {
             begin(&w);
+            fetch_rows(w, odd ? rows0 : rows1);
             if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -455,8 +605,13 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         const int mw = done.m0 + wm * (P::BM / P::WM) + (l & 15);
         const int nw = done.n0 + wn * (P::DUAL ? P::BN / P::WN / 2 : P::BN / P::WN) + 16 * (l >> 4 & 1) + 8 * (l >> 5);
         const int n_end = P::kUpToN ? A.N : A.pad;
+        const char* const rows = odd ? rows1 : rows0;
+        odd = !odd;
         auto row_out = [&](int m, const f32x4 (&row)[P::FN]) {
-            Side<T, P::EPI> side[kAcross];
+            constexpr int kSide = P::EPI == kLossGrad || P::EPI == kLossStats ? kPlain : P::EPI;
+            Side<T, kSide> side[kAcross];
+            LossRow record;
+            if constexpr (P::EPI == kLossGrad) record = ((const LossRow*)rows)[m - done.m0];
             if (P::EPI == kGatedBwd || (P::EPI == kWide && A.beta != 0.0f && A.splits <= 1))
 #pragma unroll
                 for (int j = 0; j < kAcross; ++j)
@@ -478,12 +633,40 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
                     gated_bwd_out<T>(A, m, n, v, side[j]);
                 } else if constexpr (P::EPI == kWide) {
                     plain_out<T>(A, done.z, m, n, v, side[j]);
+                } else if constexpr (P::EPI == kLossGrad) {
+                    loss_grad_out<T>(A, m, n, v, record);
                 } else {
                     put((typename T::E*)A.c[0] + (int64_t)m * A.ldc + n, v, A.N - n);
                 }
             }
         };
-        if constexpr (P::EPI == kGatedFwd || P::EPI == kGatedBwd) {
+        if constexpr (P::EPI == kLossStats) {
+            // the block's WN waves share a row
+            const int n = done.n0 + wn * (P::BN / P::WN) + 4 * (l >> 4);
+#pragma unroll
+            for (int i = 0; i < P::FM; ++i) {
+                const int r = wm * (P::BM / P::WM) + i * 16 + (l & 15);
+                const f32x2 e = row_stats<P>(A, acc[i], done.m0 + r, n, ((const int32_t*)rows)[r] - A.first_col);
+                if (l < 16) stats[r * P::WN + wn] = e;
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);         // LDS writes
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            for (int r = tid; r < P::BM; r += P::kThreads) {
+                if (done.m0 + r >= A.M) continue;
+                float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+                for (int x = 0; x < P::WN; ++x) most = fmaxf(most, stats[r * P::WN + x][0]);
+                const float by = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+                for (int x = 0; x < P::WN; ++x) {
+                    const f32x2 e = stats[r * P::WN + x];
+                    sum += e[0] == -INFINITY ? e[1] : e[1] * __expf(e[0] - by);
+                }
+                ((f32x2*)A.stats)[(int64_t)(done.n0 / P::kCols) * A.M + done.m0 + r] = f32x2{most, sum};
+            }
+        } else if constexpr (P::EPI == kGatedFwd || P::EPI == kGatedBwd) {
             // Unrolled over all rows the activations would not fit the instruction cache:
             // two rows at a time, the others move up.
 #pragma unroll 1
@@ -500,11 +683,11 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             for (int i = 0; i < P::FM; ++i) row_out(mw + i * 16, acc[i]);
         }
         if (!more) return;
-        stored = done.m0 + P::BM <= done.m_end && done.n0 + P::kCols <= A.N;
+        stored = P::EPI != kLossStats && done.m0 + P::BM <= done.m_end && done.n0 + P::kCols <= A.N;
     }
 }
 
-// Joins the parts of a split product of groups of steps: a thread takes eight columns of
+// Joins the parts of a split product: a thread takes eight columns of
 // a row of C, all parts in their order.
 template <typename P>
 __global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
@@ -544,7 +727,7 @@ hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
     groups_kernel<P><<<(unsigned)grid, P::kThreads, 0, s>>>(A, (int)tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits <= 1) return e;
-    if constexpr (P::GROUP == kStepGroups) {
+    if constexpr (P::EPI == kWide) {
         const int64_t blocks = ((int64_t)A.batch * A.M * ((A.N + 7) / 8) + 255) / 256;
         groups_join_kernel<P><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, s>>>(A);
         e = hipGetLastError();
@@ -552,43 +735,49 @@ hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
     return e;
 }
 
-// Few rows: as skinny_kernel of arena_gemm.h, for 16 columns of C and a group that has rows,
-// 16 of its rows at a time.  Bound by the read of the groups' weights: two experts of 4096 x
-// 10944 in bfloat16 read 359 MB of gate and up weights in 68 us (5.3 TB/s) and 179 MB of down
-// weights in 37 us (4.8 TB/s).
-template <typename T, bool DUAL, int WAVES>
+// Few rows: as skinny_kernel of arena_gemm.h, for 16 columns of C and a group that has rows
+// (offsets null: one group of all), 16 of its rows at a time; C plain, gated or the
+// statistics of a loss's logits.  Bound by the read of the weights: two experts of 4096 x
+// 10944 in bfloat16 read 359 MB of gate and up weights in 68 us (5.3 TB/s).
+template <typename T, int EPI, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArgs A)
 {
     typedef typename T::E E;
     typedef typename T::V8 V8;
+    constexpr bool DUAL = EPI == kGatedFwd;
     constexpr int NB = DUAL ? 2 : 1;
     __shared__ f32x4 part[WAVES][NB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the blockIdx.y-th group with rows
     int group = -1, lo = 0, hi = 0, left = blockIdx.y;
-    for (int g0 = 0; g0 < A.groups; g0 += 64) {
-        int first, end;
-        (void)tile_rows<1>(A, g0 + lane, &first, &end);
-        uint64_t some = __ballot(end > first);
-        const int n = __popcll(some);
-        if (left >= n) {
-            left -= n;
-            continue;
+    if (A.offsets) {
+        for (int g0 = 0; g0 < A.groups; g0 += 64) {
+            int first, end;
+            (void)tile_rows<1>(A, g0 + lane, &first, &end);
+            uint64_t some = __ballot(end > first);
+            const int n = __popcll(some);
+            if (left >= n) {
+                left -= n;
+                continue;
+            }
+            for (; left > 0; --left) some &= some - 1;
+            const int l = __ffsll((unsigned long long)some) - 1;
+            group = g0 + l;
+            lo = __builtin_amdgcn_readlane(first, l);
+            hi = __builtin_amdgcn_readlane(end, l);
+            break;
         }
-        for (; left > 0; --left) some &= some - 1;
-        const int l = __ffsll((unsigned long long)some) - 1;
-        group = g0 + l;
-        lo = __builtin_amdgcn_readlane(first, l);
-        hi = __builtin_amdgcn_readlane(end, l);
-        break;
+        if (group < 0) return;
+    } else {
+        group = 0;
+        hi = A.M;
     }
-    if (group < 0) return;
     const int n0 = blockIdx.x * 16, kc = (lane >> 4) * 8;
     const int row = min(n0 + (lane & 15), A.N - 1);
     const E* w[NB];
     w[0] = (const E*)A.b[0] + group * A.sb + (int64_t)row * A.ldb + kc;
     if (DUAL) w[NB - 1] = (const E*)A.b[1] + group * A.sb1 + (int64_t)row * A.ldb1 + kc;
-    constexpr int U = 4;          // steps of 32 in flight
+    constexpr int U = 8 / NB;     // steps of 32 in flight
     const int steps = (A.K + 31) / 32, per = (steps + WAVES - 1) / WAVES;
     const int begin = wave * per * 32, end = min(A.K, begin + per * 32);
     for (int m0 = lo; m0 < hi; m0 += 16) {
@@ -629,8 +818,14 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArg
             float fv[4], fu[4];
             *(f32x4*)fv = v;
             *(f32x4*)fu = u;
-            if constexpr (DUAL) {
+            if constexpr (EPI == kGatedFwd) {
                 if (m < hi && n < A.pad) gated_fwd_out<T>(A, m, n, fv, fu);
+            } else if constexpr (EPI == kLossStats) {
+                const int64_t at = min(m, hi - 1);
+                const int target = ((const int32_t*)A.target)[at << A.target_wide];       // its lower half
+                const f32x4 one[1] = {v};
+                const f32x2 e = row_stats<OneFragment>(A, one, m, n, target);
+                if (lane < 16 && m < hi) ((f32x2*)A.stats)[(int64_t)blockIdx.x * A.M + m] = e;
             } else {
                 if (m < hi && n < A.N) put((E*)A.c[0] + (int64_t)m * A.ldc + n, fv, A.N - n);
             }
@@ -639,18 +834,23 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArg
     }
 }
 
-template <typename T, bool DUAL, int WAVES>
-hipError_t launch_skinny_groups_n(const GemmArgs& A, hipStream_t s)
+template <typename T, int EPI>
+hipError_t launch_skinny_groups_of(const GemmArgs& A, hipStream_t s)
 {
-    const dim3 grid((A.N + 15) / 16, A.groups < A.M ? A.groups : A.M);
-    skinny_groups_kernel<T, DUAL, WAVES><<<grid, 64 * WAVES, 0, s>>>(A);
+    const dim3 grid((A.N + 15) / 16, !A.offsets ? 1 : A.groups < A.M ? A.groups : A.M);
+    skinny_groups_kernel<T, EPI, 8><<<grid, 512, 0, s>>>(A);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_skinny_groups_t(const GemmArgs& A, bool dual, hipStream_t s)
+hipError_t launch_skinny_groups_t(const GemmArgs& A, Product what, hipStream_t s)
 {
-    return dual ? launch_skinny_groups_n<T, true, 8>(A, s) : launch_skinny_groups_n<T, false, 8>(A, s);
+    switch (what) {
+    case kRowsRows: return launch_skinny_groups_of<T, kPlain>(A, s);
+    case kGateUp: return launch_skinny_groups_of<T, kGatedFwd>(A, s);
+    case kLossLogits: return launch_skinny_groups_of<T, kLossStats>(A, s);
+    default: return hipErrorInvalidValue;
+    }
 }
 
 template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
@@ -673,6 +873,18 @@ hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_
     case kColsCols: return launch_groups_of<T, true, true, kWide, kStepGroups>(A, kind, s);
     case kGateUp: return launch_groups_of<T, false, false, kGatedFwd, kRowGroups>(A, kind, s);
     case kGateUpBack: return launch_groups_of<T, false, true, kGatedBwd, kRowGroups>(A, kind, s);
+    default: return hipErrorInvalidValue;
+    }
+}
+
+template <typename T>
+hipError_t launch_loss_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
+{
+    switch (what) {
+    case kLossLogits: return launch_groups_of<T, false, false, kLossStats, kOneGroup>(A, kind, s);
+    case kLossGradient: return launch_groups_of<T, false, false, kLossGrad, kOneGroup>(A, kind, s);
+    case kRowsCols: return launch_groups_of<T, false, true, kWide, kOneGroup>(A, kind, s);
+    case kColsCols: return launch_groups_of<T, true, true, kWide, kOneGroup>(A, kind, s);
     default: return hipErrorInvalidValue;
     }
 }

@@ -9,9 +9,9 @@ hipError_t launch_groups_f16(const GemmArgs& A, Product what, int kind, hipStrea
     return launch_groups_t<F16>(A, what, kind, s);
 }
 
-hipError_t launch_skinny_groups_f16(const GemmArgs& A, bool dual, hipStream_t s)
+hipError_t launch_skinny_groups_f16(const GemmArgs& A, Product what, hipStream_t s)
 {
-    return launch_skinny_groups_t<F16>(A, dual, s);
+    return launch_skinny_groups_t<F16>(A, what, s);
 }
 
 }  // namespace mm

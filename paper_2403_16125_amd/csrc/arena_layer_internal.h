@@ -25,7 +25,7 @@ enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
 // Products whose rows or steps come in groups (experts) of lengths that only the
 // device knows: rows offsets[g] .. offsets[g + 1] - 1 of A and C meet matrix g of B, or
 // those steps of k of both operands make matrix g of C.
-enum Group { kRowGroups = 1, kStepGroups = 2 };
+enum Group { kOneGroup = 0, kRowGroups = 1, kStepGroups = 2 };
 
 // A token as the products of a loss's gradient read it.  target < 0: left out of the loss.
 struct LossRow {
@@ -137,12 +137,14 @@ constexpr int kGroupRows[kGroupKinds] = {256, 128, 64}, kGroupCols[kGroupKinds] 
 // and the type of C).  kind: of GroupKind; splits of k with groups of steps only.
 hipError_t launch_groups(const GemmArgs& A, int dtype, Product what, int kind, hipStream_t s);
 
-// Few rows a group: C = A B^T without LDS tiles; dual: the gated forward product.
-hipError_t launch_skinny_groups(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
+// Few rows, of groups or (offsets null) of one: C = A B^T without LDS tiles, plain, gated or
+// the statistics of a loss (columns of 16: kSkinnyCols).  Operands of any alignment.
+constexpr int kSkinnyCols = 16;
+hipError_t launch_skinny_groups(const GemmArgs& A, int dtype, Product what, hipStream_t s);
 
-// The products of a loss: the logits' statistics, their gradient (what: kLossLogits,
-// kLossGradient: one kind of tile), and the gradients of both operands (wide).
-hipError_t launch_loss(const GemmArgs& A, int dtype, Product what, const Cut& cut, hipStream_t s);
+// The products of a loss, on the same tiles: the logits' statistics, their gradient (what:
+// kLossLogits, kLossGradient), and the gradients of both operands (wide; k in A.splits parts).
+hipError_t launch_loss(const GemmArgs& A, int dtype, Product what, int kind, hipStream_t s);
 
 constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel without LDS tiles takes
 

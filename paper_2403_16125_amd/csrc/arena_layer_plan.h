@@ -273,5 +273,62 @@ inline hipError_t pack(std::initializer_list<const Operand*> operands, hipStream
     return n ? arena::mm::launch_packs(packs, n, s) : hipSuccess;
 }
 
+// ---------------------------------------------------------------- products of groups
+
+// What a kind of tile costs in microseconds (measured on one MI355X): a step of 64 of k
+// with every slot of the compute units taken and with at most one block on each, a tile
+// beside its steps, and how many blocks a compute unit holds.
+struct GroupCost {
+    double full, alone, start;
+    int slots;
+};
+constexpr GroupCost kGroupCost[mm::kGroupKinds] = {
+    {1.75, 1.30, 4.0, 1}, {1.00, 0.75, 3.0, 2}, {0.80, 0.60, 2.0, 2}};
+
+// uneven: how much longer than the average one the longest of few tiles takes.  exact: how
+// many tiles there are is known, and the last round counts as what it is; otherwise half a
+// round more than they fill.
+inline double group_time(double tiles, double steps, int kind, int64_t splits, double bytes, double uneven,
+                         bool exact)
+{
+    const GroupCost& k = kGroupCost[kind];
+    const double per = std::ceil(steps / splits), values = (double)mm::kGroupRows[kind] * mm::kGroupCols[kind];
+    const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate;
+    const double blocks = tiles * splits, round = kUnits * k.slots;
+    const double alone = per * uneven * k.alone + k.start + end, full = per * k.full + k.start + end * k.slots;
+    const double whole = std::floor(blocks / round), rest = blocks - whole * round;
+    const double t = blocks <= kUnits  ? alone
+                     : blocks <= round ? full + per * (uneven - 1.0) * k.full
+                     : exact           ? whole * full + (rest > kUnits ? full : rest > 0 ? alone : 0.0)
+                                       : (blocks / round + 0.5) * full;
+    return kLaunch + t + (splits > 1 ? kJoin + blocks * values * 4e-6 / kJoinRate : 0.0);
+}
+
+// The kind of tile, and the parts of k if it may be split, for a product on resident blocks.
+struct GroupCut {
+    int kind, splits;
+    int64_t part;             // bytes
+};
+
+inline GroupCut choose_groups(int64_t M, int64_t N, int64_t steps, int64_t batch, double bytes, bool split, double uneven,
+                              bool exact)
+{
+    using namespace mm;
+    GroupCut best = {kGroup256, 1, 0};
+    double least = INFINITY;
+    for (int kind = 0; kind < kGroupKinds; ++kind) {
+        const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * batch;
+        for (int s = 1; s <= 16 && (s == 1 || (split && s * 4 <= steps)); ++s) {
+            if (tiles * s > 0x7fffffff) continue;
+            const double t = group_time((double)tiles, (double)steps, kind, s, bytes, uneven, exact);
+            if (t < least) {
+                least = t;
+                best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0};
+            }
+        }
+    }
+    return best;
+}
+
 }  // namespace plan
 }  // namespace arena

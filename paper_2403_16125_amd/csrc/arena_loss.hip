@@ -132,7 +132,8 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(const LossArgs A)
 hipError_t launch_loss_join(const LossArgs& A, hipStream_t s)
 {
     if (A.tokens == 0) return hipSuccess;
-    if (A.tokens >= 1024) loss_join_kernel<32><<<(unsigned)((A.tokens + 31) / 32), 1024, 0, s>>>(A);
+    if (A.tokens >= 4096) loss_join_kernel<32><<<(unsigned)((A.tokens + 31) / 32), 1024, 0, s>>>(A);
+    else if (A.tokens >= 64) loss_join_kernel<8><<<(unsigned)((A.tokens + 7) / 8), 1024, 0, s>>>(A);
     else loss_join_kernel<1><<<(unsigned)A.tokens, 1024, 0, s>>>(A);
     return hipGetLastError();
 }

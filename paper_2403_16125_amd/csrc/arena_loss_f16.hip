@@ -1,12 +1,12 @@
 // The loss's tiled products in float16.
-#include "arena_gemm.h"
+#include "arena_groups.h"
 
 namespace arena {
 namespace mm {
 
-hipError_t launch_loss_f16(const GemmArgs& A, Product what, const Cut& cut, hipStream_t s)
+hipError_t launch_loss_f16(const GemmArgs& A, Product what, int kind, hipStream_t s)
 {
-    return launch_loss_t<F16>(A, what, cut, s);
+    return launch_loss_t<F16>(A, what, kind, s);
 }
 
 }  // namespace mm

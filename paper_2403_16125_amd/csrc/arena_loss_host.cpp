@@ -68,21 +68,10 @@ arena_status check_loss_grads(arena_ctx* c, const char* who, const arena_loss_de
     return ARENA_OK;
 }
 
-// A product on one kind of tile, k whole.
-Cut choose_whole(int64_t M, int64_t N, int64_t steps, double bytes)
+// The kind of tile for a product with k whole; bytes: what the epilogue moves for a value.
+int choose_whole(int64_t M, int64_t N, int64_t steps, double bytes)
 {
-    using namespace arena::mm;
-    Cut best = {k256, k256, 0, 1, (int)steps};
-    double least = INFINITY;
-    for (int kind = 0; kind < kTileKinds; ++kind) {
-        const int64_t tiles = ceil_div(M, kTileSide[kind]) * ceil_div(N, kTileSide[kind]);
-        const double t = launch_time(tiles, steps, kind, 1, bytes);
-        if (t < least) {
-            least = t;
-            best = {kind, kind, tiles, 1, (int)steps};
-        }
-    }
-    return best;
+    return choose_groups(M, N, steps, 1, bytes, false, 1.0, true).kind;
 }
 
 LossArgs loss_args(const arena_loss_desc* d)
@@ -98,19 +87,25 @@ LossArgs loss_args(const arena_loss_desc* d)
     return A;
 }
 
+// Whether a forward pass takes the kernel for few tokens, which has more reads of the weights
+// in flight than the tiles (one token, 131072 x 4096: 227 us on tiles).
+bool few_tokens(const arena_loss_desc* d) { return d->tokens <= 16; }
+
 struct LossPlan {
     Pieces w;
+    bool skinny;
     Operand x, weight;
     int64_t piece;            // tokens
-    Cut cut;
+    int kind;
     int64_t columns;          // of tiles
     void *stats, *picked;
     LossPlan(const arena_loss_desc* d, void* base)
-        : w(base), x(w, d->x, d->ld_x, d->tokens, d->model, Operand::direct(d->x, d->ld_x, d->model)),
-          weight(w, d->w, d->ld_w, d->vocabulary, d->model, Operand::direct(d->w, d->ld_w, d->model)),
+        : w(base), skinny(few_tokens(d)),
+          x(w, d->x, d->ld_x, d->tokens, d->model, skinny || Operand::direct(d->x, d->ld_x, d->model)),
+          weight(w, d->w, d->ld_w, d->vocabulary, d->model, skinny || Operand::direct(d->w, d->ld_w, d->model)),
           piece(std::min(d->tokens, kTokenPiece)),
-          cut(choose_whole(piece, d->vocabulary, ceil_div(d->model, arena::mm::kBK), 0.5)),
-          columns(ceil_div(d->vocabulary, arena::mm::kTileSide[cut.main]))
+          kind(choose_whole(piece, d->vocabulary, ceil_div(d->model, arena::mm::kBK), 0.5)),
+          columns(ceil_div(d->vocabulary, skinny ? arena::mm::kSkinnyCols : arena::mm::kGroupCols[kind]))
     {
         stats = w.take(8 * piece * columns);
         picked = w.take(4 * piece);
@@ -140,18 +135,18 @@ struct LossBackPlan {
         sum = w.take(many && o->dx ? 4 * T * D : 0);
         int64_t most = 0;
         for (int64_t n : {piece, V - (V - 1) / piece * piece}) {
-            if (o->dx && T > 0) most = std::max(most, part_bytes(cut_dx(T, D, n), T, D, 1, false, false));
-            if (o->dw) most = std::max(most, part_bytes(cut_dw(T, D, n), n, D, 1, false, false));
+            if (o->dx && T > 0) most = std::max(most, cut_dx(T, D, n).part);
+            if (o->dw) most = std::max(most, cut_dw(T, D, n).part);
         }
         part = w.take(most);
     }
-    static Cut cut_dx(int64_t T, int64_t D, int64_t n)
+    static GroupCut cut_dx(int64_t T, int64_t D, int64_t n)
     {
-        return choose_cut(T, D, ceil_div(n, arena::mm::kBK), 1, false, false, 4.0);
+        return choose_groups(T, D, ceil_div(n, arena::mm::kBK), 1, 4.0, true, 1.0, true);
     }
-    static Cut cut_dw(int64_t T, int64_t D, int64_t n)
+    static GroupCut cut_dw(int64_t T, int64_t D, int64_t n)
     {
-        return choose_cut(n, D, ceil_div(T, arena::mm::kBK), 1, false, false, 2.0);
+        return choose_groups(n, D, ceil_div(T, arena::mm::kBK), 1, 2.0, true, 1.0, true);
     }
 };
 
@@ -184,7 +179,7 @@ arena_status arena_cross_entropy_forward(arena_ctx* c, const arena_loss_desc* d,
     hipStream_t s = (hipStream_t)stream;
     hipError_t e = pack({&P.x, &P.weight}, s);
     if (e) return hip_error(c, e, "cross entropy copies");
-    const int wide = d->target_dtype == ARENA_I64 ? 8 : 4, side = arena::mm::kTileSide[P.cut.main];
+    const int wide = d->target_dtype == ARENA_I64 ? 8 : 4;
     for (int64_t t = 0; t < d->tokens; t += P.piece) {
         const int64_t n = std::min(P.piece, d->tokens - t);
         GemmArgs A = new_args(n, d->vocabulary, d->model);
@@ -194,10 +189,10 @@ arena_status arena_cross_entropy_forward(arena_ctx* c, const arena_loss_desc* d,
         A.target_wide = wide == 8;
         A.stats = (float*)P.stats;
         A.picked = (float*)P.picked;
-        Cut cut = P.cut;
-        cut.first = ceil_div(n, side) * P.columns;
-        if ((e = arena::mm::launch_loss(A, d->dtype, arena::mm::kLossLogits, cut, s)))
-            return hip_error(c, e, "cross entropy logits launch");
+        A.splits = 1;
+        e = P.skinny ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kLossLogits, s)
+                     : arena::mm::launch_loss(A, d->dtype, arena::mm::kLossLogits, P.kind, s);
+        if (e) return hip_error(c, e, "cross entropy logits launch");
         LossArgs L = loss_args(d);
         L.tokens = n;
         L.target = A.target;
@@ -264,6 +259,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             A.pad = (int)pad8(n);
             A.rows = (const LossRow*)P.rows;
             A.first_col = (int)v;
+            A.splits = 1;
             if ((e = launch_loss(A, f->dtype, kLossGradient, choose_whole(T, n, ceil_div(D, kBK), 2.0), s)))
                 return hip_error(c, e, "cross entropy logits' gradient launch");
         }
@@ -278,7 +274,9 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             X.beta = first ? 0.0f : 1.0f;
             X.factor = factor;
             X.part = (float*)P.part;
-            if ((e = launch_loss(X, f->dtype, kRowsCols, P.cut_dx(T, D, n), s)))
+            const GroupCut cut = P.cut_dx(T, D, n);
+            X.splits = cut.splits;
+            if ((e = launch_loss(X, f->dtype, kRowsCols, cut.kind, s)))
                 return hip_error(c, e, "cross entropy input gradient launch");
         }
         if (g->dw) {
@@ -295,7 +293,9 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             }
             W.factor = factor;
             W.part = (float*)P.part;
-            if ((e = launch_loss(W, f->dtype, kColsCols, P.cut_dw(T, D, n), s)))
+            const GroupCut cut = P.cut_dw(T, D, n);
+            W.splits = cut.splits;
+            if ((e = launch_loss(W, f->dtype, kColsCols, cut.kind, s)))
                 return hip_error(c, e, "cross entropy weight gradient launch");
         }
     }
