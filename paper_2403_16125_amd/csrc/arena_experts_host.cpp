@@ -251,24 +251,24 @@ arena_status check_experts_grads(arena_ctx* c, const char* who, const arena_expe
     return ARENA_OK;
 }
 
-// Whether matrices can be read in place by the tiled kernels.
-bool direct(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts)
+// Whether the loads that write to the LDS can read matrices: rows on 16 bytes.
+bool even(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts)
 {
     return Operand::direct(p, ld, cols) && (experts == 1 || stride % 8 == 0);
 }
 
 // The kind of tile for a product of groups of rows: how they fall is not known here, so
 // each group that can have rows is taken to waste half a tile.
-int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes)
+int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes, bool any)
 {
     using namespace arena::mm;
-    int best = kGroup256;
+    int best = any ? kGroup128 : kGroup256;
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
         const double tm = std::max((double)some, (double)rows / kGroupRows[kind] + 0.5 * some);
         if (group_tiles(rows, groups, kGroupRows[kind]) * tn > 0x7fffffff) continue;
-        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0, false);
+        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0, false, any);
         if (t < least) {
             least = t;
             best = kind;
@@ -279,10 +279,11 @@ int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dua
 
 // The kind of tile and the parts of k for a product of groups of steps, taken to be of
 // one length but for the longest.
-GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes)
+GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes,
+                      bool any)
 {
     return choose_groups(M, N, std::max<int64_t>(1, ceil_div(rows, groups * arena::mm::kBK)), groups * pairs, bytes, true,
-                         1.5, false);
+                         1.5, false, any);
 }
 
 // Whether a forward pass takes the kernel for few rows, which streams the weights of one
@@ -291,33 +292,29 @@ GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pa
 // against 77; 8 of 4096 x 10944: 292 against 390, 64 rows 471 against 421).
 bool few_rows(const arena_experts_desc* d) { return d->rows <= 16; }
 
-struct ExpertsPlan {
-    Pieces w;
-    bool skinny, gate_ok;
-    Operand x, gate, up, down;
-    ExpertsPlan(const arena_experts_desc* d, bool skinny_, void* base)
-        : w(base), skinny(skinny_),
-          gate_ok(direct(d->w_gate, d->ld_gate, d->model, d->stride_gate, d->experts) &&
-                  direct(d->w_up, d->ld_up, d->model, d->stride_up, d->experts) && d->ld_gate == d->ld_up &&
-                  (d->experts == 1 || d->stride_gate == d->stride_up)),
-          x(w, d->x, d->ld_x, d->rows, d->model, skinny || Operand::direct(d->x, d->ld_x, d->model)),
-          gate(w, d->w_gate, d->ld_gate, d->inner, d->model, skinny || gate_ok, d->experts, d->stride_gate),
-          up(w, d->w_up, d->ld_up, d->inner, d->model, skinny || gate_ok, d->experts, d->stride_up),
-          down(w, d->w_down, d->ld_down, d->model, d->inner,
-               skinny || direct(d->w_down, d->ld_down, d->inner, d->stride_down, d->experts), d->experts, d->stride_down)
+// Which matrices the loads that write to the LDS cannot take: their products load to
+// registers first.
+struct Uneven {
+    bool x, up, down;         // up: or the gate weights, or their row strides differ
+    explicit Uneven(const arena_experts_desc* d)
+        : x(!even(d->x, d->ld_x, d->model, 0, 1)),
+          up(!even(d->w_gate, d->ld_gate, d->model, d->stride_gate, d->experts) ||
+             !even(d->w_up, d->ld_up, d->model, d->stride_up, d->experts) || d->ld_gate != d->ld_up),
+          down(!even(d->w_down, d->ld_down, d->inner, d->stride_down, d->experts))
     {
     }
 };
 
-struct ExpertsBackPlan : ExpertsPlan {
-    Operand dy;
+struct ExpertsBackPlan {
+    Pieces w;
+    Uneven any;
+    bool dy_any;
     int64_t ld;               // rows of dg and du
     void *dg, *du, *part;
     bool pair;                // both weight gradients of the first products in one launch
     GroupCut cut_up, cut_down;
     ExpertsBackPlan(const arena_experts_desc* d, const arena_experts_grads* g, void* base)
-        : ExpertsPlan(d, false, base),
-          dy(w, g->dy, g->ld_dy, d->rows, d->model, Operand::direct(g->dy, g->ld_dy, d->model))
+        : w(base), any(d), dy_any(!even(g->dy, g->ld_dy, d->model, 0, 1))
     {
         ld = pad8(d->inner);
         dg = w.take(2 * d->rows * ld);
@@ -325,8 +322,8 @@ struct ExpertsBackPlan : ExpertsPlan {
         pair = g->dw_gate && g->dw_up && g->ld_dw_gate == g->ld_dw_up &&
                (d->experts == 1 || g->stride_dw_gate == g->stride_dw_up);
         const double bytes = bytes_of(g->grad_dtype) * (g->accumulate ? 2.0 : 1.0);
-        cut_up = choose_steps(d->inner, d->model, d->rows, d->experts, pair ? 2 : 1, bytes);
-        cut_down = choose_steps(d->model, d->inner, d->rows, d->experts, 1, bytes);
+        cut_up = choose_steps(d->inner, d->model, d->rows, d->experts, pair ? 2 : 1, bytes, any.x);
+        cut_down = choose_steps(d->model, d->inner, d->rows, d->experts, 1, bytes, dy_any);
         part = w.take(std::max(g->dw_gate || g->dw_up ? cut_up.part : 0, g->dw_down ? cut_down.part : 0));
     }
 };
@@ -464,7 +461,7 @@ arena_status arena_experts_forward_workspace(arena_ctx* c, const arena_experts_d
     if (!bytes) return ctx_fail(c, ARENA_ERR_INVALID_ARG, "experts forward: bytes is NULL");
     const arena_status s = check_experts(c, "experts forward", d, false);
     if (s) return s;
-    *bytes = d->rows ? ExpertsPlan(d, few_rows(d), nullptr).w.used : 0;
+    *bytes = 0;
     return ARENA_OK;
 }
 
@@ -474,38 +471,38 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     ctx_clear(c);
     arena_status st = check_experts(c, "experts forward", d, false);
     if (st || d->rows == 0) return st;
-    const ExpertsPlan P(d, few_rows(d), d->workspace);
-    if ((st = check_workspace(c, "experts forward", d->workspace, d->workspace_bytes, P.w.used))) return st;
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
     const int64_t R = d->rows, E = d->experts, bk = arena::mm::kBK;
-    hipError_t e = pack({&P.x, &P.gate, &P.up, &P.down}, s);
-    if (e) return hip_error(c, e, "experts forward copies");
-
+    const Uneven any(d);
+    const bool few = few_rows(d);
     GemmArgs A = new_args(R, d->inner, d->model);
     A.offsets = d->offsets; A.groups = d->experts;
     A.splits = 1;
-    A.a[0] = P.x.p; A.lda = P.x.ld;
-    A.b[0] = P.gate.p; A.b[1] = P.up.p; A.ldb = P.gate.ld; A.sb = P.gate.stride;
-    A.ldb1 = P.up.ld; A.sb1 = P.up.stride;
+    A.any = any.x || any.up;
+    A.a[0] = d->x; A.lda = d->ld_x;
+    A.b[0] = d->w_gate; A.ldb = d->ld_gate; A.sb = d->stride_gate;
+    A.b[1] = d->w_up; A.ldb1 = d->ld_up; A.sb1 = d->stride_up;
     A.c[0] = d->h; A.ldc = d->ld_inner;
     A.g = d->g; A.u = d->u; A.ldg = d->ld_inner;
     A.act = d->activation;
     A.pad = (int)pad8(d->inner);
-    e = P.skinny ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kGateUp, s)
-                 : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
-                                            choose_rows(R, E, d->inner, ceil_div(d->model, bk), true, d->g ? 4.0 : 1.0), s);
+    hipError_t e = few ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kGateUp, s)
+                       : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
+                                                  choose_rows(R, E, d->inner, ceil_div(d->model, bk), true,
+                                                              d->g ? 4.0 : 1.0, A.any), s);
     if (e) return hip_error(c, e, "experts gate and up launch");
     GemmArgs B = new_args(R, d->model, d->inner);
     B.offsets = d->offsets; B.groups = d->experts;
     B.splits = 1;
+    B.any = any.down;
     B.a[0] = d->h; B.lda = d->ld_inner;
-    B.b[0] = P.down.p; B.ldb = P.down.ld; B.sb = P.down.stride;
+    B.b[0] = d->w_down; B.ldb = d->ld_down; B.sb = d->stride_down;
     B.c[0] = d->y; B.ldc = d->ld_y;
-    e = P.skinny ? arena::mm::launch_skinny_groups(B, d->dtype, arena::mm::kRowsRows, s)
-                 : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
-                                            choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0), s);
+    e = few ? arena::mm::launch_skinny_groups(B, d->dtype, arena::mm::kRowsRows, s)
+            : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
+                                       choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0, B.any), s);
     return e == hipSuccess ? ARENA_OK : hip_error(c, e, "experts down launch");
 }
 
@@ -536,25 +533,26 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     hipStream_t s = (hipStream_t)stream;
     const int64_t R = f->rows, D = f->model, F = f->inner, E = f->experts, bk = arena::mm::kBK;
     using namespace arena::mm;
-    hipError_t e = pack({&P.x, &P.gate, &P.up, &P.down, &P.dy}, s);
-    if (e) return hip_error(c, e, "experts backward copies");
+    hipError_t e;
     if (R > 0 && (g->dx || g->dw_gate || g->dw_up)) {
         GemmArgs H = new_args(R, F, D);
         H.offsets = f->offsets; H.groups = f->experts;
         H.splits = 1;
-        H.a[0] = P.dy.p; H.lda = P.dy.ld;
-        H.b[0] = P.down.p; H.ldb = P.down.ld; H.sb = P.down.stride;
+        H.any = P.dy_any || P.any.down;
+        H.a[0] = g->dy; H.lda = g->ld_dy;
+        H.b[0] = f->w_down; H.ldb = f->ld_down; H.sb = f->stride_down;
         H.g = f->g; H.u = f->u; H.ldg = f->ld_inner;
         H.c[0] = P.dg; H.c[1] = P.du; H.ldc = P.ld;
         H.act = f->activation;
         H.pad = (int)P.ld;
-        if ((e = launch_groups(H, f->dtype, kGateUpBack, choose_rows(R, E, F, ceil_div(D, bk), false, 10.0), s)))
+        if ((e = launch_groups(H, f->dtype, kGateUpBack, choose_rows(R, E, F, ceil_div(D, bk), false, 10.0, H.any), s)))
             return hip_error(c, e, "experts inner gradient launch");
     }
     // of every group C[m, n] = sum over its rows of a(t, m) b(t, n), beside what accumulate keeps
     auto weight = [&](const void* a0, const void* a1, int64_t lda, const void* b, int64_t ldb, int64_t M, int64_t N,
-                      void* c0, void* c1, int64_t ldc, int64_t sc, const GroupCut& cut) {
+                      void* c0, void* c1, int64_t ldc, int64_t sc, const GroupCut& cut, bool any) {
         GemmArgs A = new_args(M, N, R);
+        A.any = any;
         A.offsets = f->offsets; A.groups = f->experts;
         A.pairs = c1 != nullptr;
         A.batch = (int)E * (c1 ? 2 : 1);
@@ -571,19 +569,19 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
         A.part = (float*)P.part;
         return launch_groups(A, f->dtype, kColsCols, cut.kind, s);
     };
-    if (g->dw_down && (e = weight(P.dy.p, nullptr, P.dy.ld, f->h, f->ld_inner, D, F, g->dw_down, nullptr, g->ld_dw_down,
-                                  g->stride_dw_down, P.cut_down)))
+    if (g->dw_down && (e = weight(g->dy, nullptr, g->ld_dy, f->h, f->ld_inner, D, F, g->dw_down, nullptr, g->ld_dw_down,
+                                  g->stride_dw_down, P.cut_down, P.dy_any)))
         return hip_error(c, e, "experts down gradient launch");
     if (P.pair) {
-        if ((e = weight(P.dg, P.du, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, g->dw_up, g->ld_dw_gate, g->stride_dw_gate,
-                        P.cut_up)))
+        if ((e = weight(P.dg, P.du, P.ld, f->x, f->ld_x, F, D, g->dw_gate, g->dw_up, g->ld_dw_gate, g->stride_dw_gate,
+                        P.cut_up, P.any.x)))
             return hip_error(c, e, "experts gate and up gradient launch");
     } else {
-        if (g->dw_gate && (e = weight(P.dg, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_gate, nullptr, g->ld_dw_gate,
-                                      g->stride_dw_gate, P.cut_up)))
+        if (g->dw_gate && (e = weight(P.dg, nullptr, P.ld, f->x, f->ld_x, F, D, g->dw_gate, nullptr, g->ld_dw_gate,
+                                      g->stride_dw_gate, P.cut_up, P.any.x)))
             return hip_error(c, e, "experts gate gradient launch");
-        if (g->dw_up && (e = weight(P.du, nullptr, P.ld, P.x.p, P.x.ld, F, D, g->dw_up, nullptr, g->ld_dw_up,
-                                    g->stride_dw_up, P.cut_up)))
+        if (g->dw_up && (e = weight(P.du, nullptr, P.ld, f->x, f->ld_x, F, D, g->dw_up, nullptr, g->ld_dw_up,
+                                    g->stride_dw_up, P.cut_up, P.any.x)))
             return hip_error(c, e, "experts up gradient launch");
     }
     if (R > 0 && g->dx) {
@@ -592,9 +590,11 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
         X.splits = 1;
         X.nseg = 2;
         X.a[0] = P.dg; X.a[1] = P.du; X.lda = P.ld;
-        X.b[0] = P.gate.p; X.b[1] = P.up.p; X.ldb = P.gate.ld; X.sb = P.gate.stride;
+        X.any = P.any.up;
+        X.b[0] = f->w_gate; X.ldb = f->ld_gate; X.sb = f->stride_gate;
+        X.b[1] = f->w_up; X.ldb1 = f->ld_up; X.sb1 = f->stride_up;
         X.c[0] = g->dx; X.ldc = g->ld_dx;
-        if ((e = launch_groups(X, f->dtype, kRowsCols, choose_rows(R, E, D, 2 * ceil_div(F, bk), false, 2.0), s)))
+        if ((e = launch_groups(X, f->dtype, kRowsCols, choose_rows(R, E, D, 2 * ceil_div(F, bk), false, 2.0, X.any), s)))
             return hip_error(c, e, "experts input gradient launch");
     }
     return ARENA_OK;

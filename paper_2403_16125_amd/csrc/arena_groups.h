@@ -20,13 +20,14 @@
 namespace arena {
 namespace mm {
 
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool ATR_, bool BTR_, int EPI_, int GROUP_>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool ATR_, bool BTR_, int EPI_, int GROUP_, bool DIRECT_>
 struct GroupTile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr bool ATR = ATR_, BTR = BTR_, DUAL = EPI_ == kGatedFwd;
     static constexpr int EPI = EPI_, GROUP = GROUP_;
     static constexpr bool kUpToN = EPI_ == kPlain || EPI_ == kWide;
+    static constexpr bool kDirect = DIRECT_;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     static constexpr int kCols = DUAL ? BN / 2 : BN;
@@ -301,8 +302,12 @@ struct LeanLoader {
     __device__ __forceinline__ int64_t pitch() const { return TR ? (int64_t)ld * (2 * kBK) : 2 * kBK; }
     __device__ __forceinline__ const char* base(const void* p, int64_t from) const
     {
+        return base_of(p, from, ld);
+    }
+    __device__ __forceinline__ const char* base_of(const void* p, int64_t from, int64_t ld_) const
+    {
         const char* q = (const char*)p + 2 * from;
-        return TR ? q + 2 * (int64_t)row0 : q + 2 * (int64_t)row0 * ld;
+        return TR ? q + 2 * (int64_t)row0 : q + 2 * (int64_t)row0 * ld_;
     }
     template <bool TAIL>
     __device__ __forceinline__ void fetch(const char* p0, const char* p1, char* lds, int tid, int left) const
@@ -334,14 +339,92 @@ struct LeanLoader {
     }
 };
 
-template <typename P, int R, bool TR, bool DUAL, bool LEAN>
+// Operands whose rows start on any value: loads to registers, which are unaligned, and from
+// there to the LDS once the step before is multiplied.  Lays the same chunks in the same
+// places.  A chunk that a row's end cuts is read whole where another row follows in the matrix
+// (a row further on along k it is masked; columns past the last make columns of C that are not
+// written), and value by value in the matrix's last row.  The up matrix has a row stride of its
+// own.
+template <typename P, int R, bool TR, bool DUAL>
+struct StagedLoader : LeanLoader<P, R, TR, DUAL> {
+    typedef LeanLoader<P, R, TR, DUAL> Base;
+    using Base::kChunks;
+    using Base::kEach;
+    u32x4 v[kChunks];
+
+    static __device__ __forceinline__ u32x4 whole(const char* p)
+    {
+        u32x4 w;
+        __builtin_memcpy(&w, p, 16);
+        return w;
+    }
+    // n of eight values, zeros behind them
+    static __device__ __forceinline__ u32x4 some(const char* p, int n)
+    {
+        const uint16_t* q = (const uint16_t*)p;
+        u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) w[i >> 1] |= (uint32_t)q[i] << (16 * (i & 1));
+        return w;
+    }
+    static __device__ __forceinline__ u32x4 masked(u32x4 w, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] &= n >= 2 * i + 2 ? 0xffffffffu : n == 2 * i + 1 ? 0xffffu : 0u;
+        return w;
+    }
+    __device__ __forceinline__ void load(const char* p0, const char* p1, int ld0, int ld1, int tid, int left)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        int row = Base::lane_row, at = Base::lane_at;
+        asm volatile("" : "+v"(row), "+v"(at));       // not kept over the steps
+#pragma unroll
+        for (int it = 0; it < kChunks; ++it) {
+            const bool up = DUAL && Dual<P::BN / P::WN>::up(it * kEach + wave * 8);
+            const char* p = up ? p1 : p0;
+            const uint32_t pitch = (uint32_t)(up ? ld1 : ld0) * 2;
+            if (TR) {
+                const int k = row + it * kEach;
+                int col = at ^ (kEach % 32 == 0 ? 0 : ((it * kEach >> 3 & 3) << 2 & (Base::kGran - 1)) << 4);
+                col = col < Base::last ? col : 0;
+                const char* src = p + (uint32_t)k * pitch + (uint32_t)col * 2;
+                if (left > kBK) v[it] = whole(src);
+                else if (k >= left) v[it] = u32x4{0, 0, 0, 0};
+                else if (k == left - 1 && col + 8 > Base::last) v[it] = some(src, Base::last - col);
+                else v[it] = whole(src);
+            } else {
+                const int r = min(row + (DUAL ? Dual<P::BN / P::WN>::row(it * kEach) : it * kEach), Base::last - 1);
+                const int n = left - (at >> 1);
+                const char* src = p + (uint32_t)r * pitch + (uint32_t)at;
+                if (left >= kBK) v[it] = whole(src);
+                else if (n <= 0) v[it] = u32x4{0, 0, 0, 0};
+                else if (n < 8 && r == Base::last - 1) v[it] = some(src, n);
+                else v[it] = masked(whole(src), n);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char* lds, int tid) const
+    {
+#pragma unroll
+        for (int it = 0; it < kChunks; ++it) *(u32x4*)(lds + (it * P::kThreads + tid) * 16) = v[it];
+    }
+};
+
+// LEAN: 0, 1, or 2 for operands of any alignment.
+template <typename P, int R, bool TR, bool DUAL, int LEAN>
 struct LoaderOf {
     typedef GroupLoader<P, R, TR, DUAL> Type;
 };
 
 template <typename P, int R, bool TR, bool DUAL>
-struct LoaderOf<P, R, TR, DUAL, true> {
+struct LoaderOf<P, R, TR, DUAL, 1> {
     typedef LeanLoader<P, R, TR, DUAL> Type;
+};
+
+template <typename P, int R, bool TR, bool DUAL>
+struct LoaderOf<P, R, TR, DUAL, 2> {
+    typedef StagedLoader<P, R, TR, DUAL> Type;
 };
 
 // Four columns of two fragments j and j + 1 in lanes of rows of 16 (columns 4 r + 0..3 of
@@ -447,8 +530,9 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         return true;
     };
 
-    typename LoaderOf<P, P::BM, P::ATR, false, P::kLean>::Type la;
-    typename LoaderOf<P, P::BN, P::BTR, P::DUAL, P::kLean>::Type lb;
+    constexpr int kLoader = P::kDirect ? P::kLean : 2;
+    typename LoaderOf<P, P::BM, P::ATR, false, kLoader>::Type la;
+    typename LoaderOf<P, P::BN, P::BTR, P::DUAL, kLoader>::Type lb;
     la.lanes(tid);
     lb.lanes(tid);
     Frags<P, P::BM, P::ATR> fa;
@@ -477,7 +561,9 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         a0 = la.base(A.a[sel], kRows ? 0 : k_from * A.lda);
         b0 = lb.base(A.b[sel], kRows ? w->z * A.sb : k_from * A.ldb);
         a1 = P::kSegs == 2 ? la.base(A.a[1], 0) : a0;
-        b1 = P::kSegs == 2 || P::DUAL ? lb.base(A.b[1], w->z * A.sb) : b0;
+        if constexpr (P::kSegs == 1 && !P::DUAL) b1 = b0;
+        else if constexpr (P::kDirect) b1 = lb.base(A.b[1], w->z * A.sb1);      // of the same row stride
+        else b1 = lb.base_of(A.b[1], w->z * A.sb1, A.ldb1);
     };
     auto fetch_rows = [&](const Work& w, char* to) {
         if (P::kRowBytes == 0 || wave >= P::BM / 64) return;
@@ -493,21 +579,39 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     auto fetch = [&](const Work& w, int step, char* sa, char* sb) {
         int at = w.s0 + step;
         const char *pa = a0, *pb = b0;
+        bool second = false;
         if (P::kSegs == 2 && at >= w.sps) {
             at -= w.sps;
             pa = a1;
             pb = b1;
+            second = true;
         }
         const int left = w.K - at * kBK;
         pa += at * la.pitch();
+        if constexpr (!P::kDirect) {
+            const int ld = (int)(second ? A.ldb1 : A.ldb);
+            pb += P::BTR ? at * (int64_t)ld * (2 * kBK) : at * (2 * kBK);
+            la.load(pa, pa, (int)A.lda, (int)A.lda, tid, left);
+            lb.load(pb, P::DUAL ? b1 + at * (2 * kBK) : pb, ld, (int)A.ldb1, tid, left);
+            return;
+        }
         pb += at * lb.pitch();
         const char* pu = P::DUAL ? b1 + at * lb.pitch() : pb;
-        if (left < kBK) {
+        if constexpr (!P::kDirect) {
+        } else if (left < kBK) {
             la.template fetch<true>(pa, pa, sa, tid, left);
             lb.template fetch<true>(pb, pu, sb, tid, left);
         } else {
             la.template fetch<false>(pa, pa, sa, tid, left);
             lb.template fetch<false>(pb, pu, sb, tid, left);
+        }
+    };
+
+    // what was loaded to registers goes to the LDS
+    auto commit = [&](char* sa, char* sb) {
+        if constexpr (!P::kDirect) {
+            la.store(sa, tid);
+            lb.store(sb, tid);
         }
     };
 
@@ -542,7 +646,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     bool stored = false, idle = false;
     auto arrive = [&](int step) {
         asm volatile("" ::: "memory");
-        if (stored && step == 0) wait_loads<kStores>();
+        if (!P::kDirect && !(P::kRowBytes && step == 0)) __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);    // LDS writes
+        else if (stored && step == 0) wait_loads<kStores>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -551,23 +656,28 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     auto turn = [&](const Work& w, int step, int u, bool first) {
         arrive(step);
         if (step + 1 < w.steps) fetch(w, step + 1, bufa(u ^ 1), bufb(u ^ 1));
-        if (kRows && idle) return;
-        __builtin_amdgcn_sched_barrier(0);
-        read(bufa(u), bufb(u), 0, fa0, fb0);
-        if (!first) multiply(fa1, fb1);
-        weave();
-        __builtin_amdgcn_sched_barrier(0);
-        read(bufa(u), bufb(u), 1, fa1, fb1);
-        multiply(fa0, fb0);
-        weave();
-        __builtin_amdgcn_sched_barrier(0);
+        if (!(kRows && idle)) {
+            __builtin_amdgcn_sched_barrier(0);
+            read(bufa(u), bufb(u), 0, fa0, fb0);
+            if (!first) multiply(fa1, fb1);
+            weave();
+            __builtin_amdgcn_sched_barrier(0);
+            read(bufa(u), bufb(u), 1, fa1, fb1);
+            multiply(fa0, fb0);
+            weave();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!P::kDirect && step + 1 < w.steps) commit(bufa(u ^ 1), bufb(u ^ 1));
     };
 
     Work w;
     if (!next_work(&w)) return;
     begin(&w);
     fetch_rows(w, rows0);
-    if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+    if (w.steps > 0) {
+        fetch(w, 0, bufa(0), bufb(0));
+        commit(bufa(0), bufb(0));
+    }
     bool odd = false;             // which rows are the tile's
     for (;;) {
 #pragma unroll
@@ -683,6 +793,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             for (int i = 0; i < P::FM; ++i) row_out(mw + i * 16, acc[i]);
         }
         if (!more) return;
+        if (w.steps > 0) commit(bufa(0), bufb(0));
         stored = P::EPI != kLossStats && done.m0 + P::BM <= done.m_end && done.n0 + P::kCols <= A.N;
     }
 }
@@ -856,10 +967,17 @@ hipError_t launch_skinny_groups_t(const GemmArgs& A, Product what, hipStream_t s
 template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
 hipError_t launch_groups_of(const GemmArgs& A, int kind, hipStream_t s)
 {
+    if (A.any) {
+        if (kind == kGroup128)
+            return launch_group_tile<GroupTile<T, 128, 128, 2, 2, ATR, BTR, EPI, GROUP, false>>(A, s);
+        if (kind == kGroup64x128)
+            return launch_group_tile<GroupTile<T, 64, 128, 2, 2, ATR, BTR, EPI, GROUP, false>>(A, s);
+        return hipErrorInvalidValue;
+    }
     switch (kind) {
-    case kGroup256: return launch_group_tile<GroupTile<T, 256, 256, 2, 4, ATR, BTR, EPI, GROUP>>(A, s);
-    case kGroup128: return launch_group_tile<GroupTile<T, 128, 128, 2, 2, ATR, BTR, EPI, GROUP>>(A, s);
-    case kGroup64x128: return launch_group_tile<GroupTile<T, 64, 128, 2, 2, ATR, BTR, EPI, GROUP>>(A, s);
+    case kGroup256: return launch_group_tile<GroupTile<T, 256, 256, 2, 4, ATR, BTR, EPI, GROUP, true>>(A, s);
+    case kGroup128: return launch_group_tile<GroupTile<T, 128, 128, 2, 2, ATR, BTR, EPI, GROUP, true>>(A, s);
+    case kGroup64x128: return launch_group_tile<GroupTile<T, 64, 128, 2, 2, ATR, BTR, EPI, GROUP, true>>(A, s);
     }
     return hipErrorInvalidValue;
 }

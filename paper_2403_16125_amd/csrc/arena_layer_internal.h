@@ -76,6 +76,7 @@ struct GemmArgs {
     // (se).  With pairs = 1 every group's two products are neighbouring batch indices
     const int32_t* offsets;   // [groups + 1], held inside 0 .. rows
     int32_t groups;
+    int32_t any;              // an operand's rows start on any value (tiles of 128 columns)
     // wide: C = alpha factor[0] product + beta e, e in 32 bits or in C's type
     const float* factor;      // nullable
     int32_t e_f32;

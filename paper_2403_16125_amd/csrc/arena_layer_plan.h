@@ -289,8 +289,9 @@ constexpr GroupCost kGroupCost[mm::kGroupKinds] = {
 // many tiles there are is known, and the last round counts as what it is; otherwise half a
 // round more than they fill.
 inline double group_time(double tiles, double steps, int kind, int64_t splits, double bytes, double uneven,
-                         bool exact)
+                         bool exact, bool any)
 {
+    if (any && kind == mm::kGroup256) return INFINITY;
     const GroupCost& k = kGroupCost[kind];
     const double per = std::ceil(steps / splits), values = (double)mm::kGroupRows[kind] * mm::kGroupCols[kind];
     const double end = values * (splits > 1 ? 4.0 : bytes) / kEpilogueRate;
@@ -311,16 +312,16 @@ struct GroupCut {
 };
 
 inline GroupCut choose_groups(int64_t M, int64_t N, int64_t steps, int64_t batch, double bytes, bool split, double uneven,
-                              bool exact)
+                              bool exact, bool any)
 {
     using namespace mm;
-    GroupCut best = {kGroup256, 1, 0};
+    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0};
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * batch;
         for (int s = 1; s <= 16 && (s == 1 || (split && s * 4 <= steps)); ++s) {
             if (tiles * s > 0x7fffffff) continue;
-            const double t = group_time((double)tiles, (double)steps, kind, s, bytes, uneven, exact);
+            const double t = group_time((double)tiles, (double)steps, kind, s, bytes, uneven, exact, any);
             if (t < least) {
                 least = t;
                 best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0};

@@ -69,9 +69,9 @@ arena_status check_loss_grads(arena_ctx* c, const char* who, const arena_loss_de
 }
 
 // The kind of tile for a product with k whole; bytes: what the epilogue moves for a value.
-int choose_whole(int64_t M, int64_t N, int64_t steps, double bytes)
+int choose_whole(int64_t M, int64_t N, int64_t steps, double bytes, bool any)
 {
-    return choose_groups(M, N, steps, 1, bytes, false, 1.0, true).kind;
+    return choose_groups(M, N, steps, 1, bytes, false, 1.0, true, any).kind;
 }
 
 LossArgs loss_args(const arena_loss_desc* d)
@@ -93,18 +93,16 @@ bool few_tokens(const arena_loss_desc* d) { return d->tokens <= 16; }
 
 struct LossPlan {
     Pieces w;
-    bool skinny;
-    Operand x, weight;
+    bool skinny, any;
     int64_t piece;            // tokens
     int kind;
     int64_t columns;          // of tiles
     void *stats, *picked;
     LossPlan(const arena_loss_desc* d, void* base)
         : w(base), skinny(few_tokens(d)),
-          x(w, d->x, d->ld_x, d->tokens, d->model, skinny || Operand::direct(d->x, d->ld_x, d->model)),
-          weight(w, d->w, d->ld_w, d->vocabulary, d->model, skinny || Operand::direct(d->w, d->ld_w, d->model)),
+          any(!Operand::direct(d->x, d->ld_x, d->model) || !Operand::direct(d->w, d->ld_w, d->model)),
           piece(std::min(d->tokens, kTokenPiece)),
-          kind(choose_whole(piece, d->vocabulary, ceil_div(d->model, arena::mm::kBK), 0.5)),
+          kind(choose_whole(piece, d->vocabulary, ceil_div(d->model, arena::mm::kBK), 0.5, any)),
           columns(ceil_div(d->vocabulary, skinny ? arena::mm::kSkinnyCols : arena::mm::kGroupCols[kind]))
     {
         stats = w.take(8 * piece * columns);
@@ -114,12 +112,12 @@ struct LossPlan {
 
 struct LossBackPlan {
     Pieces w;
-    Operand weight;
+    bool any;                         // the weight's rows start on any value
     int64_t piece, ld_x, ld_g;        // entries of a piece; rows of the copy of x and of the logits' gradient
     bool many;                        // pieces: dx is summed in 32 bits
     void *rows, *scale, *x, *g, *sum, *part;
     LossBackPlan(const arena_loss_desc* d, const arena_loss_grads* o, void* base)
-        : w(base), weight(w, d->w, d->ld_w, d->vocabulary, d->model, Operand::direct(d->w, d->ld_w, d->model))
+        : w(base), any(!Operand::direct(d->w, d->ld_w, d->model))
     {
         const int64_t T = d->tokens, V = d->vocabulary, D = d->model;
         piece = V;
@@ -135,18 +133,18 @@ struct LossBackPlan {
         sum = w.take(many && o->dx ? 4 * T * D : 0);
         int64_t most = 0;
         for (int64_t n : {piece, V - (V - 1) / piece * piece}) {
-            if (o->dx && T > 0) most = std::max(most, cut_dx(T, D, n).part);
+            if (o->dx && T > 0) most = std::max(most, cut_dx(T, D, n, any).part);
             if (o->dw) most = std::max(most, cut_dw(T, D, n).part);
         }
         part = w.take(most);
     }
-    static GroupCut cut_dx(int64_t T, int64_t D, int64_t n)
+    static GroupCut cut_dx(int64_t T, int64_t D, int64_t n, bool any)
     {
-        return choose_groups(T, D, ceil_div(n, arena::mm::kBK), 1, 4.0, true, 1.0, true);
+        return choose_groups(T, D, ceil_div(n, arena::mm::kBK), 1, 4.0, true, 1.0, true, any);
     }
     static GroupCut cut_dw(int64_t T, int64_t D, int64_t n)
     {
-        return choose_groups(n, D, ceil_div(T, arena::mm::kBK), 1, 2.0, true, 1.0, true);
+        return choose_groups(n, D, ceil_div(T, arena::mm::kBK), 1, 2.0, true, 1.0, true, false);
     }
 };
 
@@ -177,14 +175,14 @@ arena_status arena_cross_entropy_forward(arena_ctx* c, const arena_loss_desc* d,
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
-    hipError_t e = pack({&P.x, &P.weight}, s);
-    if (e) return hip_error(c, e, "cross entropy copies");
+    hipError_t e;
     const int wide = d->target_dtype == ARENA_I64 ? 8 : 4;
     for (int64_t t = 0; t < d->tokens; t += P.piece) {
         const int64_t n = std::min(P.piece, d->tokens - t);
         GemmArgs A = new_args(n, d->vocabulary, d->model);
-        A.a[0] = (const char*)P.x.p + 2 * t * P.x.ld; A.lda = P.x.ld;
-        A.b[0] = P.weight.p; A.ldb = P.weight.ld;
+        A.any = P.any;
+        A.a[0] = (const char*)d->x + 2 * t * d->ld_x; A.lda = d->ld_x;
+        A.b[0] = d->w; A.ldb = d->ld_w;
         A.target = (const char*)d->target + t * wide;
         A.target_wide = wide == 8;
         A.stats = (float*)P.stats;
@@ -235,8 +233,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
     using namespace arena::mm;
-    hipError_t e = T > 0 ? pack({&P.weight}, s) : hipSuccess;
-    if (e) return hip_error(c, e, "cross entropy backward copies");
+    hipError_t e;
     LossArgs L = loss_args(f);
     L.dloss = g->dloss;
     L.s_dloss = g->stride_dloss;
@@ -250,31 +247,33 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
     const int size = bytes_of(g->grad_dtype);
     for (int64_t v = 0; v < V; v += P.piece) {
         const int64_t n = std::min(P.piece, V - v);
-        const void* w = (const char*)P.weight.p + 2 * v * P.weight.ld;
+        const void* w = (const char*)f->w + 2 * v * f->ld_w;
         if (T > 0) {
             GemmArgs A = new_args(T, n, D);
+            A.any = P.any;
             A.a[0] = P.x; A.lda = P.ld_x;
-            A.b[0] = w; A.ldb = P.weight.ld;
+            A.b[0] = w; A.ldb = f->ld_w;
             A.c[0] = P.g; A.ldc = P.ld_g;
             A.pad = (int)pad8(n);
             A.rows = (const LossRow*)P.rows;
             A.first_col = (int)v;
             A.splits = 1;
-            if ((e = launch_loss(A, f->dtype, kLossGradient, choose_whole(T, n, ceil_div(D, kBK), 2.0), s)))
+            if ((e = launch_loss(A, f->dtype, kLossGradient, choose_whole(T, n, ceil_div(D, kBK), 2.0, P.any), s)))
                 return hip_error(c, e, "cross entropy logits' gradient launch");
         }
         if (dx) {
             const bool first = v == 0, last = v + n == V;
             GemmArgs X = new_args(T, D, n);
+            X.any = P.any;
             X.a[0] = P.g; X.lda = P.ld_g;
-            X.b[0] = w; X.ldb = P.weight.ld;
+            X.b[0] = w; X.ldb = f->ld_w;
             X.c[0] = last ? g->dx : P.sum; X.ldc = last ? g->ld_dx : D;
             X.out = last ? kOut16 : kOutF32;
             X.e[0] = P.sum; X.lde = D; X.e_f32 = 1;
             X.beta = first ? 0.0f : 1.0f;
             X.factor = factor;
             X.part = (float*)P.part;
-            const GroupCut cut = P.cut_dx(T, D, n);
+            const GroupCut cut = P.cut_dx(T, D, n, P.any);
             X.splits = cut.splits;
             if ((e = launch_loss(X, f->dtype, kRowsCols, cut.kind, s)))
                 return hip_error(c, e, "cross entropy input gradient launch");
