@@ -33,8 +33,11 @@ struct GroupTile {
     static constexpr int kCols = DUAL ? BN / 2 : BN;
     static constexpr bool kLean = BM == 256 && (EPI == kGatedBwd || EPI == kWide);
     static constexpr int kSegs = GROUP == kRowGroups && EPI == kPlain && BTR ? 2 : 1;    // both halves of dx
-    // blocks on a compute unit, by their LDS (the groups' table is 8 to 12 KB)
-    static constexpr int kBlocks = 2 * (BM + BN) * 128 <= 65536 ? 2 : 1;
+    // Buffers.  The smallest tiles are those of products with few: there a step is as long as
+    // a load's way, unless it starts a step earlier.
+    static constexpr int kStages = BM == 64 && DIRECT_ ? 3 : 2;
+    // blocks on a compute unit, by their LDS (the groups' table is at most 12 KB)
+    static constexpr int kBlocks = kStages * (BM + BN) * 128 <= 73728 ? 2 : 1;
     static constexpr int kWavesEach = kThreads / 256 * kBlocks;
     static constexpr int kRun = 32 * kBlocks;            // tiles that an XCD has in work at once
     // bytes of a row that the epilogue reads, brought to the LDS with the tile's first step:
@@ -58,10 +61,12 @@ __device__ __forceinline__ int tile_of_xcd(int x, int q, int tiles)
 
 constexpr int kMostGroups = 1024;
 
-// Groups of rows: their first rows and ends, and how many tile rows end with the group.
+// Of every group its first row or step and its end, and of rows how many tile rows end with
+// the group; in the LDS behind the buffers, as long as there are groups.
 struct GroupTable {
-    int first[kMostGroups], end[kMostGroups];
-    int tiles[kMostGroups];
+    int *first, *end, *tiles;
+    __device__ __forceinline__ GroupTable(int* p, int groups) : first(p), end(p + groups), tiles(p + 2 * groups) {}
+    static int bytes(int group, int groups) { return group == kOneGroup ? 0 : (group == kRowGroups ? 12 : 8) * groups; }
 };
 
 // Offset g, held inside 0 .. rows whatever the offsets are.
@@ -69,28 +74,6 @@ __device__ __forceinline__ int group_end(const int32_t* offsets, int g, int rows
 {
     return min(max(offsets[g], 0), rows);
 }
-
-// Groups of steps: first steps and ends.
-struct StepTable {
-    int first[kMostGroups], end[kMostGroups];
-};
-
-struct NoTable {};
-
-template <int GROUP>
-struct TableOf {
-    typedef NoTable Type;
-};
-
-template <>
-struct TableOf<kRowGroups> {
-    typedef GroupTable Type;
-};
-
-template <>
-struct TableOf<kStepGroups> {
-    typedef StepTable Type;
-};
 
 // Rows of group g and the tile rows that they make.
 template <int BM>
@@ -107,7 +90,7 @@ __device__ __forceinline__ int tile_rows(const GemmArgs& A, int g, int* lo, int*
 // Fills the table (one wave) and returns how many tile rows there are, at most `most`:
 // groups that overlap could have more than a launch counts.
 template <int BM>
-__device__ __forceinline__ int fill_table(const GemmArgs& A, GroupTable* table, int lane, int most)
+__device__ __forceinline__ int fill_table(const GemmArgs& A, const GroupTable* table, int lane, int most)
 {
     int total = 0;
     for (int g0 = 0; g0 < A.groups; g0 += 64) {
@@ -450,14 +433,17 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     constexpr bool kRows = P::GROUP == kRowGroups, kSteps = P::GROUP == kStepGroups;
     __shared__ __attribute__((aligned(16))) char sa0[P::BM * 128];
     __shared__ __attribute__((aligned(16))) char sa1[P::BM * 128];
+    __shared__ __attribute__((aligned(16))) char sa2[P::kStages > 2 ? P::BM * 128 : 16];
     __shared__ __attribute__((aligned(16))) char sb0[P::BN * 128];
     __shared__ __attribute__((aligned(16))) char sb1[P::BN * 128];
-    __shared__ typename TableOf<P::GROUP>::Type table;
-    __shared__ __attribute__((aligned(16))) char rows0[P::kRowBytes ? P::BM * P::kRowBytes : 16];
-    __shared__ __attribute__((aligned(16))) char rows1[P::kRowBytes ? P::BM * P::kRowBytes : 16];
+    __shared__ __attribute__((aligned(16))) char sb2[P::kStages > 2 ? P::BN * 128 : 16];
+    constexpr int kRowsEach = P::BM * P::kRowBytes;
+    __shared__ __attribute__((aligned(16))) char row_data[P::kRowBytes ? 2 * kRowsEach : 16];
     __shared__ f32x2 stats[P::EPI == kLossStats ? P::BM * P::WN : 1];
-    auto bufa = [&](int i) { return i == 0 ? sa0 : sa1; };
-    auto bufb = [&](int i) { return i == 0 ? sb0 : sb1; };
+    extern __shared__ int table_data[];
+    const GroupTable table(table_data, A.groups);
+    auto bufa = [&](int i) { return i == 0 ? sa0 : i == 1 ? sa1 : sa2; };
+    auto bufb = [&](int i) { return i == 0 ? sb0 : i == 1 ? sb1 : sb2; };
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
@@ -638,24 +624,33 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             __builtin_amdgcn_sched_group_barrier(0x008, each, 0);       // products
         }
     };
-    // Waits for a step's loads.  In a tile's first step the stores of the tile before, which
-    // were issued later, may be left: operations complete in order.  kStores is the least
-    // that a whole tile's epilogue issues; after another one everything is awaited.
+    // Waits for a step's loads.  After them the loads of the step behind may be in flight (three
+    // buffers) and, in the first steps of a tile, the stores of the tile before, which were
+    // issued later: operations complete in order, so that many may be left.  kStores is the
+    // least that a whole tile's epilogue issues; after another one everything is awaited.
+    constexpr int kAhead = P::kStages - 1, kLoads = la.kChunks + lb.kChunks;
     constexpr int kStores = P::FM * P::FN / (P::DUAL ? 4 : 2);
-    static_assert(P::FM % 2 == 0 && kStores < 64, "rows in pairs, stores counted in six bits");
+    static_assert(P::FM % 2 == 0 && kLoads + kStores < 64, "rows in pairs, operations counted in six bits");
     bool stored = false, idle = false;
-    auto arrive = [&](int step) {
+    auto arrive = [&](int step, int steps) {
         asm volatile("" ::: "memory");
-        if (!P::kDirect && !(P::kRowBytes && step == 0)) __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);    // LDS writes
-        else if (stored && step == 0) wait_loads<kStores>();
-        else wait_loads<0>();
+        if (!P::kDirect && !(P::kRowBytes && step == 0)) {
+            __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);    // LDS writes
+        } else if (kAhead == 2 && step + 1 < steps) {
+            if (stored && step < 2) wait_loads<kLoads + kStores>();
+            else wait_loads<kLoads>();
+        } else {
+            if (stored && step < kAhead) wait_loads<kStores>();
+            else wait_loads<0>();
+        }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
     // One step, from buffer u: see tile_product in arena_gemm.h.
     auto turn = [&](const Work& w, int step, int u, bool first) {
-        arrive(step);
-        if (step + 1 < w.steps) fetch(w, step + 1, bufa(u ^ 1), bufb(u ^ 1));
+        arrive(step, w.steps);
+        constexpr int kNext = P::kStages;
+        if (step + kAhead < w.steps) fetch(w, step + kAhead, bufa((u + kAhead) % kNext), bufb((u + kAhead) % kNext));
         if (!(kRows && idle)) {
             __builtin_amdgcn_sched_barrier(0);
             read(bufa(u), bufb(u), 0, fa0, fb0);
@@ -673,11 +668,13 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
     Work w;
     if (!next_work(&w)) return;
     begin(&w);
-    fetch_rows(w, rows0);
-    if (w.steps > 0) {
-        fetch(w, 0, bufa(0), bufb(0));
-        commit(bufa(0), bufb(0));
-    }
+    fetch_rows(w, row_data);
+    auto fetch_first = [&](const Work& w) {
+        if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+        if (kAhead == 2 && w.steps > 1) fetch(w, 1, bufa(1), bufb(1));
+    };
+    fetch_first(w);
+    if (w.steps > 0) commit(bufa(0), bufb(0));
     bool odd = false;             // which rows are the tile's
     for (;;) {
 #pragma unroll
@@ -688,10 +685,10 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         idle = kRows && w.m0 + wm * (P::BM / P::WM) >= w.m_end;
         if (steps > 0) {
             turn(w, 0, 0, true);
-            for (int s = 1; s < steps; s += 2) {
-                turn(w, s, 1, false);
-                if (s + 1 < steps) turn(w, s + 1, 0, false);
-            }
+            for (int s = 1; s < steps; s += P::kStages)
+#pragma unroll
+                for (int u = 0; u < P::kStages; ++u)
+                    if (s + u < steps) turn(w, s + u, (u + 1) % P::kStages, false);
         }
         // every wave holds its last fragments: the buffers are free for the next tile
         asm volatile("" ::: "memory");
@@ -703,8 +700,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         const bool more = next_work(&w);
         if (more) {
             begin(&w);
-            fetch_rows(w, odd ? rows0 : rows1);
-            if (w.steps > 0) fetch(w, 0, bufa(0), bufb(0));
+            fetch_rows(w, row_data + (odd ? 0 : kRowsEach));
+            fetch_first(w);
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -715,7 +712,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         const int mw = done.m0 + wm * (P::BM / P::WM) + (l & 15);
         const int nw = done.n0 + wn * (P::DUAL ? P::BN / P::WN / 2 : P::BN / P::WN) + 16 * (l >> 4 & 1) + 8 * (l >> 5);
         const int n_end = P::kUpToN ? A.N : A.pad;
-        const char* const rows = odd ? rows1 : rows0;
+        const char* const rows = row_data + (odd ? kRowsEach : 0);
         odd = !odd;
         auto row_out = [&](int m, const f32x4 (&row)[P::FN]) {
             constexpr int kSide = P::EPI == kLossGrad || P::EPI == kLossStats ? kPlain : P::EPI;
@@ -738,9 +735,9 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
                                       done.m0 / P::BM * A.tiles_n + done.n0 / P::kCols;
                     put(A.part + t * (P::BM * P::BN) + (m - done.m0) * P::kCols + n - done.n0, v, 8);
                 } else if constexpr (P::EPI == kGatedFwd) {
-                    gated_fwd_out<T>(A, m, n, v, u);
+                    gated_fwd_out<T, kGeluShort>(A, m, n, v, u);
                 } else if constexpr (P::EPI == kGatedBwd) {
-                    gated_bwd_out<T>(A, m, n, v, side[j]);
+                    gated_bwd_out<T, kGeluShort>(A, m, n, v, side[j]);
                 } else if constexpr (P::EPI == kWide) {
                     plain_out<T>(A, done.z, m, n, v, side[j]);
                 } else if constexpr (P::EPI == kLossGrad) {
@@ -834,8 +831,13 @@ hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
                                            : (int64_t)A.tiles_m * A.tiles_n * A.batch * A.splits;
     if (tiles == 0) return hipSuccess;
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    const int64_t most = 256 * P::kBlocks, grid = (std::min(tiles, most) + 7) / 8 * 8;
-    groups_kernel<P><<<(unsigned)grid, P::kThreads, 0, s>>>(A, (int)tiles);
+    // as many blocks as the compute units hold: with many groups the table leaves room for one
+    const int table = GroupTable::bytes(P::GROUP, A.groups);
+    constexpr int kBuffers = P::kStages * (P::BM + P::BN) * 128 + (P::kRowBytes ? 2 * P::BM * P::kRowBytes : 16) +
+                             (P::EPI == kLossStats ? 8 * P::BM * P::WN : 8) + 64;
+    const int64_t blocks = P::kBlocks > 1 && kBuffers + table > 163840 / 2 ? 1 : P::kBlocks;
+    const int64_t grid = (std::min(tiles, 256 * blocks) + 7) / 8 * 8;
+    groups_kernel<P><<<(unsigned)grid, P::kThreads, table, s>>>(A, (int)tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits <= 1) return e;
     if constexpr (P::EPI == kWide) {
@@ -930,7 +932,7 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArg
             *(f32x4*)fv = v;
             *(f32x4*)fu = u;
             if constexpr (EPI == kGatedFwd) {
-                if (m < hi && n < A.pad) gated_fwd_out<T>(A, m, n, fv, fu);
+                if (m < hi && n < A.pad) gated_fwd_out<T, kGeluShort>(A, m, n, fv, fu);
             } else if constexpr (EPI == kLossStats) {
                 const int64_t at = min(m, hi - 1);
                 const int target = ((const int32_t*)A.target)[at << A.target_wide];       // its lower half

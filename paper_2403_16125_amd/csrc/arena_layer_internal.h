@@ -21,7 +21,7 @@ constexpr int kMaxLd = 1 << 22;         // row stride limit, elements: 256 rows 
 
 enum Epi { kPlain = 0, kGatedFwd = 1, kGatedBwd = 2, kPlainRest = 3, kWide = 4, kLossStats = 5, kLossGrad = 6 };
 enum Out { kOut16 = 0, kOutF32 = 1, kOutBf16 = 2 };   // the operands' own type, float, bf16
-enum Act { kSilu = 0, kGelu = 1, kRelu = 2 };
+enum Act { kSilu = 0, kGelu = 1, kRelu = 2, kGeluShort = 3 };
 // Products whose rows or steps come in groups (experts) of lengths that only the
 // device knows: rows offsets[g] .. offsets[g + 1] - 1 of A and C meet matrix g of B, or
 // those steps of k of both operands make matrix g of C.
@@ -128,8 +128,9 @@ constexpr int64_t group_tiles(int64_t M, int64_t groups, int64_t side)
     return M / side + (groups < M ? groups : M);
 }
 
-// Tiles of the products of groups, two buffers each: 256 x 256 (8 waves, one block on a
-// compute unit), 128 x 128 and 64 x 128 (4 waves, two blocks).
+// Tiles of the products of groups: 256 x 256 (8 waves, two buffers, one block on a compute
+// unit), 128 x 128 (4 waves, two buffers, two blocks) and 64 x 128 (4 waves, three buffers,
+// two blocks).
 enum GroupKind { kGroup256 = 0, kGroup128, kGroup64x128, kGroupKinds };
 constexpr int kGroupRows[kGroupKinds] = {256, 128, 64}, kGroupCols[kGroupKinds] = {256, 128, 128};
 
