@@ -33,12 +33,11 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs A)
 {
     const Pack p = A.p[blockIdx.y];
     const int per = (int)(p.ld_to / 8);
-    const int64_t n = p.batch * p.rows * per;
+    const int64_t n = p.rows * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per;
         const int c = (int)(i % per) * 8;
-        const int64_t z = p.batch > 1 ? r / p.rows : 0;
-        const uint16_t* from = (const uint16_t*)p.from + z * p.stride + (r - z * p.rows) * p.ld_from + c;
+        const uint16_t* from = (const uint16_t*)p.from + r * p.ld_from + c;
         u32x4 v = {0, 0, 0, 0};
         if (c + 8 <= p.cols) {
             __builtin_memcpy(&v, from, 16);
@@ -59,7 +58,7 @@ hipError_t launch_packs(const Pack* packs, int n, hipStream_t s)
     int64_t most = 0;
     int k = 0;
     for (int i = 0; i < n && k < kMaxPacks; ++i) {
-        const int64_t chunks = packs[i].batch * packs[i].rows * (packs[i].ld_to / 8);
+        const int64_t chunks = packs[i].rows * (packs[i].ld_to / 8);
         if (chunks == 0) continue;
         A.p[k++] = packs[i];
         most = chunks > most ? chunks : most;

@@ -326,8 +326,9 @@ struct LeanLoader {
 // there to the LDS once the step before is multiplied.  Lays the same chunks in the same
 // places.  A chunk that a row's end cuts is read whole where another row follows in the matrix
 // (a row further on along k it is masked; columns past the last make columns of C that are not
-// written), and value by value in the matrix's last row.  The up matrix has a row stride of its
-// own.
+// written), and value by value in the matrix's last row, or in every row where rows are
+// shorter than a chunk: there the next one may not hold what is left of it.  The up matrix has a
+// row stride of its own.
 template <typename P, int R, bool TR, bool DUAL>
 struct StagedLoader : LeanLoader<P, R, TR, DUAL> {
     typedef LeanLoader<P, R, TR, DUAL> Base;
@@ -367,14 +368,15 @@ struct StagedLoader : LeanLoader<P, R, TR, DUAL> {
             const bool up = DUAL && Dual<P::BN / P::WN>::up(it * kEach + wave * 8);
             const char* p = up ? p1 : p0;
             const uint32_t pitch = (uint32_t)(up ? ld1 : ld0) * 2;
+            const bool slim = pitch < 16;
             if (TR) {
                 const int k = row + it * kEach;
                 int col = at ^ (kEach % 32 == 0 ? 0 : ((it * kEach >> 3 & 3) << 2 & (Base::kGran - 1)) << 4);
                 col = col < Base::last ? col : 0;
                 const char* src = p + (uint32_t)k * pitch + (uint32_t)col * 2;
-                if (left > kBK) v[it] = whole(src);
+                if (left > kBK && !slim) v[it] = whole(src);
                 else if (k >= left) v[it] = u32x4{0, 0, 0, 0};
-                else if (k == left - 1 && col + 8 > Base::last) v[it] = some(src, Base::last - col);
+                else if ((slim || k == left - 1) && col + 8 > Base::last) v[it] = some(src, Base::last - col);
                 else v[it] = whole(src);
             } else {
                 const int r = min(row + (DUAL ? Dual<P::BN / P::WN>::row(it * kEach) : it * kEach), Base::last - 1);
@@ -382,7 +384,7 @@ struct StagedLoader : LeanLoader<P, R, TR, DUAL> {
                 const char* src = p + (uint32_t)r * pitch + (uint32_t)at;
                 if (left >= kBK) v[it] = whole(src);
                 else if (n <= 0) v[it] = u32x4{0, 0, 0, 0};
-                else if (n < 8 && r == Base::last - 1) v[it] = some(src, n);
+                else if (n < 8 && (slim || r == Base::last - 1)) v[it] = some(src, n);
                 else v[it] = masked(whole(src), n);
             }
         }
@@ -579,17 +581,16 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             pb += P::BTR ? at * (int64_t)ld * (2 * kBK) : at * (2 * kBK);
             la.load(pa, pa, (int)A.lda, (int)A.lda, tid, left);
             lb.load(pb, P::DUAL ? b1 + at * (2 * kBK) : pb, ld, (int)A.ldb1, tid, left);
-            return;
-        }
-        pb += at * lb.pitch();
-        const char* pu = P::DUAL ? b1 + at * lb.pitch() : pb;
-        if constexpr (!P::kDirect) {
-        } else if (left < kBK) {
-            la.template fetch<true>(pa, pa, sa, tid, left);
-            lb.template fetch<true>(pb, pu, sb, tid, left);
         } else {
-            la.template fetch<false>(pa, pa, sa, tid, left);
-            lb.template fetch<false>(pb, pu, sb, tid, left);
+            pb += at * lb.pitch();
+            const char* pu = P::DUAL ? b1 + at * lb.pitch() : pb;
+            if (left < kBK) {
+                la.template fetch<true>(pa, pa, sa, tid, left);
+                lb.template fetch<true>(pb, pu, sb, tid, left);
+            } else {
+                la.template fetch<false>(pa, pa, sa, tid, left);
+                lb.template fetch<false>(pb, pu, sb, tid, left);
+            }
         }
     };
 
