@@ -125,7 +125,7 @@ SortArgs sort_args(const arena_sort_desc* d, int64_t* bytes)
     A.offsets = d->offsets;
     A.row = d->row;
     A.counts = (int32_t*)d->workspace;
-    arena::sort_plan(A.choices, A.experts, &A.blocks, &A.each);
+    arena::sort_plan(A.choices, &A.blocks, &A.each);
     *bytes = A.blocks > 1 ? pad256(4 * (int64_t)A.blocks * A.experts) : 0;
     return A;
 }

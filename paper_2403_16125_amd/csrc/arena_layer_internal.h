@@ -155,13 +155,11 @@ constexpr int kSkinnyRows = 32;         // rows of A (tokens) that the kernel wi
 hipError_t launch_skinny(const GemmArgs& A, int dtype, bool dual, hipStream_t s);
 
 // Copies of matrices of 16-bit values, rows x cols, with zeros in columns cols ..
-// ld_to - 1; one launch.  batch: so many matrices, `stride` values apart, copied one
-// behind the other.
+// ld_to - 1; one launch.
 struct Pack {
     const void* from;
     void* to;
     int64_t ld_from, ld_to, rows, cols;
-    int64_t batch = 1, stride = 0;
 };
 constexpr int kMaxPacks = 5;
 hipError_t launch_packs(const Pack* packs, int n, hipStream_t s);
@@ -225,7 +223,7 @@ struct SortArgs {
 };
 
 constexpr int kSortThreads = 1024;
-void sort_plan(int64_t choices, int experts, int* blocks, int* each);
+void sort_plan(int64_t choices, int* blocks, int* each);
 hipError_t launch_sort(const SortArgs& A, hipStream_t s);
 
 // One row of x (dispatch), y, dy or dx a token; one of xs, ys, dys or dxs a choice.

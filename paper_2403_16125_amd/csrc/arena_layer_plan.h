@@ -236,27 +236,21 @@ struct Operand {
     int64_t ld;
     const void* from = nullptr;
     int64_t ld_from = 0, rows = 0, cols = 0;
-    int64_t batch, stride, stride_from = 0;      // matrices, and values between them
     void* copy = nullptr;
 
     static bool direct(const void* p, int64_t ld, int64_t cols) { return aligned(p, 16) && ld % 8 == 0 && cols % 8 == 0; }
 
-    Operand(Pieces& w, const void* q, int64_t ld_q, int64_t rows_, int64_t cols_, bool in_place, int64_t batch_ = 1,
-            int64_t stride_ = 0)
+    Operand(Pieces& w, const void* q, int64_t ld_q, int64_t rows_, int64_t cols_, bool in_place)
     {
         p = q;
         ld = ld_q;
-        batch = batch_;
-        stride = stride_;
         if (in_place) return;
-        stride_from = stride;
         from = q;
         ld_from = ld_q;
         rows = rows_;
         cols = cols_;
         ld = pad8(cols);
-        stride = rows * ld;
-        copy = w.take(2 * batch * stride);
+        copy = w.take(2 * rows * ld);
         p = copy;
     }
 
@@ -269,7 +263,7 @@ inline hipError_t pack(std::initializer_list<const Operand*> operands, hipStream
     int n = 0;
     for (const Operand* o : operands)
         if (o->copy && n < arena::mm::kMaxPacks)
-            packs[n++] = {o->from, o->copy, o->ld_from, o->ld, o->rows, o->cols, o->batch, o->stride_from};
+            packs[n++] = {o->from, o->copy, o->ld_from, o->ld, o->rows, o->cols};
     return n ? arena::mm::launch_packs(packs, n, s) : hipSuccess;
 }
 

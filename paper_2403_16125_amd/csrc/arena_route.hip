@@ -618,9 +618,8 @@ hipError_t launch_route_backward(const RouteArgs& A, int dtype, hipStream_t s) {
 
 // One block up to 4096 choices; past that at most 128 blocks of whole chunks, whose
 // counts every block reads.
-void sort_plan(int64_t choices, int experts, int* blocks, int* each)
+void sort_plan(int64_t choices, int* blocks, int* each)
 {
-    (void)experts;
     *blocks = 1;
     *each = (int)choices;
     if (choices <= 4096) return;
