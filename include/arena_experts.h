@@ -12,7 +12,7 @@
  * The conventions, types, workspaces and limits of arena_layer.h hold here.  Index
  * and offset values lie in device memory, where the host cannot check them: the
  * kernels hold every one inside its range, as said at each call, so none of them can
- * lead a read or write out of a tensor.
+ * lead a read or write out of a tensor.  Outputs overlap neither inputs nor each other.
  */
 #ifndef ARENA_EXPERTS_H
 #define ARENA_EXPERTS_H

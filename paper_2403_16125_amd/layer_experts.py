@@ -202,6 +202,12 @@ class ExpertOps:
 
     # -- checks
 
+    @staticmethod
+    def _within(name, value, bits, least=1):
+        """A number that the descriptors' fields would cut off is refused."""
+        if not least <= value < 1 << (bits - 1):
+            raise ValueError(f"{name} is {value}")
+
     def _whole(self, name, t, shape):
         """Address and type of a contiguous tensor of int32 or int64."""
         wide = t.dtype is self.torch.int64
@@ -249,9 +255,8 @@ class ExpertOps:
         return d
 
     def _route(self, handle, logits, k, normalise, scale):
+        self._within("k", k, 32)
         d = self._route_desc(logits, k, normalise, scale)
-        if k < 1:
-            raise ValueError(f"k is {k}")
         shape = logits.shape[:-1] + (k,)
         index, weight = self._empty(shape, self.torch.int32), self._empty(shape, self.torch.float32)
         d.index, d.weight = index.data_ptr(), weight.data_ptr()
@@ -281,11 +286,10 @@ class ExpertOps:
         return self._run(stream, (index,), self._sort_by_expert, index, experts)
 
     def _sort_by_expert(self, handle, index, experts):
+        self._within("experts", experts, 32)
         p, kind = self._whole("index", index, index.shape)
         if index.dim() < 1:
             raise ValueError("index needs an axis of choices")
-        if experts < 1:
-            raise ValueError(f"experts is {experts}")
         tokens, k = self._rows(index)
         plan = ExpertPlan(self._empty((experts + 1,), self.torch.int32), self._empty(index.shape, self.torch.int32))
         d = SortDesc(index_dtype=kind, experts=experts, tokens=tokens, k=k, index=p, offsets=plan.offsets.data_ptr(),
@@ -426,6 +430,7 @@ class ExpertOps:
     # -- cross entropy over a vocabulary
 
     def _loss_desc(self, x, w, target, ignore_index):
+        self._within("ignore_index", ignore_index, 64, -1 << 63)
         tokens, model = self._rows(x)
         d = LossDesc(dtype=self._type(x), tokens=tokens, model=model, vocabulary=w.shape[0], ignore_index=ignore_index)
         d.x, d.ld_x = self._matrix("x", x, (tokens, model), x.dtype)

@@ -245,6 +245,21 @@ def test_loss_workspaces_are_bounded(ctx):
 
 # ---------------------------------------------------------------- the binding's own checks
 
+def test_binding_refuses_numbers_that_its_fields_would_cut_off():
+    ops = layer.LayerOps()
+    ops._current = lambda index: types.SimpleNamespace(cuda_stream=0)
+    x, index = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32)
+    for k in (0, -1, 2 ** 31, 2 ** 32 + 2):
+        with pytest.raises(ValueError, match="k is"):
+            ops.route(x, k)
+        with pytest.raises(ValueError, match="experts is"):
+            ops.sort_by_expert(index, k)
+    for ignore in (2 ** 63, -2 ** 63 - 1, 2 ** 64):        # the last would be entry 0
+        with pytest.raises(ValueError, match="ignore_index is"):
+            ops.cross_entropy_forward(x.bfloat16(), x.bfloat16(), index[:, 0], ignore_index=ignore)
+    ops.close()
+
+
 def test_binding_refuses_what_is_not_on_the_device():
     ops = layer.LayerOps()
     ops._current = lambda index: types.SimpleNamespace(cuda_stream=0)      # no GPU is asked
