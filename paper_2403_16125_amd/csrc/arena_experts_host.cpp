@@ -257,21 +257,27 @@ bool even(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts)
     return Operand::direct(p, ld, cols) && (experts == 1 || stride % 8 == 0);
 }
 
-// The kind of tile for a product of groups of rows: how they fall is not known here, so
-// each group that can have rows is taken to waste half a tile.
-int choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes, bool any)
+// The kind of tile and the parts of k for a product of groups of rows: how they fall is not
+// known here, so each group that can have rows is taken to waste half a tile.  The parts are
+// matrices of all rows.
+GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes, bool any)
 {
     using namespace arena::mm;
-    int best = any ? kGroup128 : kGroup256;
+    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0};
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
         const double tm = std::max((double)some, (double)rows / kGroupRows[kind] + 0.5 * some);
         if (group_tiles(rows, groups, kGroupRows[kind]) * tn > 0x7fffffff) continue;
-        const double t = group_time(tm * tn, (double)steps, kind, 1, bytes, 1.0, false, any);
-        if (t < least) {
-            least = t;
-            best = kind;
+        for (int s = 1; s <= 16 && (s == 1 || (!dual && kind != kGroup256 && s * 4 <= steps)); ++s) {
+            if (s > 1 && tm * tn * s > 2.0 * kUnits) break;      // more blocks than there is room for
+            const int64_t part = s > 1 ? 4 * s * rows * pad8(N) : 0;
+            const double t = group_time(tm * tn * s, std::ceil((double)steps / s), kind, 1, s > 1 ? 4.0 : bytes, 1.0, false,
+                                        any) + (s > 1 ? kJoin + part * 1e-6 / kJoinRate : 0.0);
+            if (t < least) {
+                least = t;
+                best = {kind, s, part};
+            }
         }
     }
     return best;
@@ -305,6 +311,21 @@ struct Uneven {
     }
 };
 
+struct ExpertsPlan {
+    Pieces w;
+    Uneven any;
+    GroupCut up, down;
+    void* part;
+    ExpertsPlan(const arena_experts_desc* d, void* base) : w(base), any(d), up{0, 1, 0}, down{0, 1, 0}, part(nullptr)
+    {
+        if (d->rows == 0 || few_rows(d)) return;
+        using arena::mm::kBK;
+        up = choose_rows(d->rows, d->experts, d->inner, ceil_div(d->model, kBK), true, d->g ? 4.0 : 1.0, any.x || any.up);
+        down = choose_rows(d->rows, d->experts, d->model, ceil_div(d->inner, kBK), false, 2.0, any.down);
+        part = w.take(down.part);
+    }
+};
+
 struct ExpertsBackPlan {
     Pieces w;
     Uneven any;
@@ -312,7 +333,7 @@ struct ExpertsBackPlan {
     int64_t ld;               // rows of dg and du
     void *dg, *du, *part;
     bool pair;                // both weight gradients of the first products in one launch
-    GroupCut cut_up, cut_down;
+    GroupCut cut_h, cut_x, cut_up, cut_down;
     ExpertsBackPlan(const arena_experts_desc* d, const arena_experts_grads* g, void* base)
         : w(base), any(d), dy_any(!even(g->dy, g->ld_dy, d->model, 0, 1))
     {
@@ -324,7 +345,14 @@ struct ExpertsBackPlan {
         const double bytes = bytes_of(g->grad_dtype) * (g->accumulate ? 2.0 : 1.0);
         cut_up = choose_steps(d->inner, d->model, d->rows, d->experts, pair ? 2 : 1, bytes, any.x);
         cut_down = choose_steps(d->model, d->inner, d->rows, d->experts, 1, bytes, dy_any);
-        part = w.take(std::max(g->dw_gate || g->dw_up ? cut_up.part : 0, g->dw_down ? cut_down.part : 0));
+        cut_h = cut_x = {0, 1, 0};
+        if (d->rows > 0 && (g->dx || g->dw_gate || g->dw_up))
+            cut_h = choose_rows(d->rows, d->experts, d->inner, ceil_div(d->model, arena::mm::kBK), false, 10.0,
+                                dy_any || any.down);
+        if (d->rows > 0 && g->dx)
+            cut_x = choose_rows(d->rows, d->experts, d->model, 2 * ceil_div(d->inner, arena::mm::kBK), false, 2.0, any.up);
+        part = w.take(std::max({g->dw_gate || g->dw_up ? cut_up.part : 0, g->dw_down ? cut_down.part : 0, cut_h.part,
+                                cut_x.part}));
     }
 };
 
@@ -461,7 +489,7 @@ arena_status arena_experts_forward_workspace(arena_ctx* c, const arena_experts_d
     if (!bytes) return ctx_fail(c, ARENA_ERR_INVALID_ARG, "experts forward: bytes is NULL");
     const arena_status s = check_experts(c, "experts forward", d, false);
     if (s) return s;
-    *bytes = 0;
+    *bytes = ExpertsPlan(d, nullptr).w.used;
     return ARENA_OK;
 }
 
@@ -471,11 +499,13 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     ctx_clear(c);
     arena_status st = check_experts(c, "experts forward", d, false);
     if (st || d->rows == 0) return st;
+    const ExpertsPlan P(d, d->workspace);
+    if ((st = check_workspace(c, "experts forward", d->workspace, d->workspace_bytes, P.w.used))) return st;
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
-    const int64_t R = d->rows, E = d->experts, bk = arena::mm::kBK;
-    const Uneven any(d);
+    const int64_t R = d->rows;
+    const Uneven& any = P.any;
     const bool few = few_rows(d);
     GemmArgs A = new_args(R, d->inner, d->model);
     A.offsets = d->offsets; A.groups = d->experts;
@@ -489,20 +519,18 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     A.act = d->activation;
     A.pad = (int)pad8(d->inner);
     hipError_t e = few ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kGateUp, s)
-                       : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp,
-                                                  choose_rows(R, E, d->inner, ceil_div(d->model, bk), true,
-                                                              d->g ? 4.0 : 1.0, A.any), s);
+                       : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp, P.up.kind, s);
     if (e) return hip_error(c, e, "experts gate and up launch");
     GemmArgs B = new_args(R, d->model, d->inner);
     B.offsets = d->offsets; B.groups = d->experts;
-    B.splits = 1;
+    B.splits = P.down.splits;
+    B.part = (float*)P.part;
     B.any = any.down;
     B.a[0] = d->h; B.lda = d->ld_inner;
     B.b[0] = d->w_down; B.ldb = d->ld_down; B.sb = d->stride_down;
     B.c[0] = d->y; B.ldc = d->ld_y;
     e = few ? arena::mm::launch_skinny_groups(B, d->dtype, arena::mm::kRowsRows, s)
-            : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows,
-                                       choose_rows(R, E, d->model, ceil_div(d->inner, bk), false, 2.0, B.any), s);
+            : arena::mm::launch_groups(B, d->dtype, arena::mm::kRowsRows, P.down.kind, s);
     return e == hipSuccess ? ARENA_OK : hip_error(c, e, "experts down launch");
 }
 
@@ -531,13 +559,14 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     DeviceScope scope(arena::ctx_device(c));
     if (scope.status != hipSuccess) return hip_error(c, scope.status, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
-    const int64_t R = f->rows, D = f->model, F = f->inner, E = f->experts, bk = arena::mm::kBK;
+    const int64_t R = f->rows, D = f->model, F = f->inner, E = f->experts;
     using namespace arena::mm;
     hipError_t e;
     if (R > 0 && (g->dx || g->dw_gate || g->dw_up)) {
         GemmArgs H = new_args(R, F, D);
         H.offsets = f->offsets; H.groups = f->experts;
-        H.splits = 1;
+        H.splits = P.cut_h.splits;
+        H.part = (float*)P.part;
         H.any = P.dy_any || P.any.down;
         H.a[0] = g->dy; H.lda = g->ld_dy;
         H.b[0] = f->w_down; H.ldb = f->ld_down; H.sb = f->stride_down;
@@ -545,7 +574,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
         H.c[0] = P.dg; H.c[1] = P.du; H.ldc = P.ld;
         H.act = f->activation;
         H.pad = (int)P.ld;
-        if ((e = launch_groups(H, f->dtype, kGateUpBack, choose_rows(R, E, F, ceil_div(D, bk), false, 10.0, H.any), s)))
+        if ((e = launch_groups(H, f->dtype, kGateUpBack, P.cut_h.kind, s)))
             return hip_error(c, e, "experts inner gradient launch");
     }
     // of every group C[m, n] = sum over its rows of a(t, m) b(t, n), beside what accumulate keeps
@@ -587,14 +616,15 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     if (R > 0 && g->dx) {
         GemmArgs X = new_args(R, D, F);
         X.offsets = f->offsets; X.groups = f->experts;
-        X.splits = 1;
+        X.splits = P.cut_x.splits;
+        X.part = (float*)P.part;
         X.nseg = 2;
         X.a[0] = P.dg; X.a[1] = P.du; X.lda = P.ld;
         X.any = P.any.up;
         X.b[0] = f->w_gate; X.ldb = f->ld_gate; X.sb = f->stride_gate;
         X.b[1] = f->w_up; X.ldb1 = f->ld_up; X.sb1 = f->stride_up;
         X.c[0] = g->dx; X.ldc = g->ld_dx;
-        if ((e = launch_groups(X, f->dtype, kRowsCols, choose_rows(R, E, D, 2 * ceil_div(F, bk), false, 2.0, X.any), s)))
+        if ((e = launch_groups(X, f->dtype, kRowsCols, P.cut_x.kind, s)))
             return hip_error(c, e, "experts input gradient launch");
     }
     return ARENA_OK;

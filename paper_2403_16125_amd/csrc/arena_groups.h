@@ -32,6 +32,8 @@ struct GroupTile {
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     static constexpr int kCols = DUAL ? BN / 2 : BN;
     static constexpr bool kLean = BM == 256 && (EPI == kGatedBwd || EPI == kWide);
+    // k in parts: of few rows the tiles do not fill the compute units
+    static constexpr bool kSplit = EPI == kWide || (GROUP == kRowGroups && BM < 256 && (EPI == kPlain || EPI == kGatedBwd));
     static constexpr int kSegs = GROUP == kRowGroups && EPI == kPlain && BTR ? 2 : 1;    // both halves of dx
     // Buffers.  The smallest tiles are those of products with few: there a step is as long as
     // a load's way, unless it starts a step earlier.
@@ -427,7 +429,7 @@ __device__ __forceinline__ void eight_columns(const f32x4& a, const f32x4& b, fl
 }
 
 // tiles: of groups of steps, all of them (parts of k behind each other); of groups of rows,
-// the most there can be.
+// the most there can be of a part.
 template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GemmArgs A, const int tiles)
 {
@@ -449,7 +451,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
-    int n_tiles = tiles;
+    int n_tiles = tiles, part_tiles = 0;
     if constexpr (kRows) {
         __shared__ int rows;
         if (wave == 0) {
@@ -457,7 +459,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             if (lane == 0) rows = total;
         }
         __syncthreads();
-        n_tiles = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
+        part_tiles = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
+        n_tiles = P::kSplit ? part_tiles * A.splits : part_tiles;
     }
     if constexpr (kSteps) {
         for (int g = tid; g < A.groups; g += P::kThreads) {
@@ -480,6 +483,10 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         w->part = 0;
         w->K = A.K;
         if constexpr (kRows) {
+            if (P::kSplit && A.splits > 1) {
+                w->part = quotient(tile, part_tiles);
+                tile -= w->part * part_tiles;
+            }
             int below = 0;
             for (int g0 = 0;; g0 += 64) {
                 const int ends = g0 + lane < A.groups ? table.tiles[g0 + lane] : 0x7fffffff;
@@ -538,7 +545,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         w->sps = (w->K + kBK - 1) / kBK;
         w->steps = w->sps * P::kSegs;
         w->s0 = 0;
-        if (!kRows && A.splits > 1) {
+        if (P::kSplit && A.splits > 1) {
             const int per = quotient(w->steps + A.splits - 1, A.splits);
             w->s0 = min(w->part * per, w->steps);
             w->steps = min(per, w->steps - w->s0);
@@ -720,7 +727,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             Side<T, kSide> side[kAcross];
             LossRow record;
             if constexpr (P::EPI == kLossGrad) record = ((const LossRow*)rows)[m - done.m0];
-            if (P::EPI == kGatedBwd || (P::EPI == kWide && A.beta != 0.0f && A.splits <= 1))
+            if ((P::EPI == kGatedBwd && !(P::kSplit && A.splits > 1)) || (P::EPI == kWide && A.beta != 0.0f && A.splits <= 1))
 #pragma unroll
                 for (int j = 0; j < kAcross; ++j)
                     if (m < done.m_end && nw + j * 32 < n_end) side[j].load(A, done.z, m, nw + j * 32);
@@ -731,7 +738,9 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
                 eight_columns(row[2 * j], row[2 * j + 1], v);
                 if constexpr (P::DUAL) eight_columns(row[2 * (j + kAcross)], row[2 * (j + kAcross) + 1], u);
                 if (m >= done.m_end || n >= n_end) continue;
-                if (!kRows && A.splits > 1) {
+                if (kRows && P::kSplit && A.splits > 1) {
+                    put(A.part + ((int64_t)done.part * A.M + m) * ((A.N + 7) & ~7) + n, v, 8);
+                } else if (!kRows && P::kSplit && A.splits > 1) {
                     const int64_t t = ((int64_t)done.part * A.batch + done.z) * (A.tiles_m * A.tiles_n) +
                                       done.m0 / P::BM * A.tiles_n + done.n0 / P::kCols;
                     put(A.part + t * (P::BM * P::BN) + (m - done.m0) * P::kCols + n - done.n0, v, 8);
@@ -823,25 +832,58 @@ __global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
     }
 }
 
+// The same of groups of rows, whose parts are matrices of all rows: a wave takes 512 columns of
+// a row, if it is a group's.
+template <typename T, int EPI>
+__global__ __launch_bounds__(256) void rows_join_kernel(const GemmArgs A)
+{
+    const int lane = threadIdx.x & 63, stretches = (A.N + 511) / 512, ld = (A.N + 7) & ~7;
+    const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = (int)(i / stretches), n = (int)(i % stretches) * 512 + lane * 8;
+    if (m >= A.M) return;
+    bool some = false;
+    for (int g = lane; g < A.groups; g += 64)
+        some |= m >= group_end(A.offsets, g, A.M) && m < group_end(A.offsets, g + 1, A.M);
+    if (!__any(some) || n >= ld) return;
+    float v[8] = {};
+    for (int s = 0; s < A.splits; ++s) {
+        float w[8];
+        get(A.part + ((int64_t)s * A.M + m) * ld + n, w, 8);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] += w[r];
+    }
+    if constexpr (EPI == kGatedBwd) {
+        Side<T, kGatedBwd> side;
+        side.load(A, 0, m, n);
+        gated_bwd_out<T, kGeluShort>(A, m, n, v, side);
+    } else {
+        put((typename T::E*)A.c[0] + (int64_t)m * A.ldc + n, v, A.N - n);
+    }
+}
+
 template <typename P>
 hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
 {
     A.tiles_m = (A.M + P::BM - 1) / P::BM;
     A.tiles_n = (A.N + P::kCols - 1) / P::kCols;
-    int64_t tiles = P::GROUP == kRowGroups ? group_tiles(A.M, A.groups, P::BM) * A.tiles_n
-                                           : (int64_t)A.tiles_m * A.tiles_n * A.batch * A.splits;
+    const int64_t one = P::GROUP == kRowGroups ? group_tiles(A.M, A.groups, P::BM) * A.tiles_n
+                                               : (int64_t)A.tiles_m * A.tiles_n * A.batch, tiles = one * A.splits;
     if (tiles == 0) return hipSuccess;
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    if (tiles > 0x7fffffff || (A.splits > 1 && !P::kSplit)) return hipErrorInvalidValue;
     // as many blocks as the compute units hold: with many groups the table leaves room for one
     const int table = GroupTable::bytes(P::GROUP, A.groups);
     constexpr int kBuffers = P::kStages * (P::BM + P::BN) * 128 + (P::kRowBytes ? 2 * P::BM * P::kRowBytes : 16) +
                              (P::EPI == kLossStats ? 8 * P::BM * P::WN : 8) + 64;
     const int64_t blocks = P::kBlocks > 1 && kBuffers + table > 163840 / 2 ? 1 : P::kBlocks;
     const int64_t grid = (std::min(tiles, 256 * blocks) + 7) / 8 * 8;
-    groups_kernel<P><<<(unsigned)grid, P::kThreads, table, s>>>(A, (int)tiles);
+    groups_kernel<P><<<(unsigned)grid, P::kThreads, table, s>>>(A, (int)(P::GROUP == kRowGroups ? one : tiles));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits <= 1) return e;
-    if constexpr (P::EPI == kWide) {
+    if constexpr (P::kSplit && P::GROUP == kRowGroups) {
+        const int64_t waves = (int64_t)A.M * ((A.N + 511) / 512);
+        rows_join_kernel<typename P::T, P::EPI><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(A);
+        e = hipGetLastError();
+    } else if constexpr (P::EPI == kWide) {
         const int64_t blocks = ((int64_t)A.batch * A.M * ((A.N + 7) / 8) + 255) / 256;
         groups_join_kernel<P><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, s>>>(A);
         e = hipGetLastError();

@@ -136,7 +136,8 @@ constexpr int kGroupRows[kGroupKinds] = {256, 128, 64}, kGroupCols[kGroupKinds] 
 
 // The products of experts: C of groups of rows (gate and up, down, and the gradients of
 // both operands' inner sides), C of groups of steps (the weights' gradients, wide: beta e
-// and the type of C).  kind: of GroupKind; splits of k with groups of steps only.
+// and the type of C).  kind: of GroupKind; A.splits parts of k, joined in a launch of their own
+// (not of gate and up, nor of groups of rows on the largest tiles).
 hipError_t launch_groups(const GemmArgs& A, int dtype, Product what, int kind, hipStream_t s);
 
 // Few rows, of groups or (offsets null) of one: C = A B^T without LDS tiles, plain, gated or

@@ -287,6 +287,14 @@ def test_experts_larger(ops, counts, D, F):
     check_experts(ops, experts_inputs(counts, D, F, BF16), "silu", BF16)
 
 
+@pytest.mark.parametrize("typ,act", [(BF16, "silu"), (F16, "gelu")])
+@pytest.mark.parametrize("counts,first,past,D,F", [([1], 0, 0, 2048, 1024), ([20, 0, 3], 2, 1, 1500, 2100), ([0, 17, 40, 1], 0, 70, 1001, 2051),
+                                                   ([70, 1, 64], 5, 3, 3000, 520), ([2] * 40, 1, 1, 520, 3000)])
+def test_experts_few_rows_of_long_products(ops, counts, first, past, D, F, typ, act):
+    """Tiles that do not fill the card: the products are split along k, rows of no group stay out."""
+    check_experts(ops, experts_inputs(counts, D, F, typ, first, past), act, typ)
+
+
 @pytest.mark.parametrize("rows", [6, 300])
 @pytest.mark.parametrize("pad,offset", [(0, 1), (8, 0), (3, 0), (24, 8)])
 def test_experts_strides_and_alignment(ops, rows, pad, offset):
