@@ -292,11 +292,18 @@ GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pa
                          1.5, false, any);
 }
 
-// Whether a forward pass takes the kernel for few rows, which streams the weights of one
-// group after the other past 16 rows.  With more the tiles read them as fast, and those
-// of a group only once (64 experts of 2048 x 1408: 16 rows 48 us against 58, 32 rows 86
-// against 77; 8 of 4096 x 10944: 292 against 390, 64 rows 471 against 421).
-bool few_rows(const arena_experts_desc* d) { return d->rows <= 16; }
+// Whether a forward pass takes the kernel for few rows, which streams the weights and has no
+// tiles to fill, but reads those of a group again for every 16 rows.  Up to 16 rows it is
+// faster at all sizes (one row of 8 experts 4096 x 10944: 64 us, on tiles 73; 16 rows of 64
+// experts 2048 x 1408: 60 and 65).  Past that where an expert has about 12 rows at most and its
+// matrices stay in the caches (32 rows of 4 experts 4096 x 512: 23 and 39; 64 rows of 64 experts
+// 2048 x 1408: 148 and 161), not with larger ones (32 rows of 8 experts 4096 x 10944: 387 and
+// 371) or more rows (32 rows of 2 experts 2048 x 5461: 69 and 44).
+bool few_rows(const arena_experts_desc* d)
+{
+    return d->rows <= 16 || (d->rows <= 64 && d->rows <= 12 * (int64_t)d->experts &&
+                             (int64_t)d->model * d->inner <= 1 << 22);
+}
 
 // Which matrices the loads that write to the LDS cannot take: their products load to
 // registers first.
