@@ -269,7 +269,7 @@ GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, boo
         const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
         const double tm = std::max((double)some, (double)rows / kGroupRows[kind] + 0.5 * some);
         if (group_tiles(rows, groups, kGroupRows[kind]) * tn > 0x7fffffff) continue;
-        for (int s = 1; s <= 16 && (s == 1 || (!dual && kind != kGroup256 && s * 4 <= steps)); ++s) {
+        for (int s = 1; s <= 64 && (s == 1 || (!dual && kind != kGroup256 && s * 4 <= steps)); ++s) {
             if (s > 1 && tm * tn * s > 2.0 * kUnits) break;      // more blocks than there is room for
             const int64_t part = s > 1 ? 4 * s * rows * pad8(N) : 0;
             const double t = group_time(tm * tn * s, std::ceil((double)steps / s), kind, 1, s > 1 ? 4.0 : bytes, 1.0, false,

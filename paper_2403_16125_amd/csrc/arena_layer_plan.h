@@ -313,7 +313,7 @@ inline GroupCut choose_groups(int64_t M, int64_t N, int64_t steps, int64_t batch
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * batch;
-        for (int s = 1; s <= 16 && (s == 1 || (split && s * 4 <= steps)); ++s) {
+        for (int s = 1; s <= 64 && (s == 1 || (split && s * 4 <= steps)); ++s) {
             if (tiles * s > 0x7fffffff) continue;
             const double t = group_time((double)tiles, (double)steps, kind, s, bytes, uneven, exact, any);
             if (t < least) {
