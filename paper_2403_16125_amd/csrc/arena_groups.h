@@ -11,6 +11,17 @@
 //
 // Waves whose rows all lie past the group's end only load for the others: they share a
 // SIMD with waves that do not, so such a step takes little more than half the time.
+//
+// Large products are bound by the matrix cores and the clock under load, and by last rounds
+// that do not fill the card.  In bfloat16, 16384 rows of 8 experts 4096 x 10944: gate and up
+// 2.73 ms (1080 TFLOP/s), down 1.37 (1080), inner gradients 1.63 (900), weights' gradients 1.33
+// and 2.68 (1100), dx 2.64 (1110), matrix cores busy in 48 to 66 % of the cycles.  A loss of
+// 8192 tokens, 131072 x 4096: logits 6.65 ms (1320), a piece of 16384 entries 0.84 ms for their
+// gradient, 0.82 for dx, 0.80 for dw (1310 to 1380).  With 256 rows an expert (64 of 2048 x 1408)
+// the weights are read or written once for every two to four tiles and groups waste half a tile:
+// 320 us, 155, 212, 240 + 416 and 296 (430 to 640), matrix cores busy in 25 to 34 %.  Small ones are
+// bound by latency: about 8 us for the launch, the table, the first loads and the epilogue, and
+// 0.6 to 0.8 for a step.
 #pragma once
 
 #include <algorithm>
@@ -833,7 +844,7 @@ __global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
 }
 
 // The same of groups of rows, whose parts are matrices of all rows: a wave takes 512 columns of
-// a row, if it is a group's.
+// a row, if it is a group's.  Bound by its launch: 5 us for 50 rows of 1024 columns in 14 parts.
 template <typename T, int EPI>
 __global__ __launch_bounds__(256) void rows_join_kernel(const GemmArgs A)
 {
