@@ -454,3 +454,50 @@ def test_layer_on_another_stream(ops):
     y = ops.combine(ys, plan, weight, stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(y, want[0])
+
+
+def test_many_experts_on_the_largest_tiles(ops):
+    """The largest table beside the largest buffers."""
+    check_experts(ops, experts_inputs([300] * 1000 + [0] * 23 + [1], 256, 256, BF16), "silu", BF16)
+
+
+def test_split_products_captured_and_replayed(ops):
+    """Few rows of long products, whose parts lie in workspaces of the graph; the replays' tokens take other experts."""
+    static = layer_inputs(30, 2048, 1100, 4)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        layer_of_experts(ops, *static[:5], 2, static[5])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = layer_of_experts(ops, *static[:5], 2, static[5])
+    for seed in (21, 22, 23):
+        for s, n in zip(static, layer_inputs(30, 2048, 1100, 4, seed)):
+            s.copy_(n)
+        want = layer_of_experts(ops, *static[:5], 2, static[5])
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(out, want, layer_of_experts(ops, *static[:5], 2, static[5])):
+            assert torch.equal(a, b) and torch.equal(b, c)
+
+
+def test_experts_do_not_see_each_other(ops):
+    """NaN and infinities in one expert's rows, and in the weights of one without rows, stay there."""
+    for counts in ([5, 7, 0, 3], [130, 70, 0, 300]):
+        x, offsets, wg, wu, wd, dy = experts_inputs(counts, 136, 200, BF16)
+        first = slice(0, counts[0])
+
+        def run():
+            ys, saved = ops.experts_forward(x, offsets, wg, wu, wd, save=True)
+            return [ys, *ops.experts_backward(dy, x, offsets, wg, wu, wd, saved)]
+
+        want = run()
+        x[first] = math.nan
+        dy[first] = math.inf
+        for w in (wg, wu, wd):
+            w[2] = math.nan
+        got = run()
+        for a, b in zip(got[:2], want[:2]):
+            assert torch.equal(a[counts[0]:], b[counts[0]:])
+        for a, b in zip(got[2:], want[2:]):
+            assert torch.equal(a[1:], b[1:]) and not a[2].any()
