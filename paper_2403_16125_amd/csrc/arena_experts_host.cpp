@@ -260,10 +260,11 @@ bool even(const void* p, int64_t ld, int64_t cols, int64_t stride, int experts)
 // The kind of tile and the parts of k for a product of groups of rows: how they fall is not
 // known here, so each group that can have rows is taken to waste half a tile.  The parts are
 // matrices of all rows.
-GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes, bool any)
+GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, bool dual, double bytes, bool any,
+                     bool gated = false)
 {
     using namespace arena::mm;
-    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0};
+    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0, 0};
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t some = std::min(groups, rows), tn = ceil_div(N, dual ? kGroupCols[kind] / 2 : kGroupCols[kind]);
@@ -276,7 +277,16 @@ GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, boo
                                         any) + (s > 1 ? kJoin + part * 1e-6 / kJoinRate : 0.0);
             if (t < least) {
                 least = t;
-                best = {kind, s, part};
+                best = {kind, s, part, 0};
+            }
+        }
+        if (!dual && !gated && !(any && kind == kGroup256)) {
+            int tail;
+            int64_t part;
+            const double t = tail_time(tm * tn, (double)steps, kind, bytes, &tail, &part);
+            if (t < least) {
+                least = t;
+                best = {kind, 1, part, tail};
             }
         }
     }
@@ -323,7 +333,7 @@ struct ExpertsPlan {
     Uneven any;
     GroupCut up, down;
     void* part;
-    ExpertsPlan(const arena_experts_desc* d, void* base) : w(base), any(d), up{0, 1, 0}, down{0, 1, 0}, part(nullptr)
+    ExpertsPlan(const arena_experts_desc* d, void* base) : w(base), any(d), up{0, 1, 0, 0}, down{0, 1, 0, 0}, part(nullptr)
     {
         if (d->rows == 0 || few_rows(d)) return;
         using arena::mm::kBK;
@@ -352,10 +362,10 @@ struct ExpertsBackPlan {
         const double bytes = bytes_of(g->grad_dtype) * (g->accumulate ? 2.0 : 1.0);
         cut_up = choose_steps(d->inner, d->model, d->rows, d->experts, pair ? 2 : 1, bytes, any.x);
         cut_down = choose_steps(d->model, d->inner, d->rows, d->experts, 1, bytes, dy_any);
-        cut_h = cut_x = {0, 1, 0};
+        cut_h = cut_x = {0, 1, 0, 0};
         if (d->rows > 0 && (g->dx || g->dw_gate || g->dw_up))
             cut_h = choose_rows(d->rows, d->experts, d->inner, ceil_div(d->model, arena::mm::kBK), false, 10.0,
-                                dy_any || any.down);
+                                dy_any || any.down, true);
         if (d->rows > 0 && g->dx)
             cut_x = choose_rows(d->rows, d->experts, d->model, 2 * ceil_div(d->inner, arena::mm::kBK), false, 2.0, any.up);
         part = w.take(std::max({g->dw_gate || g->dw_up ? cut_up.part : 0, g->dw_down ? cut_down.part : 0, cut_h.part,
@@ -531,6 +541,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     GemmArgs B = new_args(R, d->model, d->inner);
     B.offsets = d->offsets; B.groups = d->experts;
     B.splits = P.down.splits;
+    B.tail = P.down.tail;
     B.part = (float*)P.part;
     B.any = any.down;
     B.a[0] = d->h; B.lda = d->ld_inner;
@@ -624,6 +635,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
         GemmArgs X = new_args(R, D, F);
         X.offsets = f->offsets; X.groups = f->experts;
         X.splits = P.cut_x.splits;
+        X.tail = P.cut_x.tail;
         X.part = (float*)P.part;
         X.nseg = 2;
         X.a[0] = P.dg; X.a[1] = P.du; X.lda = P.ld;

@@ -14,8 +14,8 @@
 //
 // Large products are bound by the matrix cores and the clock under load, and by last rounds
 // that do not fill the card.  In bfloat16, 16384 rows of 8 experts 4096 x 10944: gate and up
-// 2.73 ms (1080 TFLOP/s), down 1.37 (1080), inner gradients 1.63 (900), weights' gradients 1.33
-// and 2.68 (1100), dx 2.64 (1110), matrix cores busy in 48 to 66 % of the cycles.  A loss of
+// 2.73 ms (1080 TFLOP/s), down 1.26 (1170), inner gradients 1.63 (900), weights' gradients 1.33
+// and 2.68 (1100), dx 2.36 (1240), matrix cores busy in 48 to 66 % of the cycles.  A loss of
 // 8192 tokens, 131072 x 4096: logits 6.65 ms (1320), a piece of 16384 entries 0.84 ms for their
 // gradient, 0.82 for dx, 0.80 for dw (1310 to 1380).  With 256 rows an expert (64 of 2048 x 1408)
 // the weights are read or written once for every two to four tiles and groups waste half a tile:
@@ -45,6 +45,7 @@ struct GroupTile {
     static constexpr bool kLean = BM == 256 && (EPI == kGatedBwd || EPI == kWide);
     // k in parts: of few rows the tiles do not fill the compute units
     static constexpr bool kSplit = EPI == kWide || (GROUP == kRowGroups && BM < 256 && (EPI == kPlain || EPI == kGatedBwd));
+    static constexpr bool kTail = GROUP == kRowGroups && EPI == kPlain;      // the last round's tiles too
     static constexpr int kSegs = GROUP == kRowGroups && EPI == kPlain && BTR ? 2 : 1;    // both halves of dx
     // Buffers.  The smallest tiles are those of products with few: there a step is as long as
     // a load's way, unless it starts a step earlier.
@@ -249,10 +250,64 @@ struct OneFragment {
 // A tile: its place, its steps and its operands' first addresses.
 struct Work {
     int m0, n0, m_end, z;       // z: group, or with pairs twice that and which of the two
-    int part;                   // of a split k
+    int part, parts;            // of a split k
+    int slot;                   // of the last round's tiles
     int steps, sps, K;          // steps of all segments, of one, and k of a segment
     int s0;                     // first step of the part
 };
+
+// The tiles past the last whole round of `blocks` resident ones, and in how many parts of k
+// they are shared out among all blocks (16384 rows of 8 experts 4096 x 10944, 4.25 rounds: down
+// 1365 us whole, 1245 with the last 64 tiles in four parts; dx 2642 and 2341).
+struct Tail {
+    int tiles, parts;
+    __device__ __forceinline__ Tail(int all, int blocks, int most)
+    {
+        tiles = most > 1 ? all % blocks : 0;
+        parts = tiles > 0 ? min(most, blocks / tiles) : 1;
+        if (parts < 2) tiles = 0, parts = 1;
+    }
+};
+
+// Group and place of a tile, counted without parts.
+template <typename P>
+__device__ __forceinline__ void locate(const GemmArgs& A, const GroupTable& table, int lane, int tile, Work* w)
+{
+    constexpr bool kRows = P::GROUP == kRowGroups;
+    int band_rows, in;
+    if constexpr (kRows) {
+        int below = 0;
+        for (int g0 = 0;; g0 += 64) {
+            const int ends = g0 + lane < A.groups ? table.tiles[g0 + lane] : 0x7fffffff;
+            const int first = g0 + lane < A.groups ? table.first[g0 + lane] : 0;
+            const uint64_t past = __ballot(tile < (int64_t)ends * A.tiles_n);
+            if (past) {
+                const int l = __ffsll((unsigned long long)past) - 1;
+                if (l > 0) below = __builtin_amdgcn_readlane(ends, l - 1);
+                w->z = g0 + l;
+                w->m0 = __builtin_amdgcn_readlane(first, l);
+                band_rows = __builtin_amdgcn_readlane(ends, l) - below;
+                break;
+            }
+            below = __builtin_amdgcn_readlane(ends, 63);
+        }
+        in = tile - below * A.tiles_n;
+    } else {
+        const int each = A.tiles_m * A.tiles_n;
+        w->z = quotient(tile, each);
+        w->m0 = 0;
+        band_rows = A.tiles_m;
+        in = tile - w->z * each;
+    }
+    // bands of 8 tile rows
+    const int band = 8 * A.tiles_n, b = quotient(in, band), at = in - b * band;
+    const int high = min(8, band_rows - b * 8), tn = quotient(at, high);
+    const int tm = b * 8 + at - tn * high;
+    w->n0 = tn * P::kCols;
+    w->m_end = A.M;
+    if constexpr (kRows) w->m_end = __builtin_amdgcn_readfirstlane(table.end[w->z]);
+    w->m0 += tm * P::BM;
+}
 
 // The loader of arena_gemm.h, with its lanes' part apart.
 template <typename P, int R, bool TR, bool DUAL>
@@ -439,8 +494,7 @@ __device__ __forceinline__ void eight_columns(const f32x4& a, const f32x4& b, fl
     }
 }
 
-// tiles: of groups of steps, all of them (parts of k behind each other); of groups of rows,
-// the most there can be of a part.
+// tiles: of a part, of groups of rows the most that there can be.
 template <typename P>
 __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GemmArgs A, const int tiles)
 {
@@ -462,7 +516,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / P::WN, wn = wave % P::WN;
-    int n_tiles = tiles, part_tiles = 0;
+    int part_tiles = tiles;
     if constexpr (kRows) {
         __shared__ int rows;
         if (wave == 0) {
@@ -471,7 +525,6 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         }
         __syncthreads();
         part_tiles = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
-        n_tiles = P::kSplit ? part_tiles * A.splits : part_tiles;
     }
     if constexpr (kSteps) {
         for (int g = tid; g < A.groups; g += P::kThreads) {
@@ -483,6 +536,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         __syncthreads();
     }
 
+    const Tail tail(part_tiles, (int)gridDim.x, P::kTail ? A.tail : 0);
+    const int n_tiles = (P::kSplit ? part_tiles * A.splits : part_tiles) + tail.tiles * (tail.parts - 1);
     const int xcd = blockIdx.x & 7;
     int q = blockIdx.x >> 3;
     // The tile that comes next; false if there is none.
@@ -490,49 +545,21 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         int tile = tile_of_xcd<P::kRun>(xcd, q, n_tiles);
         q += gridDim.x >> 3;
         if (tile < 0) return false;
-        int band_rows, in;
         w->part = 0;
+        w->parts = 1;
         w->K = A.K;
-        if constexpr (kRows) {
-            if (P::kSplit && A.splits > 1) {
-                w->part = quotient(tile, part_tiles);
-                tile -= w->part * part_tiles;
-            }
-            int below = 0;
-            for (int g0 = 0;; g0 += 64) {
-                const int ends = g0 + lane < A.groups ? table.tiles[g0 + lane] : 0x7fffffff;
-                const int first = g0 + lane < A.groups ? table.first[g0 + lane] : 0;
-                const uint64_t past = __ballot(tile < (int64_t)ends * A.tiles_n);
-                if (past) {
-                    const int l = __ffsll((unsigned long long)past) - 1;
-                    if (l > 0) below = __builtin_amdgcn_readlane(ends, l - 1);
-                    w->z = g0 + l;
-                    w->m0 = __builtin_amdgcn_readlane(first, l);
-                    band_rows = __builtin_amdgcn_readlane(ends, l) - below;
-                    break;
-                }
-                below = __builtin_amdgcn_readlane(ends, 63);
-            }
-            in = tile - below * A.tiles_n;
-        } else {
-            const int each = A.tiles_m * A.tiles_n, all = each * A.batch;
-            if (A.splits > 1) {
-                w->part = quotient(tile, all);
-                tile -= w->part * all;
-            }
-            w->z = quotient(tile, each);
-            w->m0 = 0;
-            band_rows = A.tiles_m;
-            in = tile - w->z * each;
+        if (P::kSplit && A.splits > 1) {
+            w->parts = A.splits;
+            w->part = quotient(tile, part_tiles);
+            tile -= w->part * part_tiles;
+        } else if (P::kTail && tile >= part_tiles - tail.tiles && tail.parts > 1) {
+            const int in = tile - (part_tiles - tail.tiles);
+            w->parts = tail.parts;
+            w->part = quotient(in, tail.tiles);
+            w->slot = in - w->part * tail.tiles;
+            tile = part_tiles - tail.tiles + w->slot;
         }
-        // bands of 8 tile rows
-        const int band = 8 * A.tiles_n, b = quotient(in, band), at = in - b * band;
-        const int high = min(8, band_rows - b * 8), tn = quotient(at, high);
-        const int tm = b * 8 + at - tn * high;
-        w->n0 = tn * P::kCols;
-        w->m_end = A.M;
-        if constexpr (kRows) w->m_end = __builtin_amdgcn_readfirstlane(table.end[w->z]);
-        w->m0 += tm * P::BM;
+        locate<P>(A, table, lane, tile, w);
         return true;
     };
 
@@ -556,8 +583,8 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
         w->sps = (w->K + kBK - 1) / kBK;
         w->steps = w->sps * P::kSegs;
         w->s0 = 0;
-        if (P::kSplit && A.splits > 1) {
-            const int per = quotient(w->steps + A.splits - 1, A.splits);
+        if ((P::kSplit || P::kTail) && w->parts > 1) {
+            const int per = quotient(w->steps + w->parts - 1, w->parts);
             w->s0 = min(w->part * per, w->steps);
             w->steps = min(per, w->steps - w->s0);
         }
@@ -738,7 +765,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
             Side<T, kSide> side[kAcross];
             LossRow record;
             if constexpr (P::EPI == kLossGrad) record = ((const LossRow*)rows)[m - done.m0];
-            if ((P::EPI == kGatedBwd && !(P::kSplit && A.splits > 1)) || (P::EPI == kWide && A.beta != 0.0f && A.splits <= 1))
+            if ((P::EPI == kGatedBwd || (P::EPI == kWide && A.beta != 0.0f)) && !(P::kSplit && A.splits > 1))
 #pragma unroll
                 for (int j = 0; j < kAcross; ++j)
                     if (m < done.m_end && nw + j * 32 < n_end) side[j].load(A, done.z, m, nw + j * 32);
@@ -749,7 +776,10 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
                 eight_columns(row[2 * j], row[2 * j + 1], v);
                 if constexpr (P::DUAL) eight_columns(row[2 * (j + kAcross)], row[2 * (j + kAcross) + 1], u);
                 if (m >= done.m_end || n >= n_end) continue;
-                if (kRows && P::kSplit && A.splits > 1) {
+                if (P::kTail && A.tail > 1 && done.parts > 1) {
+                    put(A.part + ((int64_t)done.part * tail.tiles + done.slot) * (P::BM * P::BN) +
+                            (m - done.m0) * P::kCols + n - done.n0, v, 8);
+                } else if (kRows && P::kSplit && A.splits > 1) {
                     put(A.part + ((int64_t)done.part * A.M + m) * ((A.N + 7) & ~7) + n, v, 8);
                 } else if (!kRows && P::kSplit && A.splits > 1) {
                     const int64_t t = ((int64_t)done.part * A.batch + done.z) * (A.tiles_m * A.tiles_n) +
@@ -872,6 +902,41 @@ __global__ __launch_bounds__(256) void rows_join_kernel(const GemmArgs A)
     }
 }
 
+// Joins the parts of the last round's tiles: eight blocks a tile, the same number of groups' tiles
+// and of parts as the product found (`tiles` and `blocks` of its launch).  9 to 15 us.
+template <typename P>
+__global__ __launch_bounds__(256) void tail_join_kernel(const GemmArgs A, const int tiles, const int blocks)
+{
+    extern __shared__ int table_data[];
+    const GroupTable table(table_data, A.groups);
+    const int lane = threadIdx.x & 63;
+    __shared__ int rows;
+    if (threadIdx.x < 64) {
+        const int total = fill_table<P::BM>(A, &table, lane, quotient(tiles, A.tiles_n));
+        if (lane == 0) rows = total;
+    }
+    __syncthreads();
+    const int all = __builtin_amdgcn_readfirstlane(rows) * A.tiles_n;
+    const Tail tail(all, blocks, A.tail);
+    const int slot = blockIdx.x >> 3;
+    if (slot >= tail.tiles) return;
+    Work w;
+    locate<P>(A, table, lane, all - tail.tiles + slot, &w);
+    constexpr int kChunks = P::BM * P::kCols / 8;
+    for (int i = (blockIdx.x & 7) * 256 + threadIdx.x; i < kChunks; i += 2048) {
+        const int r = i / (P::kCols / 8), c = i % (P::kCols / 8) * 8, m = w.m0 + r, n = w.n0 + c;
+        if (m >= w.m_end || n >= A.N) continue;
+        float v[8] = {};
+        for (int s = 0; s < tail.parts; ++s) {
+            float x[8];
+            get(A.part + ((int64_t)s * tail.tiles + slot) * (P::BM * P::BN) + r * P::kCols + c, x, 8);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += x[k];
+        }
+        put((typename P::T::E*)A.c[0] + (int64_t)m * A.ldc + n, v, A.N - n);
+    }
+}
+
 template <typename P>
 hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
 {
@@ -887,8 +952,15 @@ hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
                              (P::EPI == kLossStats ? 8 * P::BM * P::WN : 8) + 64;
     const int64_t blocks = P::kBlocks > 1 && kBuffers + table > 163840 / 2 ? 1 : P::kBlocks;
     const int64_t grid = (std::min(tiles, 256 * blocks) + 7) / 8 * 8;
-    groups_kernel<P><<<(unsigned)grid, P::kThreads, table, s>>>(A, (int)(P::GROUP == kRowGroups ? one : tiles));
+    if (!P::kTail || A.splits > 1 || one < grid) A.tail = 0;
+    groups_kernel<P><<<(unsigned)grid, P::kThreads, table, s>>>(A, (int)one);
     hipError_t e = hipGetLastError();
+    if constexpr (P::kTail)
+        if (e == hipSuccess && A.tail > 1) {
+            // not more than half of the blocks' tiles are shared out
+            tail_join_kernel<P><<<(unsigned)(grid / 2 * 8), 256, table, s>>>(A, (int)one, (int)grid);
+            return hipGetLastError();
+        }
     if (e != hipSuccess || A.splits <= 1) return e;
     if constexpr (P::kSplit && P::GROUP == kRowGroups) {
         const int64_t waves = (int64_t)A.M * ((A.N + 511) / 512);

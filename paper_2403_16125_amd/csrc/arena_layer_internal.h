@@ -76,6 +76,7 @@ struct GemmArgs {
     // (se).  With pairs = 1 every group's two products are neighbouring batch indices
     const int32_t* offsets;   // [groups + 1], held inside 0 .. rows
     int32_t groups;
+    int32_t tail;             // most parts of k for the tiles past the last whole round, in part too; 0: whole
     int32_t any;              // an operand's rows start on any value (tiles of 128 columns)
     // wide: C = alpha factor[0] product + beta e, e in 32 bits or in C's type
     const float* factor;      // nullable

@@ -303,13 +303,29 @@ inline double group_time(double tiles, double steps, int kind, int64_t splits, d
 struct GroupCut {
     int kind, splits;
     int64_t part;             // bytes
+    int tail;                 // most parts of the last round's tiles
 };
+
+constexpr double kTailJoin = 15.0;          // its launch and reads
+
+// Whether the tiles past the last whole round are worth parts of their own: they cost a join.
+// Sets *tail and the bytes of the parts (not more tiles than there are blocks); returns the time.
+inline double tail_time(double tiles, double steps, int kind, double bytes, int* tail, int64_t* part)
+{
+    const GroupCost& k = kGroupCost[kind];
+    const double values = (double)mm::kGroupRows[kind] * mm::kGroupCols[kind], round = kUnits * k.slots;
+    const double full = steps * k.full + k.start + values * bytes / kEpilogueRate * k.slots;
+    *tail = (int)std::min(8.0, steps / 8);
+    *part = (int64_t)(4 * round * values);
+    if (*tail < 2 || tiles < round) return INFINITY;
+    return kLaunch + (tiles / round + 0.25) * full + kTailJoin;
+}
 
 inline GroupCut choose_groups(int64_t M, int64_t N, int64_t steps, int64_t batch, double bytes, bool split, double uneven,
                               bool exact, bool any)
 {
     using namespace mm;
-    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0};
+    GroupCut best = {any ? kGroup128 : kGroup256, 1, 0, 0};
     double least = INFINITY;
     for (int kind = 0; kind < kGroupKinds; ++kind) {
         const int64_t tiles = ceil_div(M, kGroupRows[kind]) * ceil_div(N, kGroupCols[kind]) * batch;
@@ -318,7 +334,7 @@ inline GroupCut choose_groups(int64_t M, int64_t N, int64_t steps, int64_t batch
             const double t = group_time((double)tiles, (double)steps, kind, s, bytes, uneven, exact, any);
             if (t < least) {
                 least = t;
-                best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0};
+                best = {kind, s, s > 1 ? 4 * s * tiles * kGroupRows[kind] * kGroupCols[kind] : 0, 0};
             }
         }
     }

@@ -461,6 +461,12 @@ def test_many_experts_on_the_largest_tiles(ops):
     check_experts(ops, experts_inputs([300] * 1000 + [0] * 23 + [1], 256, 256, BF16), "silu", BF16)
 
 
+@pytest.mark.parametrize("counts,first,past,D,F", [([6000, 0, 5200, 37], 0, 0, 2048, 4096), ([3000, 1, 2000], 3, 700, 2047, 6001)])
+def test_experts_last_round_in_parts(ops, counts, first, past, D, F):
+    """One round of tiles and a little more: the rest is split along k."""
+    check_experts(ops, experts_inputs(counts, D, F, BF16, first, past), "silu", BF16)
+
+
 def test_split_products_captured_and_replayed(ops):
     """Few rows of long products, whose parts lie in workspaces of the graph; the replays' tokens take other experts."""
     static = layer_inputs(30, 2048, 1100, 4)
