@@ -208,6 +208,15 @@ class ExpertOps:
         if not least <= value < 1 << (bits - 1):
             raise ValueError(f"{name} is {value}")
 
+    def _choices(self, name, t):
+        """Tokens, and choices of a token, of a tensor with a value a choice."""
+        if t.dim() < 1:
+            raise ValueError(f"{name} needs an axis of choices")
+        tokens, k = self._rows(t)
+        if k >> 31:
+            raise ValueError(f"{name} has {k} choices a token")
+        return tokens, k
+
     def _whole(self, name, t, shape):
         """Address and type of a contiguous tensor of int32 or int64."""
         wide = t.dtype is self.torch.int64
@@ -269,7 +278,7 @@ class ExpertOps:
         return self._run(stream, (dweight, logits, index), self._route_backward, dweight, logits, index, normalise, scale)
 
     def _route_backward(self, handle, dweight, logits, index, normalise, scale):
-        k = index.shape[-1]
+        k = self._choices("index", index)[1]
         d = self._route_desc(logits, k, normalise, scale)
         d.index = self._int32("index", index, logits.shape[:-1] + (k,))
         p, ld = self._matrix("dweight", dweight, (d.tokens, k), self.torch.float32)
@@ -287,10 +296,8 @@ class ExpertOps:
 
     def _sort_by_expert(self, handle, index, experts):
         self._within("experts", experts, 32)
+        tokens, k = self._choices("index", index)
         p, kind = self._whole("index", index, index.shape)
-        if index.dim() < 1:
-            raise ValueError("index needs an axis of choices")
-        tokens, k = self._rows(index)
         plan = ExpertPlan(self._empty((experts + 1,), self.torch.int32), self._empty(index.shape, self.torch.int32))
         d = SortDesc(index_dtype=kind, experts=experts, tokens=tokens, k=k, index=p, offsets=plan.offsets.data_ptr(),
                      row=plan.row.data_ptr())
@@ -301,7 +308,7 @@ class ExpertOps:
 
     def _move_desc(self, dtype, model, plan, rows, weight=None):
         row = plan.row
-        tokens, k = self._rows(row)
+        tokens, k = self._choices("plan.row", row)
         d = MoveDesc(dtype=self._code(dtype), model=model, tokens=tokens, rows=rows, k=k,
                      row=self._int32("plan.row", row, row.shape))
         if weight is not None:
@@ -360,6 +367,8 @@ class ExpertOps:
         if w_gate.dim() != 3:
             raise ValueError("the weights have three axes: experts, rows and columns")
         experts, inner = w_gate.shape[:2]
+        if experts >> 31:
+            raise ValueError(f"w_gate has {experts} experts")
         d = ExpertsDesc(dtype=self._type(xs), activation=self._activation(activation), rows=rows, model=model, inner=inner,
                         experts=experts, offsets=self._int32("offsets", offsets, (experts + 1,)))
         d.x, d.ld_x = self._matrix("xs", xs, (rows, model), xs.dtype)
