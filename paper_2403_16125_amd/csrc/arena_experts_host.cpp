@@ -17,7 +17,7 @@ using arena::ctx_fail;
 using arena::MoveArgs;
 using arena::RouteArgs;
 using arena::SortArgs;
-using arena::mm::GemmArgs;
+using arena::mm::GroupArgs;
 
 static_assert(ARENA_MAX_EXPERTS == arena::kRouteMaxExperts, "experts of the header and the kernels");
 static_assert(ARENA_ROUTE_MAX_CHOICES == arena::kRouteMaxChoices, "choices of the header and the kernels");
@@ -524,7 +524,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     const int64_t R = d->rows;
     const Uneven& any = P.any;
     const bool few = few_rows(d);
-    GemmArgs A = new_args(R, d->inner, d->model);
+    GroupArgs A = new_args<GroupArgs>(R, d->inner, d->model);
     A.offsets = d->offsets; A.groups = d->experts;
     A.splits = 1;
     A.any = any.x || any.up;
@@ -538,7 +538,7 @@ arena_status arena_experts_forward(arena_ctx* c, const arena_experts_desc* d, vo
     hipError_t e = few ? arena::mm::launch_skinny_groups(A, d->dtype, arena::mm::kGateUp, s)
                        : arena::mm::launch_groups(A, d->dtype, arena::mm::kGateUp, P.up.kind, s);
     if (e) return hip_error(c, e, "experts gate and up launch");
-    GemmArgs B = new_args(R, d->model, d->inner);
+    GroupArgs B = new_args<GroupArgs>(R, d->model, d->inner);
     B.offsets = d->offsets; B.groups = d->experts;
     B.splits = P.down.splits;
     B.tail = P.down.tail;
@@ -581,7 +581,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     using namespace arena::mm;
     hipError_t e;
     if (R > 0 && (g->dx || g->dw_gate || g->dw_up)) {
-        GemmArgs H = new_args(R, F, D);
+        GroupArgs H = new_args<GroupArgs>(R, F, D);
         H.offsets = f->offsets; H.groups = f->experts;
         H.splits = P.cut_h.splits;
         H.part = (float*)P.part;
@@ -598,7 +598,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
     // of every group C[m, n] = sum over its rows of a(t, m) b(t, n), beside what accumulate keeps
     auto weight = [&](const void* a0, const void* a1, int64_t lda, const void* b, int64_t ldb, int64_t M, int64_t N,
                       void* c0, void* c1, int64_t ldc, int64_t sc, const GroupCut& cut, bool any) {
-        GemmArgs A = new_args(M, N, R);
+        GroupArgs A = new_args<GroupArgs>(M, N, R);
         A.any = any;
         A.offsets = f->offsets; A.groups = f->experts;
         A.pairs = c1 != nullptr;
@@ -632,7 +632,7 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
             return hip_error(c, e, "experts up gradient launch");
     }
     if (R > 0 && g->dx) {
-        GemmArgs X = new_args(R, D, F);
+        GroupArgs X = new_args<GroupArgs>(R, D, F);
         X.offsets = f->offsets; X.groups = f->experts;
         X.splits = P.cut_x.splits;
         X.tail = P.cut_x.tail;

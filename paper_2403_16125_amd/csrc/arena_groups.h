@@ -91,7 +91,7 @@ __device__ __forceinline__ int group_end(const int32_t* offsets, int g, int rows
 
 // Rows of group g and the tile rows that they make.
 template <int BM>
-__device__ __forceinline__ int tile_rows(const GemmArgs& A, int g, int* lo, int* hi)
+__device__ __forceinline__ int tile_rows(const GroupArgs& A, int g, int* lo, int* hi)
 {
     *lo = *hi = 0;
     if (g < A.groups) {
@@ -104,7 +104,7 @@ __device__ __forceinline__ int tile_rows(const GemmArgs& A, int g, int* lo, int*
 // Fills the table (one wave) and returns how many tile rows there are, at most `most`:
 // groups that overlap could have more than a launch counts.
 template <int BM>
-__device__ __forceinline__ int fill_table(const GemmArgs& A, const GroupTable* table, int lane, int most)
+__device__ __forceinline__ int fill_table(const GroupArgs& A, const GroupTable* table, int lane, int most)
 {
     int total = 0;
     for (int g0 = 0; g0 < A.groups; g0 += 64) {
@@ -130,7 +130,7 @@ __device__ __forceinline__ int fill_table(const GemmArgs& A, const GroupTable* t
 template <typename T>
 struct Side<T, kWide> {
     u32x4 raw[2];
-    __device__ __forceinline__ void load(const GemmArgs& A, int z, int m, int n)
+    __device__ __forceinline__ void load(const GroupArgs& A, int z, int m, int n)
     {
         if (A.beta == 0.0f) return;
         const char* p = (const char*)A.e[A.pairs ? z & 1 : 0];
@@ -163,7 +163,7 @@ struct Side<T, kWide> {
 };
 
 template <typename T>
-__device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n, float (&v)[8],
+__device__ __forceinline__ void plain_out(const GroupArgs& A, int z, int m, int n, float (&v)[8],
                                           const Side<T, kWide>& side)
 {
     typedef typename T::E E;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void plain_out(const GemmArgs& A, int z, int m, int n
 // factor (exp(l - lse) - [column is the target]), zero for tokens left out of the loss,
 // whatever their logits: rounded to 16 bits as the next two products' operand.
 template <typename T>
-__device__ __forceinline__ void loss_grad_out(const GemmArgs& A, int m, int n, const float (&v)[8], const LossRow& row)
+__device__ __forceinline__ void loss_grad_out(const GroupArgs& A, int m, int n, const float (&v)[8], const LossRow& row)
 {
     typedef typename T::E E;
     const float lse = row.lse, factor = row.factor;
@@ -202,7 +202,7 @@ __device__ __forceinline__ void loss_grad_out(const GemmArgs& A, int m, int n, c
 // largest, the sum of exponentials beside it, and the target's (in A.picked[m]), if it is
 // among them.
 template <typename P>
-__device__ __forceinline__ f32x2 row_stats(const GemmArgs& A, const f32x4 (&row)[P::FN], int m, int n, int target)
+__device__ __forceinline__ f32x2 row_stats(const GroupArgs& A, const f32x4 (&row)[P::FN], int m, int n, int target)
 {
     float most = -INFINITY, sum = 0.0f;
     const bool whole = __all(n + (P::FN - 1) * 16 + 4 <= A.N);
@@ -271,7 +271,7 @@ struct Tail {
 
 // Group and place of a tile, counted without parts.
 template <typename P>
-__device__ __forceinline__ void locate(const GemmArgs& A, const GroupTable& table, int lane, int tile, Work* w)
+__device__ __forceinline__ void locate(const GroupArgs& A, const GroupTable& table, int lane, int tile, Work* w)
 {
     constexpr bool kRows = P::GROUP == kRowGroups;
     int band_rows, in;
@@ -496,7 +496,7 @@ __device__ __forceinline__ void eight_columns(const f32x4& a, const f32x4& b, fl
 
 // tiles: of a part, of groups of rows the most that there can be.
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GemmArgs A, const int tiles)
+__global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(const GroupArgs A, const int tiles)
 {
     typedef typename P::T T;
     constexpr bool kRows = P::GROUP == kRowGroups, kSteps = P::GROUP == kStepGroups;
@@ -849,7 +849,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
 // Joins the parts of a split product: a thread takes eight columns of
 // a row of C, all parts in their order.
 template <typename P>
-__global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
+__global__ __launch_bounds__(256) void groups_join_kernel(const GroupArgs A)
 {
     typedef typename P::T T;
     const int chunks = (A.N + 7) / 8;
@@ -876,7 +876,7 @@ __global__ __launch_bounds__(256) void groups_join_kernel(const GemmArgs A)
 // The same of groups of rows, whose parts are matrices of all rows: a wave takes 512 columns of
 // a row, if it is a group's.  Bound by its launch: 5 us for 50 rows of 1024 columns in 14 parts.
 template <typename T, int EPI>
-__global__ __launch_bounds__(256) void rows_join_kernel(const GemmArgs A)
+__global__ __launch_bounds__(256) void rows_join_kernel(const GroupArgs A)
 {
     const int lane = threadIdx.x & 63, stretches = (A.N + 511) / 512, ld = (A.N + 7) & ~7;
     const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -905,7 +905,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(const GemmArgs A)
 // Joins the parts of the last round's tiles: eight blocks a tile, the same number of groups' tiles
 // and of parts as the product found (`tiles` and `blocks` of its launch).  9 to 15 us.
 template <typename P>
-__global__ __launch_bounds__(256) void tail_join_kernel(const GemmArgs A, const int tiles, const int blocks)
+__global__ __launch_bounds__(256) void tail_join_kernel(const GroupArgs A, const int tiles, const int blocks)
 {
     extern __shared__ int table_data[];
     const GroupTable table(table_data, A.groups);
@@ -938,7 +938,7 @@ __global__ __launch_bounds__(256) void tail_join_kernel(const GemmArgs A, const 
 }
 
 template <typename P>
-hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
+hipError_t launch_group_tile(GroupArgs A, hipStream_t s)
 {
     A.tiles_m = (A.M + P::BM - 1) / P::BM;
     A.tiles_n = (A.N + P::kCols - 1) / P::kCols;
@@ -979,7 +979,7 @@ hipError_t launch_group_tile(GemmArgs A, hipStream_t s)
 // statistics of a loss's logits.  Bound by the read of the weights: two experts of 4096 x
 // 10944 in bfloat16 read 359 MB of gate and up weights in 68 us (5.3 TB/s).
 template <typename T, int EPI, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArgs A)
+__global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GroupArgs A)
 {
     typedef typename T::E E;
     typedef typename T::V8 V8;
@@ -1074,7 +1074,7 @@ __global__ __launch_bounds__(64 * WAVES) void skinny_groups_kernel(const GemmArg
 }
 
 template <typename T, int EPI>
-hipError_t launch_skinny_groups_of(const GemmArgs& A, hipStream_t s)
+hipError_t launch_skinny_groups_of(const GroupArgs& A, hipStream_t s)
 {
     const dim3 grid((A.N + 15) / 16, !A.offsets ? 1 : A.groups < A.M ? A.groups : A.M);
     skinny_groups_kernel<T, EPI, 8><<<grid, 512, 0, s>>>(A);
@@ -1082,7 +1082,7 @@ hipError_t launch_skinny_groups_of(const GemmArgs& A, hipStream_t s)
 }
 
 template <typename T>
-hipError_t launch_skinny_groups_t(const GemmArgs& A, Product what, hipStream_t s)
+hipError_t launch_skinny_groups_t(const GroupArgs& A, Product what, hipStream_t s)
 {
     switch (what) {
     case kRowsRows: return launch_skinny_groups_of<T, kPlain>(A, s);
@@ -1093,7 +1093,7 @@ hipError_t launch_skinny_groups_t(const GemmArgs& A, Product what, hipStream_t s
 }
 
 template <typename T, bool ATR, bool BTR, int EPI, int GROUP>
-hipError_t launch_groups_of(const GemmArgs& A, int kind, hipStream_t s)
+hipError_t launch_groups_of(const GroupArgs& A, int kind, hipStream_t s)
 {
     if (A.any) {
         if (kind == kGroup128)
@@ -1111,7 +1111,7 @@ hipError_t launch_groups_of(const GemmArgs& A, int kind, hipStream_t s)
 }
 
 template <typename T>
-hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
+hipError_t launch_groups_t(const GroupArgs& A, Product what, int kind, hipStream_t s)
 {
     switch (what) {
     case kRowsRows: return launch_groups_of<T, false, false, kPlain, kRowGroups>(A, kind, s);
@@ -1124,7 +1124,7 @@ hipError_t launch_groups_t(const GemmArgs& A, Product what, int kind, hipStream_
 }
 
 template <typename T>
-hipError_t launch_loss_t(const GemmArgs& A, Product what, int kind, hipStream_t s)
+hipError_t launch_loss_t(const GroupArgs& A, Product what, int kind, hipStream_t s)
 {
     switch (what) {
     case kLossLogits: return launch_groups_of<T, false, false, kLossStats, kOneGroup>(A, kind, s);

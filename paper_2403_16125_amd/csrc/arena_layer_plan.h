@@ -217,10 +217,11 @@ inline int64_t part_bytes(const Cut& cut, int64_t M, int64_t N, int64_t batch, b
     return 4 * cut.splits * (all - cut.first) * side * side;
 }
 
-inline GemmArgs new_args(int64_t M, int64_t N, int64_t K)
+template <typename Args = GemmArgs>
+inline Args new_args(int64_t M, int64_t N, int64_t K)
 {
-    GemmArgs A;
-    std::memset(&A, 0, sizeof(A));
+    Args A;
+    std::memset((void*)&A, 0, sizeof(A));
     A.M = (int)M;
     A.N = (int)N;
     A.K = (int)K;

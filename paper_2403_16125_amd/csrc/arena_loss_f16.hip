@@ -4,7 +4,7 @@
 namespace arena {
 namespace mm {
 
-hipError_t launch_loss_f16(const GemmArgs& A, Product what, int kind, hipStream_t s)
+hipError_t launch_loss_f16(const GroupArgs& A, Product what, int kind, hipStream_t s)
 {
     return launch_loss_t<F16>(A, what, kind, s);
 }

@@ -15,7 +15,7 @@ using namespace arena::plan;
 using arena::ctx_clear;
 using arena::ctx_fail;
 using arena::LossArgs;
-using arena::mm::GemmArgs;
+using arena::mm::GroupArgs;
 
 namespace {
 
@@ -179,7 +179,7 @@ arena_status arena_cross_entropy_forward(arena_ctx* c, const arena_loss_desc* d,
     const int wide = d->target_dtype == ARENA_I64 ? 8 : 4;
     for (int64_t t = 0; t < d->tokens; t += P.piece) {
         const int64_t n = std::min(P.piece, d->tokens - t);
-        GemmArgs A = new_args(n, d->vocabulary, d->model);
+        GroupArgs A = new_args<GroupArgs>(n, d->vocabulary, d->model);
         A.any = P.any;
         A.a[0] = (const char*)d->x + 2 * t * d->ld_x; A.lda = d->ld_x;
         A.b[0] = d->w; A.ldb = d->ld_w;
@@ -249,7 +249,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
         const int64_t n = std::min(P.piece, V - v);
         const void* w = (const char*)f->w + 2 * v * f->ld_w;
         if (T > 0) {
-            GemmArgs A = new_args(T, n, D);
+            GroupArgs A = new_args<GroupArgs>(T, n, D);
             A.any = P.any;
             A.a[0] = P.x; A.lda = P.ld_x;
             A.b[0] = w; A.ldb = f->ld_w;
@@ -263,7 +263,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
         }
         if (dx) {
             const bool first = v == 0, last = v + n == V;
-            GemmArgs X = new_args(T, D, n);
+            GroupArgs X = new_args<GroupArgs>(T, D, n);
             X.any = P.any;
             X.a[0] = P.g; X.lda = P.ld_g;
             X.b[0] = w; X.ldb = f->ld_w;
@@ -280,7 +280,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
         }
         if (g->dw) {
             char* dw = (char*)g->dw + size * v * g->ld_dw;
-            GemmArgs W = new_args(n, D, T);
+            GroupArgs W = new_args<GroupArgs>(n, D, T);
             W.a[0] = P.g; W.lda = P.ld_g;
             W.b[0] = P.x; W.ldb = P.ld_x;
             W.c[0] = dw; W.ldc = g->ld_dw;
