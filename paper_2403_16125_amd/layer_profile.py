@@ -115,7 +115,9 @@ class FeedForwardLayer:
 class ExpertLayer(FeedForwardLayer):
     """The same with a mixture of `experts` gated blocks: each token goes through the
     `choices` experts whose logits n router^T are largest, their outputs weighted by
-    the softmax over these."""
+    the softmax over these.  With one choice the router has a gradient of zero: its weight
+    is 1, and any other would be taken out again by the norm behind the block, so that only the
+    experts learn."""
 
     def __init__(self, ops: LayerOps, model: int, inner: int, experts: int, choices: int, **given):
         self.experts, self.choices, self.stack = experts, choices, (experts,)
