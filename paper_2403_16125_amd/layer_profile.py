@@ -143,7 +143,8 @@ class ExpertLayer(FeedForwardLayer):
         dys, dweight = ops.combine_backward(dy, ys, plan, weight)
         dxs, *dw = ops.experts_backward(dys, xs, plan.offsets, *self.weights, inner, activation=self.activation)
         dlogits = ops.route_backward(dweight, logits, index)
-        dn = ops.dispatch_backward(dxs, plan) + (dlogits @ self.router).to(n.dtype)
+        # the sum of both is formed in 32 bits
+        dn = (ops.dispatch_backward(dxs, plan) + dlogits @ self.router).to(n.dtype)
         return dn, dw, [dlogits.t() @ n.float()]
 
     def all_to_all_bytes(self, tokens) -> int:

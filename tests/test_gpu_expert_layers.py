@@ -61,3 +61,25 @@ def test_one_choice_has_no_gradient_for_its_router(ops):
     y = exp.route_weight(n @ router.T, e[:, None], False, 1.0) * v
     assert bool((y ** 2).mean(1).min() > 1e-3)
     assert through(ref.norm(y, "rms", 1e-6)[0]) <= 2.0 ** -8 * through(y)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_the_routers_share_of_dn_is_added_in_32_bits(ops, dtype):
+    """dn is the experts' share (a tensor of 16 bits) and the router's in one rounding of their sum: u of it, and what 32
+    bits leave of the router's product of 6 and of the sum."""
+    layer = lp.ExpertLayer(ops, 96, 160, 6, 2, dtype=dtype, seed=5)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n, dy = (torch.randn(200, 96, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    layer.router.mul_(4)        # of the experts' share's size
+    _, kept = layer.block(n)
+    dn, _, _ = layer.block_backward(dy, n, kept)
+    logits, index, weight, plan, xs, ys, inner = kept
+    dys, dweight = ops.combine_backward(dy, ys, plan, weight)
+    dxs, *_ = ops.experts_backward(dys, xs, plan.offsets, *layer.weights, inner)
+    own = ops.dispatch_backward(dxs, plan).double()
+    dlogits = ops.route_backward(dweight, logits, index).double()
+    share, size = dlogits @ layer.router.double(), dlogits.abs() @ layer.router.double().abs()
+    want = own + share
+    off = (dn.double() - want).abs()
+    assert bool((off <= ref.U[dtype] * want.abs() + 8 * 2.0 ** -23 * (size + own.abs()) + ref.TINY[dtype]).all())
+    assert bool((share.abs() > 2.0 ** -4 * own.abs()).float().mean() > 0.5)
