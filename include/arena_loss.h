@@ -46,7 +46,12 @@ arena_status arena_cross_entropy_forward(arena_ctx* ctx, const arena_loss_desc* 
  * bits.  A token whose target is ignore_index has a dx of 0 and no part in dw, whatever
  * its x, lse and dloss hold; any other target outside of the vocabulary makes both NaN.
  * dw is of grad_dtype (dtype or ARENA_F32), accumulate != 0 adds to what it holds.  NULL
- * outputs are not computed. */
+ * outputs are not computed.
+ *
+ * exp(l - lse) is off by lse's own rounding, 2^-24 |lse| of it, so the target's entry of dl is off by
+ * as much of dloss: of a token whose target has all but 1e-6 of the sum, at an lse of 30, it is
+ * rounding for the greater part, and its row of dl need not add up to 0.  loss does not have this error: it is formed
+ * from the sum, not from lse. */
 typedef struct arena_loss_grads {
     int32_t grad_dtype, accumulate;
     const float* dloss; int64_t stride_dloss;
