@@ -41,7 +41,9 @@ arena_status arena_cross_entropy_forward(arena_ctx* ctx, const arena_loss_desc* 
 /* With dloss the losses' gradient (element t at t stride_dloss; 0: one for all),
  *   dl[t, v] = dloss[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),  dx = dl w,  dw = dl^T x.
  * The logits are formed again, in pieces of the vocabulary whose gradient takes at most 256 MB
- * (or 4096 entries), rounded to dtype as the products' operand; in float16 after a power of
+ * (or 4096 entries), rounded to dtype as the products' operand (of up to 32 tokens in two
+ * operands, the second what rounding took off the first; of more a token's dx and dw are off by
+ * the rounding of its entries, most of all its target's: 2^-8 of that in bfloat16, 2^-11 in float16); in float16 after a power of
  * two that brings the largest dloss to about 2^10.  dx is summed over the pieces in 32
  * bits.  A token whose target is ignore_index has a dx of 0 and no part in dw, whatever
  * its x, lse and dloss hold; any other target outside of the vocabulary makes both NaN.

@@ -182,7 +182,8 @@ __device__ __forceinline__ void plain_out(const GroupArgs& A, int z, int m, int 
 
 // factor (exp(l - lse) - [column is the target]), zero for tokens left out of the loss,
 // whatever their logits: rounded to 16 bits as the next two products' operand.
-template <typename T>
+// LOW: for few tokens, what that rounding took off too, as rows of their own.
+template <typename T, bool LOW>
 __device__ __forceinline__ void loss_grad_out(const GroupArgs& A, int m, int n, const float (&v)[8], const LossRow& row)
 {
     typedef typename T::E E;
@@ -195,6 +196,14 @@ __device__ __forceinline__ void loss_grad_out(const GroupArgs& A, int m, int n, 
         g[r] = n + r < A.N && target >= 0 ? factor * p : 0.0f;
     }
     put((E*)A.c[0] + (int64_t)m * A.ldc + n, g, 8);
+    if (LOW && A.low) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const float high = (float)(E)g[r];
+            g[r] = __builtin_fabsf(high) < INFINITY ? g[r] - high : 0.0f;
+        }
+        put((E*)A.c[0] + (int64_t)(m + A.low) * A.ldc + n, g, 8);
+    }
 }
 
 // The statistics of a row's logits as they lie in the sums: a lane has columns 4 (lane >> 4) +
@@ -792,7 +801,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesEach) void groups_kernel(cons
                 } else if constexpr (P::EPI == kWide) {
                     plain_out<T>(A, done.z, m, n, v, side[j]);
                 } else if constexpr (P::EPI == kLossGrad) {
-                    loss_grad_out<T>(A, m, n, v, record);
+                    loss_grad_out<T, P::BM == 64>(A, m, n, v, record);
                 } else {
                     put((typename T::E*)A.c[0] + (int64_t)m * A.ldc + n, v, A.N - n);
                 }

@@ -90,12 +90,13 @@ struct GroupArgs : GemmArgs {
     int32_t e_f32;
     // loss: columns are entries first_col + n of the vocabulary.  Statistics: of each tile
     // column and row the largest logit and the sum of exponentials beside it, at pair
-    // stats[column * M + row], and the logit of target[row]; gradient: c[0]
+    // stats[column * M + row], and the logit of target[row]; gradient: c[0], and what rounding took
+    // off it `low` rows further on, unless 0 (64 x 128 tiles)
     const LossRow* rows;
     const void* target;
     float* stats;
     float* picked;            // [M]
-    int32_t first_col, target_wide;
+    int32_t first_col, target_wide, low;
 };
 
 // Products by the layouts of their operands (rows: k contiguous; cols: m or n
@@ -196,10 +197,13 @@ struct LossArgs {
     int64_t ld_x;
     void* x_to;
     int64_t ld_to;
+    int32_t twice;                // x_to has that copy twice
 };
 
 hipError_t launch_loss_join(const LossArgs& A, hipStream_t s);
 hipError_t launch_loss_rows(const LossArgs& A, hipStream_t s);
+// dx of dtype, rows of ld: the sum of `sum`'s first and second `tokens` rows.
+hipError_t launch_loss_fold(const float* sum, void* dx, int64_t ld, int64_t tokens, int model, int dtype, hipStream_t s);
 
 // Router and tokens to experts.
 constexpr int kRouteMaxExperts = 1024;

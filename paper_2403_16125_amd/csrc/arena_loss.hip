@@ -125,7 +125,17 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(const LossArgs A)
             }
         }
         *(u32x4*)(to + c) = v;
+        if (A.twice) *(u32x4*)(to + A.tokens * A.ld_to + c) = v;
     }
+}
+
+// Both halves of a gradient become one, rounded once.  Bound by its launch.
+template <typename E>
+__global__ __launch_bounds__(256) void loss_fold_kernel(const float* sum, E* dx, int64_t ld, int64_t tokens, int model)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    const int64_t t = blockIdx.y;
+    if (c < model) dx[t * ld + c] = (E)(sum[t * model + c] + sum[(tokens + t) * model + c]);
 }
 
 }  // namespace
@@ -148,6 +158,14 @@ hipError_t launch_loss_rows(const LossArgs& A, hipStream_t s)
         if (e != hipSuccess) return e;
     }
     loss_rows_kernel<<<(unsigned)((A.tokens + 3) / 4), 256, 0, s>>>(A);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_fold(const float* sum, void* dx, int64_t ld, int64_t tokens, int model, int dtype, hipStream_t s)
+{
+    const dim3 grid((unsigned)(model + 255) / 256, (unsigned)tokens);
+    if (dtype == ARENA_BF16) loss_fold_kernel<<<grid, 256, 0, s>>>(sum, (__bf16*)dx, ld, tokens, model);
+    else loss_fold_kernel<<<grid, 256, 0, s>>>(sum, (_Float16*)dx, ld, tokens, model);
     return hipGetLastError();
 }
 

@@ -110,9 +110,19 @@ struct LossPlan {
     }
 };
 
+// Up to how many tokens the logits' gradient is kept in two operands of 16 bits, the second what
+// rounding took off the first.  One entry of a token, its target's, is most of dx and of
+// dw[target], so its rounding would be as much as the results' own.  Both operands' rows are
+// those of one tile of 64, and one step of 64 of the weights' gradient, so the products read and
+// multiply no more (loss with gradients, 131072 x 4096: one token 886 us with one operand, 892 with
+// two; 8 tokens 947 and 971; 32 tokens 980 and 1040; 32 tokens, 5000 x 1024, 54 and 58).  Past that they would.
+constexpr int64_t kFineTokens = 32;
+
 struct LossBackPlan {
     Pieces w;
     bool any;                         // the weight's rows start on any value
+    bool fine;
+    int64_t count;                    // rows of the logits' gradient
     int64_t piece, ld_x, ld_g;        // entries of a piece; rows of the copy of x and of the logits' gradient
     bool many;                        // pieces: dx is summed in 32 bits
     void *rows, *scale, *x, *g, *sum, *part;
@@ -120,21 +130,23 @@ struct LossBackPlan {
         : w(base), any(!Operand::direct(d->w, d->ld_w, d->model))
     {
         const int64_t T = d->tokens, V = d->vocabulary, D = d->model;
+        fine = T > 0 && T <= kFineTokens;
+        count = fine ? 2 * T : T;
         piece = V;
-        if (2 * T * pad8(V) > kGradientBytes)
-            piece = std::min(V, std::max(kLeastPiece, kGradientBytes / (2 * T) / 256 * 256));
+        if (2 * count * pad8(V) > kGradientBytes)
+            piece = std::min(V, std::max(kLeastPiece, kGradientBytes / (2 * count) / 256 * 256));
         many = piece < V;
         ld_x = pad8(D);
         ld_g = pad8(piece);
         rows = w.take(T * (int64_t)sizeof(arena::mm::LossRow));
         scale = w.take(T > 0 && d->dtype == ARENA_F16 ? 8 : 0);
-        x = w.take(2 * T * ld_x);
-        g = w.take(2 * T * ld_g);
-        sum = w.take(many && o->dx ? 4 * T * D : 0);
+        x = w.take(2 * count * ld_x);
+        g = w.take(2 * count * ld_g);
+        sum = w.take((many || fine) && o->dx ? 4 * count * D : 0);
         int64_t most = 0;
         for (int64_t n : {piece, V - (V - 1) / piece * piece}) {
-            if (o->dx && T > 0) most = std::max(most, cut_dx(T, D, n, any).part);
-            if (o->dw) most = std::max(most, cut_dw(T, D, n).part);
+            if (o->dx && T > 0) most = std::max(most, cut_dx(count, D, n, any).part);
+            if (o->dw) most = std::max(most, cut_dw(count, D, n).part);
         }
         part = w.take(most);
     }
@@ -226,7 +238,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
     if ((st = check_loss(c, who, f)) || (st = check_loss_grads(c, who, f, g))) return st;
     const LossBackPlan P(f, g, f->workspace);
     if ((st = check_workspace(c, who, f->workspace, f->workspace_bytes, P.w.used))) return st;
-    const int64_t T = f->tokens, V = f->vocabulary, D = f->model;
+    const int64_t T = f->tokens, V = f->vocabulary, D = f->model, count = P.count;
     const bool dx = g->dx && T > 0, scaled = f->dtype == ARENA_F16 && T > 0;
     if (!dx && !g->dw) return ARENA_OK;
     DeviceScope scope(arena::ctx_device(c));
@@ -242,6 +254,7 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
     L.scale = scaled ? (float*)P.scale : nullptr;
     L.x = f->x; L.ld_x = f->ld_x;
     L.x_to = P.x; L.ld_to = P.ld_x;
+    L.twice = P.fine;
     if ((e = arena::launch_loss_rows(L, s))) return hip_error(c, e, "cross entropy rows launch");
     const float* factor = scaled ? (const float*)P.scale + 1 : nullptr;
     const int size = bytes_of(g->grad_dtype);
@@ -258,12 +271,14 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             A.rows = (const LossRow*)P.rows;
             A.first_col = (int)v;
             A.splits = 1;
-            if ((e = launch_loss(A, f->dtype, kLossGradient, choose_whole(T, n, ceil_div(D, kBK), 2.0, P.any), s)))
+            A.low = P.fine ? (int)T : 0;
+            const int kind = P.fine ? (int)kGroup64x128 : choose_whole(T, n, ceil_div(D, kBK), 2.0, P.any);
+            if ((e = launch_loss(A, f->dtype, kLossGradient, kind, s)))
                 return hip_error(c, e, "cross entropy logits' gradient launch");
         }
         if (dx) {
-            const bool first = v == 0, last = v + n == V;
-            GroupArgs X = new_args<GroupArgs>(T, D, n);
+            const bool first = v == 0, last = v + n == V && !P.fine;
+            GroupArgs X = new_args<GroupArgs>(count, D, n);
             X.any = P.any;
             X.a[0] = P.g; X.lda = P.ld_g;
             X.b[0] = w; X.ldb = f->ld_w;
@@ -273,14 +288,14 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             X.beta = first ? 0.0f : 1.0f;
             X.factor = factor;
             X.part = (float*)P.part;
-            const GroupCut cut = P.cut_dx(T, D, n, P.any);
+            const GroupCut cut = P.cut_dx(count, D, n, P.any);
             X.splits = cut.splits;
             if ((e = launch_loss(X, f->dtype, kRowsCols, cut.kind, s)))
                 return hip_error(c, e, "cross entropy input gradient launch");
         }
         if (g->dw) {
             char* dw = (char*)g->dw + size * v * g->ld_dw;
-            GroupArgs W = new_args<GroupArgs>(n, D, T);
+            GroupArgs W = new_args<GroupArgs>(n, D, count);
             W.a[0] = P.g; W.lda = P.ld_g;
             W.b[0] = P.x; W.ldb = P.ld_x;
             W.c[0] = dw; W.ldc = g->ld_dw;
@@ -292,12 +307,15 @@ arena_status arena_cross_entropy_backward(arena_ctx* c, const arena_loss_desc* f
             }
             W.factor = factor;
             W.part = (float*)P.part;
-            const GroupCut cut = P.cut_dw(T, D, n);
+            const GroupCut cut = P.cut_dw(count, D, n);
             W.splits = cut.splits;
             if ((e = launch_loss(W, f->dtype, kColsCols, cut.kind, s)))
                 return hip_error(c, e, "cross entropy weight gradient launch");
         }
     }
+    if (dx && P.fine &&
+        (e = arena::launch_loss_fold((const float*)P.sum, g->dx, g->ld_dx, T, (int)D, f->dtype, s)))
+        return hip_error(c, e, "cross entropy input gradient fold launch");
     return ARENA_OK;
 }
 

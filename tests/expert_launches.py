@@ -94,6 +94,7 @@ hipError_t launch_combine(const MoveArgs&, int, hipStream_t) { return hipSuccess
 hipError_t launch_combine_backward(const MoveArgs&, int, hipStream_t) { return hipSuccess; }
 hipError_t launch_loss_join(const LossArgs&, hipStream_t) { return hipSuccess; }
 hipError_t launch_loss_rows(const LossArgs&, hipStream_t) { return hipSuccess; }
+hipError_t launch_loss_fold(const float*, void*, int64_t, int64_t, int, int, hipStream_t) { return hipSuccess; }
 namespace mm {
 hipError_t launch_groups(const GroupArgs& A, int dtype, Product what, int kind, hipStream_t)
 {
