@@ -148,7 +148,7 @@ arena_status check_move(arena_ctx* c, const char* who, const arena_move_desc* d)
     return ARENA_OK;
 }
 
-// Row strides here only enter 64-bit products.
+// Row strides here only enter 64-bit products, but the limit is that of all operators.
 arena_status check_rows(arena_ctx* c, const char* who, const char* name, const void* p, int64_t ld, int64_t rows,
                         const arena_move_desc* d)
 {
@@ -294,7 +294,9 @@ GroupCut choose_rows(int64_t rows, int64_t groups, int64_t N, int64_t steps, boo
 }
 
 // The kind of tile and the parts of k for a product of groups of steps, taken to be of
-// one length but for the longest.
+// one length but for the longest, half as long again.  (How much is of little weight: with 1, 1.25, 1.5 and 2
+// times, training takes the same to 1 % at 200 to 16384 rows of 8 experts 1024 x 2752, 1000 to 16384 of 64 experts
+// 2048 x 1408 and 3000 of 8 experts 4096 x 10944.)
 GroupCut choose_steps(int64_t M, int64_t N, int64_t rows, int64_t groups, int pairs, double bytes,
                       bool any)
 {
@@ -637,7 +639,6 @@ arena_status arena_experts_backward(arena_ctx* c, const arena_experts_desc* f, c
         X.splits = P.cut_x.splits;
         X.tail = P.cut_x.tail;
         X.part = (float*)P.part;
-        X.nseg = 2;
         X.a[0] = P.dg; X.a[1] = P.du; X.lda = P.ld;
         X.any = P.any.up;
         X.b[0] = f->w_gate; X.ldb = f->ld_gate; X.sb = f->stride_gate;

@@ -73,8 +73,6 @@ __device__ __forceinline__ int tile_of_xcd(int x, int q, int tiles)
     return r < per + (x < more ? 1 : 0) ? whole * 8 * RUN + x * per + min(x, more) + r : -1;
 }
 
-constexpr int kMostGroups = 1024;
-
 // Of every group its first row or step and its end, and of rows how many tile rows end with
 // the group; in the LDS behind the buffers, as long as there are groups.
 struct GroupTable {
