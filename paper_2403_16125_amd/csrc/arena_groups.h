@@ -13,13 +13,13 @@
 // SIMD with waves that do not, so such a step takes little more than half the time.
 //
 // Large products are bound by the matrix cores and the clock under load, and by last rounds
-// that do not fill the card.  In bfloat16, 16384 rows of 8 experts 4096 x 10944: gate and up
-// 2.73 ms (1080 TFLOP/s), down 1.26 (1170), inner gradients 1.63 (900), weights' gradients 1.33
-// and 2.68 (1100), dx 2.36 (1240), matrix cores busy in 48 to 66 % of the cycles.  A loss of
-// 8192 tokens, 131072 x 4096: logits 6.65 ms (1320), a piece of 16384 entries 0.84 ms for their
-// gradient, 0.82 for dx, 0.80 for dw (1310 to 1380).  With 256 rows an expert (64 of 2048 x 1408)
+// that do not fill the card.  In bfloat16, 16384 rows of 8 experts 4096 x 10944 (medians of six passes;
+// other runs' differ by up to 4 %): gate and up 2.74 ms (1070 TFLOP/s), down 1.24 (1190), inner gradients
+// 1.64 (890), weights' gradients 1.35 and 2.57 (1090 and 1140), dx 2.38 (1230), matrix cores busy in 48 to
+// 66 % of the cycles.  A loss of 8192 tokens, 131072 x 4096: logits 6.63 ms (1330), a piece of 16384 entries
+// 0.85 ms for their gradient, 0.84 for dx, 0.82 for dw (1290 to 1340).  With 256 rows an expert (64 of 2048 x 1408)
 // the weights are read or written once for every two to four tiles and groups waste half a tile:
-// 320 us, 155, 212, 240 + 416 and 296 (430 to 640), matrix cores busy in 25 to 34 %.  Small ones are
+// 323 us, 157, 215, 238 + 445 and 297 (400 to 640), matrix cores busy in 25 to 34 %.  Small ones are
 // bound by latency: about 8 us for the launch, the table, the first loads and the epilogue, and
 // 0.6 to 0.8 for a step.
 #pragma once

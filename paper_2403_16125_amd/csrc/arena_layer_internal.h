@@ -76,7 +76,7 @@ struct GemmArgs {
 
 // The products of groups and of a loss.  A struct of its own: what a kernel is handed is on
 // the path of a short product, and the dense ones take up to 4 % longer with these fields
-// among theirs (of 512 x 512 on 64 x 64 tiles 7.6 us, without 7.3).
+// among theirs (512 x 512 on 64 x 64 tiles 7.6 us, without 7.3).
 struct GroupArgs : GemmArgs {
     int64_t sb1;              // matrices of b[1] lie so many values apart
     // groups: of rows, matrix g of b lies sb values on; of steps, matrix g of c (and e) sc

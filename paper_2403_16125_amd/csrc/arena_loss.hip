@@ -93,7 +93,7 @@ __global__ __launch_bounds__(1024) void loss_scale_kernel(const LossArgs A)
     A.scale[1] = ldexpf(1.0f, -up);
 }
 
-// A wave a token: its record, and its row of x.  Bound by memory: 8192 x 4096 22.9 us, 134 MB.
+// A wave a token: its record, and its row of x.  Bound by memory: 8192 x 4096 23.7 us, 134 MB.
 __global__ __launch_bounds__(256) void loss_rows_kernel(const LossArgs A)
 {
     const int lane = threadIdx.x & 63;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(const LossArgs A)
     }
 }
 
-// Both halves of a gradient become one, rounded once.  Bound by its launch.
+// Both halves of a gradient become one, rounded once.  Bound by its launch: 4.8 us for one token of 4096.
 template <typename E>
 __global__ __launch_bounds__(256) void loss_fold_kernel(const float* sum, E* dx, int64_t ld, int64_t tokens, int model)
 {

@@ -267,6 +267,7 @@ class LayerOps(ExpertOps):
                 if t is not None and t.requires_grad:
                     raise ValueError(f"a tensor of shape {tuple(t.shape)} requires a gradient, which these calls do not "
                                      "record: detach it, or call under torch.no_grad()")
+        # not where the host's tests, which have no GPU to ask, put a stream of their own
         if stream is None and self._handle is not None and self._current is self._torch_current:
             return body(self._handle(self._index), *args)
         current = self._current(self._index)
