@@ -41,19 +41,19 @@ arena_status arena_cross_entropy_forward(arena_ctx* ctx, const arena_loss_desc* 
 /* With dloss the losses' gradient (element t at t stride_dloss; 0: one for all),
  *   dl[t, v] = dloss[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),  dx = dl w,  dw = dl^T x.
  * The logits are formed again, in pieces of the vocabulary whose gradient takes at most 256 MB
- * (or 4096 entries), rounded to dtype as the products' operand (of up to 32 tokens in two
- * operands, the second what rounding took off the first; of more a token's dx and dw are off by
- * the rounding of its entries, most of all its target's: 2^-8 of that in bfloat16, 2^-11 in float16); in float16 after a power of
- * two that brings the largest dloss to about 2^10.  dx is summed over the pieces in 32
- * bits.  A token whose target is ignore_index has a dx of 0 and no part in dw, whatever
- * its x, lse and dloss hold; any other target outside of the vocabulary makes both NaN.
- * dw is of grad_dtype (dtype or ARENA_F32), accumulate != 0 adds to what it holds.  NULL
- * outputs are not computed.
+ * (or 4096 entries), rounded to dtype as the products' operand; in float16 after a power of
+ * two that brings the largest dloss to about 2^10.  Of up to 32 tokens there are two operands, the
+ * second what rounding took off the first; of more a token's dx and dw are off by the rounding of
+ * its entries, most of all its target's: 2^-8 of that in bfloat16, 2^-11 in float16.  dx is
+ * summed over the pieces in 32 bits.  A token whose target is ignore_index has a dx of 0 and no
+ * part in dw, whatever its x, lse and dloss hold; any other target outside of the vocabulary makes
+ * both NaN.  dw is of grad_dtype (dtype or ARENA_F32), accumulate != 0 adds to what it holds.
+ * NULL outputs are not computed.
  *
- * exp(l - lse) is off by lse's own rounding, 2^-24 |lse| of it, so the target's entry of dl is off by
- * as much of dloss: of a token whose target has all but 1e-6 of the sum, at an lse of 30, it is
- * rounding for the greater part, and its row of dl need not add up to 0.  loss does not have this error: it is formed
- * from the sum, not from lse. */
+ * exp(l - lse) is off by lse's own rounding, 2^-24 |lse| of it, so the target's entry of dl is off
+ * by as much of dloss: of a token whose target has all but 1e-6 of the sum, at an lse of 30, it is
+ * rounding for the greater part, and its row of dl need not add up to 0.  loss does not have this
+ * error: it is formed from the sum, not from lse. */
 typedef struct arena_loss_grads {
     int32_t grad_dtype, accumulate;
     const float* dloss; int64_t stride_dloss;

@@ -207,7 +207,7 @@ def draw(rng, most, weights):
         else:
             s = ("loss", typ, size(1, 8192, 1), size(64, 6144, step), size(257, 131072, step), grad, accumulate)
             work, held = 8 * s[2] * s[3] * s[4], s[3] * s[4]
-        if work <= most and held <= weights and 3072 not in s:
+        if work <= most and held <= weights:
             return s
 
 
